@@ -56,6 +56,7 @@ extern "C" {
 /* Score dtypes. */
 #define PAIR_F32 0
 #define PAIR_BF16 1
+#define PAIR_F16 2           /* gradients, caches and queries; scores are fp32 or bf16 */
 
 /* Device status bits (OR-ed into *d_status). */
 #define PAIR_ST_BAD_GROUP 1  /* G_b < 2, G_b > gmax or offsets not monotone    */
@@ -68,6 +69,11 @@ extern "C" {
 #define PAIR_ST_SOLVER 32    /* design: the solver reached its sweep cap or a
                                 search limit before converging; the prompt
                                 fell back to the uniform design               */
+#define PAIR_ST_PAGES 64     /* the page pool is exhausted or its list is full,
+                                a table row is too narrow, or a page or slot is
+                                outside the cache                             */
+#define PAIR_ST_LENGTH 128   /* a negative length, or lengths beyond the bounds
+                                that the call was given                       */
 
 /* Edge-weight rules: the estimator variants compared in the paper's audit and
  * ablation tables (Sec. 6, Tables 2, 4, 5; App. A "Naive selection bias" and
@@ -523,6 +529,160 @@ int pair_audit_exact(int64_t B, int64_t nv, int32_t gmax, const int64_t* offsets
                      const float* p, const float* pi_w, int32_t rule, float wmax, double* mse,
                      double* bias_norm, double* gram, void* workspace, size_t ws_bytes,
                      int32_t* d_status, void* stream);
+
+/*
+ * Continuing the drawn rollouts (paper Algorithm 1: the kept prefixes resume
+ * from their cached keys and values, the others are released).
+ *
+ * The cache is paged: `page` consecutive tokens of one request share a page,
+ * and row r of `table` (int32 [n][ldt]) lists the pages of request r in order,
+ * so that its token at position x lies in slot
+ *     table[r][x / page] * page + x % page.
+ * Keys and values are separate arrays of the same layout, in bf16 or fp16:
+ * element d of head h in slot y is at
+ *     (y / page) * page_stride + (y % page) * slot_stride + h * head_stride + d
+ * (strides in elements, multiples of 8; bases 16-byte aligned).
+ */
+
+/* pair_page_plan_workspace_bytes -- device workspace of pair_page_plan. */
+size_t pair_page_plan_workspace_bytes(int64_t n);
+
+/*
+ * pair_page_plan -- one step's block tables, slot map and page pool, from
+ * request lengths and the completion mask.
+ *
+ * Request r has `cached[r]` tokens in the cache, in its first
+ * h_r = ceil(cached_r / page) table entries, and wants `fresh[r]` more.  Where
+ * mask[r] is 0 the rollout is released: it gets no token and its h_r pages
+ * return to the pool.  Otherwise it needs m_r = ceil((cached_r + fresh_r) /
+ * page) - h_r further pages.  With the pool
+ *     pool = free_pages[0 .. free_count) ++ released pages,
+ * (released pages in request order, each row in table order) request r takes
+ * the m_r entries that follow those of the requests before it, and the rest
+ * of the pool, in order, is the new list.  The result does not depend on
+ * scheduling.
+ *
+ *   n            requests (1 .. 2^24), n * ldt < 2^31
+ *   cached,fresh int32 [n] token counts >= 0
+ *   mask         uint8 [n], 0 = released (or NULL: all continue)
+ *   page         tokens per page >= 1
+ *   table        int32 [n][ldt] in/out: entries h_r .. h_r + m_r - 1 are written
+ *   capacity     entries of free_pages and free_out (the pool's page count)
+ *   free_pages   int32 [capacity] in: the first *free_count are free
+ *   free_count   int64 [1] in (device)
+ *   max_tokens   entries of slots and positions (>= the new tokens; < 2^31)
+ *   q_offsets    int64 [n+1] out: first new token of each request, packed
+ *   lens         int32 [n] out: cached + fresh, 0 for a released request
+ *   slots        int64 [max_tokens] out: slot of each new token, -1 past the last
+ *   positions    int32 [max_tokens] out: position of each, -1 past the last (or NULL)
+ *   free_out     int32 [capacity] out: the new list, -1 past its end
+ *                (not overlapping free_pages)
+ *   free_count_out int64 [1] out
+ *   workspace    device scratch, 256-byte aligned
+ * A request whose lengths are negative or whose table row is too narrow is
+ * left out (no token, no page, length 0); tokens that the pool has no page for
+ * get slot -1 and table entry -1.
+ * Device status: PAIR_ST_PAGES, PAIR_ST_LENGTH.
+ */
+int pair_page_plan(int64_t n, const int32_t* cached, const int32_t* fresh, const uint8_t* mask,
+                   int32_t page, int32_t* table, int64_t ldt, int64_t capacity,
+                   const int32_t* free_pages, const int64_t* free_count, int64_t max_tokens,
+                   int64_t* q_offsets, int32_t* lens, int64_t* slots, int32_t* positions,
+                   int32_t* free_out, int64_t* free_count_out, void* workspace, size_t ws_bytes,
+                   int32_t* d_status, void* stream);
+
+/*
+ * pair_cache_store -- the new tokens' keys and values into their slots.
+ *
+ *   tokens       rows of k and v (>= 0); row t goes to slot slots[t], a
+ *                negative slot is skipped; slots of one call are distinct
+ *   kv_heads, dim  heads and head width (dim a multiple of 8, at most 256)
+ *   dtype        PAIR_BF16 or PAIR_F16
+ *   k, v         element d of head h of row t at t * token_stride +
+ *                h * new_head_stride + d (the same strides for both)
+ *   k_cache, v_cache  the caches (see above), n_pages * page < 2^31
+ * Device status: PAIR_ST_PAGES (a slot beyond the cache; it is skipped).
+ */
+int pair_cache_store(int64_t tokens, int32_t kv_heads, int32_t dim, int32_t dtype, const void* k,
+                     const void* v, int64_t token_stride, int64_t new_head_stride, void* k_cache,
+                     void* v_cache, int64_t page_stride, int64_t slot_stride, int64_t head_stride,
+                     int32_t page, int64_t n_pages, const int64_t* slots, int32_t* d_status,
+                     void* stream);
+
+/* pair_paged_attention_workspace_bytes -- device workspace of pair_paged_attention. */
+size_t pair_paged_attention_workspace_bytes(int64_t n, int64_t tokens, int32_t q_heads,
+                                            int32_t kv_heads, int32_t dim, int32_t max_q,
+                                            int32_t max_len);
+
+/*
+ * pair_paged_attention -- causal attention of each request's new tokens over
+ * its pages, the new tokens' keys included (pair_cache_store comes first).
+ *
+ * Request r has Q_r = q_offsets[r+1] - q_offsets[r] new tokens (one when
+ * decoding, a few drafted ones, or a chunk of a prompt) and lens[r] keys in
+ * all.  Its token i sees key j where j <= lens[r] - Q_r + i; query head h
+ * reads key/value head h / (q_heads / kv_heads):
+ *     s_j = scale * <q, k_j>,   l = sum_j exp(s_j),
+ *     out = sum_j exp(s_j) v_j / l,   lse = log l.
+ * A token that sees no key gets out = 0 and lse = -inf.  What a key or value
+ * that a token does not see holds, NaN and infinities among it, has no
+ * effect on that token.  Scores, statistics and sums are fp32; exp(s_j - m)
+ * is rounded to the type of v for the matrix cores.
+ *
+ *   n, tokens    requests and packed new tokens (rows of q and out)
+ *   q_heads      a multiple of kv_heads, at most 64 * kv_heads
+ *   dim          head width: 64 or 128
+ *   dtype        PAIR_BF16 or PAIR_F16, of q, the caches and out
+ *   q, out       element d of head h of token t at t * q_token + h * q_head + d
+ *                (strides multiples of 8; out likewise)
+ *   table, ldt   int32 [n][ldt]; the first ceil(lens[r] / page) entries of row
+ *                r are read
+ *   q_offsets    int64 [n+1], q_offsets[0] = 0, q_offsets[n] = tokens
+ *   lens         int32 [n]
+ *   max_q, max_len  host bounds on Q_r and lens[r]
+ *   lse          fp32 [tokens][q_heads] out                        (or NULL)
+ *   workspace    device scratch, 256-byte aligned
+ * Device status: PAIR_ST_BAD_GROUP (offsets), PAIR_ST_LENGTH (a request beyond
+ * max_q, max_len or its table row), PAIR_ST_PAGES (a page outside the cache).
+ */
+int pair_paged_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads, int32_t dim,
+                         int32_t dtype, const void* q, int64_t q_token, int64_t q_head,
+                         const void* k_cache, const void* v_cache, int64_t page_stride,
+                         int64_t slot_stride, int64_t head_stride, int32_t page, int64_t n_pages,
+                         const int32_t* table, int64_t ldt, const int64_t* q_offsets,
+                         const int32_t* lens, int32_t max_q, int32_t max_len, float scale,
+                         void* out, int64_t out_token, int64_t out_head, float* lse,
+                         void* workspace, size_t ws_bytes, int32_t* d_status, void* stream);
+
+/* pair_clip_grads_workspace_bytes -- device workspace for `count` tensors. */
+size_t pair_clip_grads_workspace_bytes(int64_t count);
+
+/*
+ * pair_clip_grads -- the 2-norm over a list of gradient tensors, and the
+ * gradients clipped to it:
+ *     norm = sqrt( sum over tensors and elements of g^2 )   (fp64 sums),
+ *     coef = max_norm / norm where norm > max_norm, else 1,
+ *     out  = coef * g, rounded once to the type of out.
+ * If the norm is not finite, coef = 1 and the gradients stay as they are, so
+ * that a step can be skipped by the status word.
+ *
+ *   count        tensors (>= 0)
+ *   grads, outs, sizes, dtypes, out_dtypes   HOST arrays of `count` entries,
+ *                read during the call: device pointers (aligned to an element),
+ *                element counts (>= 0) and PAIR_F32 / PAIR_BF16 / PAIR_F16.
+ *                An out is of the grad's type or fp32.  outs = NULL clips in
+ *                place (out_dtypes is then ignored); nothing is written to a
+ *                gradient in place where coef = 1.  Tensors of one call do
+ *                not overlap, except an out with its own grad of the same type.
+ *   max_norm     > 0; infinity: the norm alone (copies where outs are given)
+ *   norm, coef   fp32 [1] out
+ *   workspace    device scratch, 256-byte aligned
+ * Device status: PAIR_ST_NONFINITE (the norm is not finite).
+ */
+int pair_clip_grads(int64_t count, const void* const* grads, void* const* outs,
+                    const int64_t* sizes, const int32_t* dtypes, const int32_t* out_dtypes,
+                    float max_norm, float* norm, float* coef, void* workspace, size_t ws_bytes,
+                    int32_t* d_status, void* stream);
 
 /* Human-readable text for a return code. */
 const char* pair_strerror(int code);

@@ -10,7 +10,7 @@ import of the library fails loudly (build it with
 ``python -m paper_2608_11368_amd.build``).
 
 The lower-case helpers (``design_inclusion``, ``edge_coeffs``,
-``weighted_grad``, ``audit``) allocate the outputs with torch and call the
+``weighted_grad``, ``audit``, ``page_plan``, ``paged_attention``, ...) allocate the outputs with torch and call the
 ``pair_*`` functions.  Given an explicit ``stream``, a helper makes it torch's
 current stream while it allocates, clears and launches, so the zero-fills are
 ordered before the kernels and the caching allocator hands a temporary
@@ -32,12 +32,15 @@ LIB_PATH = os.environ.get("PAIR_LIB") or os.path.join(_HERE, "libpair.so")
 
 PAIR_F32 = 0
 PAIR_BF16 = 1
+PAIR_F16 = 2
 ST_BAD_GROUP = 1
 ST_RHO_RANGE = 2
 ST_P_RANGE = 4
 ST_NONFINITE = 8
 ST_BUDGET = 16
 ST_SOLVER = 32
+ST_PAGES = 64
+ST_LENGTH = 128
 DESIGN_PAIR = 0
 DESIGN_POINTWISE = 1
 DESIGN_UNIFORM = 2
@@ -56,6 +59,9 @@ EXPORTED = ("pair_design_coeffs", "pair_design_alloc", "pair_design_alloc_ex", "
             "pair_weighted_grad", "pair_audit_workspace_bytes", "pair_audit", "pair_audit_rule",
             "pair_audit_exact_workspace_bytes", "pair_audit_exact",
             "pair_audit_direction_workspace_bytes", "pair_audit_direction", "pair_audit_noalloc",
+            "pair_page_plan_workspace_bytes", "pair_page_plan", "pair_cache_store",
+            "pair_paged_attention_workspace_bytes", "pair_paged_attention",
+            "pair_clip_grads_workspace_bytes", "pair_clip_grads",
             "pair_strerror", "pair_version")
 
 
@@ -119,6 +125,25 @@ def lib() -> ctypes.CDLL:
         L.pair_audit_noalloc.argtypes = [i64, i64, i32, P, i64, P, i32, i64, P, P, P, u64, i64,
                                          i64, P, P, P, P, P, P]
         L.pair_audit_noalloc.restype = ctypes.c_int
+        size = ctypes.c_size_t
+        L.pair_page_plan_workspace_bytes.argtypes = [i64]
+        L.pair_page_plan_workspace_bytes.restype = size
+        L.pair_page_plan.argtypes = [i64, P, P, P, i32, P, i64, i64, P, P, i64, P, P, P, P, P, P,
+                                     P, size, P, P]
+        L.pair_page_plan.restype = ctypes.c_int
+        L.pair_cache_store.argtypes = [i64, i32, i32, i32, P, P, i64, i64, P, P, i64, i64, i64,
+                                       i32, i64, P, P, P]
+        L.pair_cache_store.restype = ctypes.c_int
+        L.pair_paged_attention_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32, i32]
+        L.pair_paged_attention_workspace_bytes.restype = size
+        L.pair_paged_attention.argtypes = [i64, i64, i32, i32, i32, i32, P, i64, i64, P, P, i64,
+                                           i64, i64, i32, i64, P, i64, P, P, i32, i32, f32, P,
+                                           i64, i64, P, P, size, P, P]
+        L.pair_paged_attention.restype = ctypes.c_int
+        L.pair_clip_grads_workspace_bytes.argtypes = [i64]
+        L.pair_clip_grads_workspace_bytes.restype = size
+        L.pair_clip_grads.argtypes = [i64, P, P, P, P, P, f32, P, P, P, size, P, P]
+        L.pair_clip_grads.restype = ctypes.c_int
         L.pair_strerror.argtypes = [ctypes.c_int]
         L.pair_strerror.restype = ctypes.c_char_p
         L.pair_version.argtypes = []
@@ -361,6 +386,138 @@ def pair_audit_exact(B, nv, gmax, offsets, scores, rewards, p, pi_w, rule, wmax,
         _dev(d_status, "d_status", torch.int32, 1, True), _stream(stream)), "pair_audit_exact")
 
 
+_DTYPE_CODE = {torch.float32: PAIR_F32, torch.bfloat16: PAIR_BF16, torch.float16: PAIR_F16}
+
+
+def pair_page_plan_workspace_bytes(n) -> int:
+    return int(lib().pair_page_plan_workspace_bytes(n))
+
+
+def pair_page_plan(n, cached, fresh, mask, page, table, free_pages, free_count, max_tokens,
+                   q_offsets, lens, slots, positions, free_out, free_count_out, workspace,
+                   d_status=None, stream=None):
+    if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[0] < n:
+        raise ValueError("table must be a 2-D tensor with a row for each request")
+    capacity = free_pages.numel()
+    _rc(lib().pair_page_plan(
+        n, _dev(cached, "cached", torch.int32, n), _dev(fresh, "fresh", torch.int32, n),
+        _dev(mask, "mask", torch.uint8, n, True), int(page), _dev(table, "table", torch.int32),
+        table.shape[1], capacity, _dev(free_pages, "free_pages", torch.int32),
+        _dev(free_count, "free_count", torch.int64, 1), int(max_tokens),
+        _dev(q_offsets, "q_offsets", torch.int64, n + 1), _dev(lens, "lens", torch.int32, n),
+        _dev(slots, "slots", torch.int64, max_tokens),
+        _dev(positions, "positions", torch.int32, max_tokens, True),
+        _dev(free_out, "free_out", torch.int32, capacity),
+        _dev(free_count_out, "free_count_out", torch.int64, 1),
+        _dev(workspace, "workspace", torch.uint8), workspace.numel(),
+        _dev(d_status, "d_status", torch.int32, 1, True), _stream(stream)), "pair_page_plan")
+
+
+def _cache_arg(k_cache, v_cache):
+    """Pointers, element type and layout of a key and a value cache."""
+    for name, c in (("k_cache", k_cache), ("v_cache", v_cache)):
+        if not isinstance(c, torch.Tensor) or not c.is_cuda or c.dim() != 4:
+            raise ValueError(f"{name} must be a 4-D CUDA tensor [pages][page][kv_heads][dim]")
+    if k_cache.dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError("the caches must be bfloat16 or float16")
+    if v_cache.dtype != k_cache.dtype or v_cache.shape != k_cache.shape:
+        raise ValueError("k_cache and v_cache must have the same type and shape")
+    if v_cache.stride() != k_cache.stride() or k_cache.stride(3) != 1:
+        raise ValueError("k_cache and v_cache must have the same strides and contiguous rows")
+    return k_cache.data_ptr(), v_cache.data_ptr(), _DTYPE_CODE[k_cache.dtype], k_cache.stride()
+
+
+def _rows_arg(t, name, dtype, heads, dim):
+    """Pointer and strides of rows [tokens][heads][dim]."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 3:
+        raise ValueError(f"{name} must be a 3-D CUDA tensor [tokens][heads][dim]")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, needs {heads} heads of {dim}")
+    if t.stride(2) != 1:
+        raise ValueError(f"{name} rows must be contiguous")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def pair_cache_store(k, v, slots, k_cache, v_cache, d_status=None, stream=None):
+    kc, vc, code, st = _cache_arg(k_cache, v_cache)
+    pages, page, heads, dim = k_cache.shape
+    kp, tok, head = _rows_arg(k, "k", k_cache.dtype, heads, dim)
+    vp, vtok, vhead = _rows_arg(v, "v", k_cache.dtype, heads, dim)
+    if (vtok, vhead) != (tok, head) or v.shape != k.shape:
+        raise ValueError("k and v must have the same shape and strides")
+    tokens = k.shape[0]
+    _rc(lib().pair_cache_store(
+        tokens, heads, dim, code, kp, vp, tok, head, kc, vc, st[0], st[1], st[2], page, pages,
+        _dev(slots, "slots", torch.int64, tokens), _dev(d_status, "d_status", torch.int32, 1, True),
+        _stream(stream)), "pair_cache_store")
+
+
+def pair_paged_attention_workspace_bytes(n, tokens, q_heads, kv_heads, dim, max_q, max_len) -> int:
+    return int(lib().pair_paged_attention_workspace_bytes(n, tokens, q_heads, kv_heads, dim, max_q,
+                                                          max_len))
+
+
+def pair_paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max_len, scale, out,
+                         lse, workspace, d_status=None, stream=None):
+    kc, vc, code, st = _cache_arg(k_cache, v_cache)
+    pages, page, kv_heads, dim = k_cache.shape
+    qp, qt, qh = _rows_arg(q, "q", k_cache.dtype, None, dim)
+    tokens, heads = q.shape[0], q.shape[1]
+    op, ot, oh = _rows_arg(out, "out", k_cache.dtype, heads, dim)
+    n = lens.numel()
+    if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[0] < n:
+        raise ValueError("table must be a 2-D tensor with a row for each request")
+    if out.shape[0] < tokens:
+        raise ValueError(f"out holds {out.shape[0]} tokens, needs {tokens}")
+    _rc(lib().pair_paged_attention(
+        n, tokens, heads, kv_heads, dim, code, qp, qt, qh, kc, vc, st[0], st[1], st[2], page,
+        pages, _dev(table, "table", torch.int32), table.shape[1],
+        _dev(q_offsets, "q_offsets", torch.int64, n + 1), _dev(lens, "lens", torch.int32, n),
+        int(max_q), int(max_len), float(scale), op, ot, oh,
+        _dev(lse, "lse", torch.float32, tokens * heads, True),
+        _dev(workspace, "workspace", torch.uint8), workspace.numel(),
+        _dev(d_status, "d_status", torch.int32, 1, True), _stream(stream)),
+        "pair_paged_attention")
+
+
+def pair_clip_grads_workspace_bytes(count) -> int:
+    return int(lib().pair_clip_grads_workspace_bytes(count))
+
+
+def _grad_table(grads, name):
+    """Host arrays of the tensors' addresses and types for one call."""
+    ptr, size, code = [], [], []
+    for t in grads:
+        if not (t.is_cuda and t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous CUDA (HIP) tensors")
+        if t.dtype not in _DTYPE_CODE:
+            raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+        ptr.append(t.data_ptr())
+        size.append(t.numel())
+        code.append(_DTYPE_CODE[t.dtype])
+    n = len(ptr)
+    return ((ctypes.c_void_p * n)(*ptr), (ctypes.c_int64 * n)(*size), (ctypes.c_int32 * n)(*code),
+            size)
+
+
+def pair_clip_grads(grads, max_norm, norm, coef, workspace, out=None, d_status=None, stream=None):
+    """`out`: None clips in place, else a list of tensors of the gradients'
+    sizes, each of its gradient's type or float32."""
+    gp, sizes, codes, numel = _grad_table(grads, "grads")
+    op = ocodes = None
+    if out is not None:
+        op, _, ocodes, onumel = _grad_table(out, "out")
+        if onumel != numel:
+            raise ValueError("out must hold a tensor of each gradient's size")
+    _rc(lib().pair_clip_grads(
+        len(numel), gp, op, sizes, codes, ocodes, float(max_norm),
+        _dev(norm, "norm", torch.float32, 1), _dev(coef, "coef", torch.float32, 1),
+        _dev(workspace, "workspace", torch.uint8), workspace.numel(),
+        _dev(d_status, "d_status", torch.int32, 1, True), _stream(stream)), "pair_clip_grads")
+
+
 # ------------------------------------------------ allocating helpers -------
 def _nv(offsets):
     return int(offsets[-1].item())
@@ -578,3 +735,79 @@ def cps_draw(offsets, w, n, seed, rep0, R, gmax, nv=None, stream=None):
     pair_cps_draw(B, nv, gmax, offsets, w, n, seed, rep0, R, out["mask"], out["edge_count"],
                   out["status"], stream)
     return out
+
+
+@_allocating
+def page_plan(cached, fresh, table, free_pages, free_count, page, max_tokens, mask=None,
+              stream=None):
+    """One step's block tables and slot map: the requests that `mask` keeps (all
+    without one) get pages for `fresh` new tokens after `cached` ones, the
+    others' pages return to the pool.  `table` int32 [n][entries] is updated in
+    place; `free_pages` int32 lists the pool's pages, the first `free_count`
+    (int64 [1], on the GPU) of them free, and the new list and count come back
+    as `free_pages` and `free_count`.  `max_tokens` bounds the new tokens."""
+    n, dev = cached.numel(), cached.device
+    out = {
+        "q_offsets": torch.empty(n + 1, dtype=torch.int64, device=dev),
+        "lens": torch.empty(n, dtype=torch.int32, device=dev),
+        "slots": torch.empty(max_tokens, dtype=torch.int64, device=dev),
+        "positions": torch.empty(max_tokens, dtype=torch.int32, device=dev),
+        "table": table,
+        "free_pages": torch.empty_like(free_pages),
+        "free_count": torch.empty(1, dtype=torch.int64, device=dev),
+        "status": torch.zeros(1, dtype=torch.int32, device=dev),
+    }
+    ws = torch.empty(pair_page_plan_workspace_bytes(n), dtype=torch.uint8, device=dev)
+    pair_page_plan(n, cached, fresh, mask, page, table, free_pages, free_count, max_tokens,
+                   out["q_offsets"], out["lens"], out["slots"], out["positions"],
+                   out["free_pages"], out["free_count"], ws, out["status"], stream)
+    return out
+
+
+@_allocating
+def cache_store(k, v, slots, k_cache, v_cache, stream=None):
+    """New keys and values [tokens][kv_heads][dim] into their slots of the
+    caches [pages][page][kv_heads][dim]; negative slots are skipped."""
+    st = torch.zeros(1, dtype=torch.int32, device=k_cache.device)
+    pair_cache_store(k, v, slots, k_cache, v_cache, st, stream)
+    return {"k_cache": k_cache, "v_cache": v_cache, "status": st}
+
+
+@_allocating
+def paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max_len, scale=None,
+                    want_lse=False, out=None, workspace=None, stream=None):
+    """Causal attention of the packed new tokens q [tokens][q_heads][dim] over
+    their requests' pages, the new tokens' own keys included.  `max_q` and
+    `max_len` bound a request's new tokens and keys; `scale` defaults to
+    1/sqrt(dim)."""
+    tokens, heads, dim = q.shape
+    dev = q.device
+    if out is None:
+        out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=dev)
+    lse = torch.empty((tokens, heads), dtype=torch.float32, device=dev) if want_lse else None
+    need = pair_paged_attention_workspace_bytes(lens.numel(), tokens, heads, k_cache.shape[2], dim,
+                                                max_q, max_len)
+    if workspace is None or workspace.numel() < need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    st = torch.zeros(1, dtype=torch.int32, device=dev)
+    pair_paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max_len,
+                         dim ** -0.5 if scale is None else scale, out, lse, workspace, st, stream)
+    return {"out": out, "lse": lse, "status": st}
+
+
+@_allocating
+def clip_grads(grads, max_norm, out=None, stream=None):
+    """The gradients' common 2-norm, and the gradients clipped to `max_norm`:
+    in place, or into the tensors of `out`.  A norm that is not finite leaves
+    them as they are and sets ST_NONFINITE."""
+    grads = list(grads)
+    if not grads:
+        raise ValueError("grads is empty")
+    out = None if out is None else list(out)
+    dev = grads[0].device
+    norm = torch.empty(1, dtype=torch.float32, device=dev)
+    coef = torch.empty(1, dtype=torch.float32, device=dev)
+    st = torch.zeros(1, dtype=torch.int32, device=dev)
+    ws = torch.empty(pair_clip_grads_workspace_bytes(len(grads)), dtype=torch.uint8, device=dev)
+    pair_clip_grads(grads, max_norm, norm, coef, ws, out, st, stream)
+    return {"norm": norm, "coef": coef, "out": grads if out is None else out, "status": st}

@@ -31,6 +31,10 @@ int device_cu_count() {
 namespace {
 
 constexpr int64_t kMaxCount = (int64_t)1 << 40;
+constexpr int64_t kMaxTensors = (int64_t)1 << 20;
+constexpr int64_t kMaxRequests = (int64_t)1 << 24;
+constexpr int64_t kMaxSlots = 0x7fffffff;
+constexpr int32_t kMaxHeads = 1024;
 
 bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; }
 
@@ -297,13 +301,186 @@ int pair_audit_noalloc(int64_t B, int64_t nv, int32_t gmax, const int64_t* offse
                                     as_stream(stream));
 }
 
+static bool bad_workspace(const void* workspace, size_t ws_bytes, size_t need) {
+  return workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 ||
+         ws_bytes < need;
+}
+
+size_t pair_clip_grads_workspace_bytes(int64_t count) {
+  return count < 0 || count > kMaxTensors ? 0 : pair::clip_workspace_bytes(count);
+}
+
+int pair_clip_grads(int64_t count, const void* const* grads, void* const* outs,
+                    const int64_t* sizes, const int32_t* dtypes, const int32_t* out_dtypes,
+                    float max_norm, float* norm, float* coef, void* workspace, size_t ws_bytes,
+                    int32_t* d_status, void* stream) {
+  if (count < 0 || count > kMaxTensors) return PAIR_ERANGE;
+  if (norm == nullptr || coef == nullptr) return PAIR_EINVAL;
+  if (count > 0 && (grads == nullptr || sizes == nullptr || dtypes == nullptr)) return PAIR_EINVAL;
+  if (count > 0 && outs != nullptr && out_dtypes == nullptr) return PAIR_EINVAL;
+  if (!(max_norm > 0.0f)) return PAIR_ERANGE;
+  int64_t total = 0;
+  for (int64_t i = 0; i < count; ++i) {
+    const int32_t t = dtypes[i];
+    if (t != PAIR_F32 && t != PAIR_BF16 && t != PAIR_F16) return PAIR_EDTYPE;
+    if (outs != nullptr && out_dtypes[i] != t && out_dtypes[i] != PAIR_F32) return PAIR_EDTYPE;
+    if (sizes[i] < 0 || sizes[i] > kMaxCount || (total += sizes[i]) > kMaxCount) return PAIR_ERANGE;
+    if (sizes[i] == 0) continue;
+    if (grads[i] == nullptr || (outs != nullptr && outs[i] == nullptr)) return PAIR_EINVAL;
+    const uintptr_t unit = t == PAIR_F32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(grads[i]) % unit != 0) return PAIR_EALIGN;
+    if (outs != nullptr &&
+        reinterpret_cast<uintptr_t>(outs[i]) % (out_dtypes[i] == PAIR_F32 ? 4 : 2) != 0)
+      return PAIR_EALIGN;
+  }
+  if (bad_workspace(workspace, ws_bytes, pair::clip_workspace_bytes(count))) return PAIR_EWORKSPACE;
+  return pair::launch_clip(count, grads, outs, sizes, dtypes, out_dtypes, max_norm, norm, coef,
+                           workspace, d_status, as_stream(stream));
+}
+
+size_t pair_page_plan_workspace_bytes(int64_t n) {
+  return n < 1 || n > kMaxRequests ? 0 : pair::page_plan_workspace_bytes(n);
+}
+
+int pair_page_plan(int64_t n, const int32_t* cached, const int32_t* fresh, const uint8_t* mask,
+                   int32_t page, int32_t* table, int64_t ldt, int64_t capacity,
+                   const int32_t* free_pages, const int64_t* free_count, int64_t max_tokens,
+                   int64_t* q_offsets, int32_t* lens, int64_t* slots, int32_t* positions,
+                   int32_t* free_out, int64_t* free_count_out, void* workspace, size_t ws_bytes,
+                   int32_t* d_status, void* stream) {
+  if (cached == nullptr || fresh == nullptr || table == nullptr || free_count == nullptr ||
+      q_offsets == nullptr || lens == nullptr || free_count_out == nullptr)
+    return PAIR_EINVAL;
+  if (n < 1 || n > kMaxRequests || page < 1 || ldt < 1 || ldt > kMaxSlots / n) return PAIR_ERANGE;
+  if (capacity < 0 || capacity > kMaxSlots / page || max_tokens < 0 || max_tokens > kMaxSlots)
+    return PAIR_ERANGE;
+  if (capacity > 0 && (free_pages == nullptr || free_out == nullptr || free_pages == free_out))
+    return PAIR_EINVAL;
+  if (max_tokens > 0 && slots == nullptr) return PAIR_EINVAL;
+  if (bad_workspace(workspace, ws_bytes, pair::page_plan_workspace_bytes(n)))
+    return PAIR_EWORKSPACE;
+  return pair::launch_page_plan(n, cached, fresh, mask, page, table, ldt, capacity, free_pages,
+                                free_count, max_tokens, q_offsets, lens, slots, positions,
+                                free_out, free_count_out, workspace, d_status, as_stream(stream));
+}
+
+// Layout of a paged cache: 16-byte pieces, slots numbered in 31 bits.
+static int check_cache(const void* k_cache, const void* v_cache, int64_t page_stride,
+                       int64_t slot_stride, int64_t head_stride, int32_t page, int64_t n_pages) {
+  if (k_cache == nullptr || v_cache == nullptr) return PAIR_EINVAL;
+  if (page < 1 || n_pages < 1 || n_pages > kMaxSlots / page) return PAIR_ERANGE;
+  if (page_stride < 0 || slot_stride < 0 || head_stride < 0 || page_stride > kMaxCount ||
+      slot_stride > kMaxCount || head_stride > kMaxCount)
+    return PAIR_ERANGE;
+  if (!aligned16(k_cache) || !aligned16(v_cache) || page_stride % 8 != 0 || slot_stride % 8 != 0 ||
+      head_stride % 8 != 0)
+    return PAIR_EALIGN;
+  return PAIR_OK;
+}
+
+int pair_cache_store(int64_t tokens, int32_t kv_heads, int32_t dim, int32_t dtype, const void* k,
+                     const void* v, int64_t token_stride, int64_t new_head_stride, void* k_cache,
+                     void* v_cache, int64_t page_stride, int64_t slot_stride, int64_t head_stride,
+                     int32_t page, int64_t n_pages, const int64_t* slots, int32_t* d_status,
+                     void* stream) {
+  if (dtype != PAIR_BF16 && dtype != PAIR_F16) return PAIR_EDTYPE;
+  if (tokens < 0 || tokens > kMaxSlots || kv_heads < 1 || kv_heads > kMaxHeads || dim < 8 ||
+      dim > 256 || dim % 8 != 0)
+    return PAIR_ERANGE;
+  const int st = check_cache(k_cache, v_cache, page_stride, slot_stride, head_stride, page, n_pages);
+  if (st) return st;
+  if (tokens == 0) return PAIR_OK;
+  if (k == nullptr || v == nullptr || slots == nullptr) return PAIR_EINVAL;
+  if (token_stride < 0 || new_head_stride < 0 || token_stride > kMaxCount ||
+      new_head_stride > kMaxCount)
+    return PAIR_ERANGE;
+  if (!aligned16(k) || !aligned16(v) || token_stride % 8 != 0 || new_head_stride % 8 != 0)
+    return PAIR_EALIGN;
+  const pair::PagedCache cache = {page_stride, slot_stride, head_stride, page, n_pages};
+  return pair::launch_cache_store(tokens, kv_heads, dim, k, v, token_stride, new_head_stride,
+                                  k_cache, v_cache, cache, slots, d_status, as_stream(stream));
+}
+
+static int check_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads,
+                           int32_t dim, int32_t max_q, int32_t max_len) {
+  if (n < 1 || n > kMaxRequests || tokens < 0 || tokens > kMaxSlots) return PAIR_ERANGE;
+  if (kv_heads < 1 || kv_heads > kMaxHeads || q_heads < kv_heads || q_heads % kv_heads != 0 ||
+      q_heads / kv_heads > 64)
+    return PAIR_ERANGE;
+  if (dim != 64 && dim != 128) return PAIR_ERANGE;
+  if (max_q < 0 || max_len < 0 || (tokens > 0 && max_q < 1)) return PAIR_ERANGE;
+  return PAIR_OK;
+}
+
+size_t pair_paged_attention_workspace_bytes(int64_t n, int64_t tokens, int32_t q_heads,
+                                            int32_t kv_heads, int32_t dim, int32_t max_q,
+                                            int32_t max_len) {
+  if (check_attention(n, tokens, q_heads, kv_heads, dim, max_q, max_len)) return 0;
+  return pair::attention_workspace_bytes(n, tokens, q_heads, kv_heads, dim, max_q, max_len);
+}
+
+int pair_paged_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads, int32_t dim,
+                         int32_t dtype, const void* q, int64_t q_token, int64_t q_head,
+                         const void* k_cache, const void* v_cache, int64_t page_stride,
+                         int64_t slot_stride, int64_t head_stride, int32_t page, int64_t n_pages,
+                         const int32_t* table, int64_t ldt, const int64_t* q_offsets,
+                         const int32_t* lens, int32_t max_q, int32_t max_len, float scale,
+                         void* out, int64_t out_token, int64_t out_head, float* lse,
+                         void* workspace, size_t ws_bytes, int32_t* d_status, void* stream) {
+  if (dtype != PAIR_BF16 && dtype != PAIR_F16) return PAIR_EDTYPE;
+  int st = check_attention(n, tokens, q_heads, kv_heads, dim, max_q, max_len);
+  if (st) return st;
+  st = check_cache(k_cache, v_cache, page_stride, slot_stride, head_stride, page, n_pages);
+  if (st) return st;
+  if (table == nullptr || q_offsets == nullptr || lens == nullptr) return PAIR_EINVAL;
+  if (ldt < 1 || ldt > kMaxSlots / n) return PAIR_ERANGE;
+  if (!(scale > 0.0f && scale <= 3.4e38f)) return PAIR_ERANGE;
+  if (tokens == 0) return PAIR_OK;
+  if (q == nullptr || out == nullptr) return PAIR_EINVAL;
+  if (q_token < 0 || q_head < 0 || out_token < 0 || out_head < 0 || q_token > kMaxCount ||
+      q_head > kMaxCount || out_token > kMaxCount || out_head > kMaxCount)
+    return PAIR_ERANGE;
+  if (!aligned16(q) || !aligned16(out) || q_token % 8 != 0 || q_head % 8 != 0 ||
+      out_token % 8 != 0 || out_head % 8 != 0)
+    return PAIR_EALIGN;
+  if (bad_workspace(workspace, ws_bytes, pair::attention_workspace_bytes(
+                                             n, tokens, q_heads, kv_heads, dim, max_q, max_len)))
+    return PAIR_EWORKSPACE;
+  pair::AttnCall c;
+  c.n = n;
+  c.tokens = tokens;
+  c.q_heads = q_heads;
+  c.kv_heads = kv_heads;
+  c.dim = dim;
+  c.bf16 = dtype == PAIR_BF16;
+  c.q = q;
+  c.q_token = q_token;
+  c.q_head = q_head;
+  c.k_cache = k_cache;
+  c.v_cache = v_cache;
+  c.cache = {page_stride, slot_stride, head_stride, page, n_pages};
+  c.table = table;
+  c.ldt = ldt;
+  c.q_offsets = q_offsets;
+  c.lens = lens;
+  c.max_q = max_q;
+  c.max_len = max_len;
+  c.scale = scale;
+  c.out = out;
+  c.out_token = out_token;
+  c.out_head = out_head;
+  c.lse = lse;
+  c.d_status = d_status;
+  return pair::launch_attention(c, workspace, as_stream(stream));
+}
+
 const char* pair_strerror(int code) {
   switch (code) {
     case PAIR_OK: return "ok";
     case PAIR_EINVAL: return "invalid argument (null pointer or malformed size)";
-    case PAIR_EDTYPE: return "unsupported score dtype";
+    case PAIR_EDTYPE: return "unsupported dtype";
     case PAIR_ERANGE: return "size out of the supported range";
-    case PAIR_EALIGN: return "scores base pointer or row stride not 16-byte aligned";
+    case PAIR_EALIGN: return "base pointer or row stride misaligned (16 bytes; gradients: an element)";
     case PAIR_EHIP: return "HIP launch or runtime error";
     case PAIR_EWORKSPACE: return "workspace missing, misaligned or too small";
     case PAIR_ESCRATCH:
@@ -312,6 +489,6 @@ const char* pair_strerror(int code) {
   }
 }
 
-int pair_version(void) { return 300; }   // 0.3.0: pair_audit_noalloc added
+int pair_version(void) { return 400; }   // 0.4.0: paged cache and gradient clipping added
 
 }  // extern "C"

@@ -81,4 +81,57 @@ int launch_audit_direction(int64_t B, int64_t nv, int32_t gmax, const int64_t* o
                            int64_t rep0, int64_t R, double* cosine, double* target_norm,
                            void* workspace, int32_t* d_status, hipStream_t stream);
 
+size_t clip_workspace_bytes(int64_t count);
+
+int launch_clip(int64_t count, const void* const* grads, void* const* outs, const int64_t* sizes,
+                const int32_t* dtypes, const int32_t* out_dtypes, float max_norm, float* norm,
+                float* coef, void* workspace, int32_t* d_status, hipStream_t stream);
+
+size_t page_plan_workspace_bytes(int64_t n);
+
+int launch_page_plan(int64_t n, const int32_t* cached, const int32_t* fresh, const uint8_t* mask,
+                     int32_t page, int32_t* table, int64_t ldt, int64_t capacity,
+                     const int32_t* free_pages, const int64_t* free_count, int64_t max_tokens,
+                     int64_t* q_offsets, int32_t* lens, int64_t* slots, int32_t* positions,
+                     int32_t* free_out, int64_t* free_count_out, void* workspace,
+                     int32_t* d_status, hipStream_t stream);
+
+// A paged cache of 16-bit elements: strides in elements.
+struct PagedCache {
+  int64_t page_stride, slot_stride, head_stride;
+  int32_t page;
+  int64_t n_pages;
+};
+
+int launch_cache_store(int64_t tokens, int32_t kv_heads, int32_t dim, const void* k, const void* v,
+                       int64_t token_stride, int64_t new_head_stride, void* k_cache,
+                       void* v_cache, const PagedCache& cache, const int64_t* slots,
+                       int32_t* d_status, hipStream_t stream);
+
+struct AttnCall {
+  int64_t n, tokens;
+  int32_t q_heads, kv_heads, dim;
+  bool bf16;
+  const void* q;
+  int64_t q_token, q_head;
+  const void* k_cache;
+  const void* v_cache;
+  PagedCache cache;
+  const int32_t* table;
+  int64_t ldt;
+  const int64_t* q_offsets;
+  const int32_t* lens;
+  int32_t max_q, max_len;
+  float scale;
+  void* out;
+  int64_t out_token, out_head;
+  float* lse;
+  int32_t* d_status;
+};
+
+size_t attention_workspace_bytes(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads,
+                                 int32_t dim, int32_t max_q, int32_t max_len);
+
+int launch_attention(const AttnCall& call, void* workspace, hipStream_t stream);
+
 }  // namespace pair

@@ -1,0 +1,420 @@
+// Paged key/value cache: one step's block tables, slot map and page pool from
+// request lengths (pair_page_plan), and the new keys and values into their
+// slots (pair_cache_store).
+#include "paged.hpp"
+
+namespace pair {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// ------------------------------------------------------------------- plan --
+// Three exclusive scans over the requests (new tokens, pages taken, pages
+// given back) settle everything; each output element then finds its request
+// by bisection of the scans' ends.  Sums saturate at 2^31 - 1, beyond every
+// capacity; saturating addition of counts is associative, so the scans may be
+// split anywhere.
+struct PlanArgs {
+  int64_t n;
+  const int32_t* cached;
+  const int32_t* fresh;
+  const uint8_t* mask;
+  FastDiv page;
+  int32_t* table;
+  int64_t ldt;
+  int32_t capacity;
+  const int32_t* free_pages;
+  const int64_t* free_count;
+  int32_t max_tokens;
+  int64_t* q_offsets;
+  int32_t* lens;
+  int64_t* slots;
+  int32_t* positions;
+  int32_t* free_out;
+  int64_t* free_count_out;
+  int32_t* d_status;
+};
+
+struct Counts {
+  uint32_t tokens, taken, given;
+};
+
+__device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) {
+  const uint32_t s = a + b;                     // both at most 2^31 - 1
+  return s < 0x7fffffffu ? s : 0x7fffffffu;
+}
+
+__device__ __forceinline__ Counts operator+(const Counts& a, const Counts& b) {
+  return Counts{sat_add(a.tokens, b.tokens), sat_add(a.taken, b.taken),
+                sat_add(a.given, b.given)};
+}
+
+__device__ __forceinline__ uint32_t pages_of(uint32_t tokens, const FastDiv& page) {
+  return tokens == 0 ? 0u : div_by(tokens - 1, page) + 1;
+}
+
+// What request r takes and gives; its length after the step in *len.
+__device__ __forceinline__ Counts request(const PlanArgs& a, int64_t r, int32_t* len,
+                                          int32_t* bad) {
+  const int32_t c = a.cached[r], f = a.fresh[r];
+  const bool live = a.mask == nullptr || a.mask[r] != 0;
+  Counts k = {0u, 0u, 0u};
+  *len = 0;
+  if (c < 0 || f < 0 || (int64_t)c + f > 0x7fffffff) {
+    *bad |= PAIR_ST_LENGTH;
+    return k;
+  }
+  const uint32_t held = pages_of((uint32_t)c, a.page);
+  const uint32_t all = live ? pages_of((uint32_t)c + (uint32_t)f, a.page) : held;
+  if ((int64_t)all > a.ldt) {
+    *bad |= PAIR_ST_PAGES;
+    return k;
+  }
+  if (live) {
+    k.tokens = (uint32_t)f;
+    k.taken = all - held;
+    *len = c + f;
+  } else {
+    k.given = held;
+  }
+  return k;
+}
+
+__device__ __forceinline__ Counts shfl_up(const Counts& v, int by) {
+  return Counts{(uint32_t)__shfl_up((int)v.tokens, by, kWave),
+                (uint32_t)__shfl_up((int)v.taken, by, kWave),
+                (uint32_t)__shfl_up((int)v.given, by, kWave)};
+}
+
+// Inclusive scan over a workgroup of NT threads; *total the sum of all.
+template <int NT>
+__device__ __forceinline__ Counts group_scan(Counts v, Counts* total) {
+  __shared__ Counts ends[NT / kWave];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+#pragma unroll
+  for (int by = 1; by < kWave; by <<= 1) {
+    const Counts u = shfl_up(v, by);
+    if (lane >= by) v = v + u;
+  }
+  if (lane == kWave - 1) ends[wave] = v;
+  __syncthreads();
+  Counts before = {0u, 0u, 0u}, all = {0u, 0u, 0u};
+#pragma unroll
+  for (int w = 0; w < NT / kWave; ++w) {
+    if (w < wave) before = before + ends[w];
+    all = all + ends[w];
+  }
+  __syncthreads();
+  *total = all;
+  return before + v;
+}
+
+// The scans' ends (inclusive sums), in LDS or in the workspace.
+struct Ends {
+  const uint32_t* tokens;
+  const uint32_t* taken;
+  const uint32_t* given;
+};
+
+// First request of [lo, hi] whose end is beyond x (hi if none before it is).
+__device__ __forceinline__ int owner(const uint32_t* ends, uint32_t x, int lo, int hi) {
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (ends[mid] > x)
+      hi = mid;
+    else
+      lo = mid + 1;
+  }
+  return lo;
+}
+
+// Entry j of the pool: the free list, then the released requests' pages.
+__device__ __forceinline__ int32_t pool_entry(const PlanArgs& a, const Ends& e, uint32_t j,
+                                              uint32_t free, int lo, int hi) {
+  if (j < free) return a.free_pages[j];
+  const uint32_t x = j - free;
+  const int r = owner(e.given, x, lo, hi);
+  const uint32_t at = x - (r > 0 ? e.given[r - 1] : 0u);
+  return a.table[(int64_t)r * a.ldt + at];
+}
+
+__device__ __forceinline__ uint32_t free_pages_of(const PlanArgs& a) {
+  const int64_t f = *a.free_count;
+  return f < 0 ? 0u : (f > a.capacity ? (uint32_t)a.capacity : (uint32_t)f);
+}
+
+constexpr int kTile = 4 * kThreads;   // outputs of a workgroup
+
+// Outputs [tile * kTile, ...) of the tokens, then of the pages (the taken ones
+// into the table, the rest into the new list).
+__device__ void plan_outputs(const PlanArgs& a, const Ends& e, const Counts& total,
+                             int64_t tile, int64_t token_tiles) {
+  const int last = (int)a.n - 1;
+  const uint32_t free = free_pages_of(a);
+  const uint32_t avail = sat_add(free, total.given);
+  if (tile < token_tiles) {
+    const int64_t t0 = tile * kTile;
+    for (int s = 0; s < kTile / kThreads; ++s) {
+      const int64_t t = t0 + s * kThreads + threadIdx.x;
+      if (t >= a.max_tokens) break;
+      int64_t slot = -1;
+      int32_t pos = -1;
+      if ((uint32_t)t < total.tokens) {
+        const int r = owner(e.tokens, (uint32_t)t, 0, last);
+        const uint32_t c = (uint32_t)a.cached[r];
+        const uint32_t x = c + (uint32_t)t - (r > 0 ? e.tokens[r - 1] : 0u);
+        const uint32_t held = pages_of(c, a.page);
+        const uint32_t pg = div_by(x, a.page);
+        int32_t id;
+        if (pg < held) {
+          id = a.table[(int64_t)r * a.ldt + pg];
+        } else {
+          const uint32_t j = (r > 0 ? e.taken[r - 1] : 0u) + (pg - held);
+          id = j < avail ? pool_entry(a, e, j, free, 0, last) : -1;
+        }
+        pos = (int32_t)x;
+        if (id >= 0) slot = (int64_t)id * a.page.d + (x - pg * a.page.d);
+      }
+      a.slots[t] = slot;
+      if (a.positions != nullptr) a.positions[t] = pos;
+    }
+    return;
+  }
+  const int64_t j0 = (tile - token_tiles) * kTile;
+  const uint32_t used = total.taken < avail ? total.taken : avail;
+  for (int s = 0; s < kTile / kThreads; ++s) {
+    const int64_t j = j0 + s * kThreads + threadIdx.x;
+    if (j >= a.capacity) break;
+    const uint32_t from = used + (uint32_t)j;
+    a.free_out[j] = from < avail ? pool_entry(a, e, from, free, 0, last) : -1;
+    if ((uint32_t)j < used) {
+      const int r = owner(e.taken, (uint32_t)j, 0, last);
+      const uint32_t held = pages_of((uint32_t)a.cached[r], a.page);
+      const uint32_t at = held + (uint32_t)j - (r > 0 ? e.taken[r - 1] : 0u);
+      a.table[(int64_t)r * a.ldt + at] = pool_entry(a, e, (uint32_t)j, free, 0, last);
+    }
+  }
+}
+
+// Table entries that the pool has no page for become -1, and what does not fit
+// is reported; thread `i` of `step` of one workgroup.
+__device__ void plan_totals(const PlanArgs& a, const Ends& e, const Counts& total) {
+  const uint32_t free = free_pages_of(a);
+  const uint32_t avail = sat_add(free, total.given);
+  const uint32_t used = total.taken < avail ? total.taken : avail;
+  if (threadIdx.x == 0) {
+    const uint32_t left = avail - used;
+    *a.free_count_out = left < (uint32_t)a.capacity ? left : (uint32_t)a.capacity;
+    if (total.taken > avail || left > (uint32_t)a.capacity) raise_status(a.d_status, PAIR_ST_PAGES);
+    if (total.tokens > (uint32_t)a.max_tokens) raise_status(a.d_status, PAIR_ST_LENGTH);
+  }
+  if (total.taken > used) {
+    const int last = (int)a.n - 1;
+    for (uint32_t j = used + threadIdx.x; j < total.taken; j += blockDim.x) {
+      const int r = owner(e.taken, j, 0, last);
+      const uint32_t held = pages_of((uint32_t)a.cached[r], a.page);
+      a.table[(int64_t)r * a.ldt + held + j - (r > 0 ? e.taken[r - 1] : 0u)] = -1;
+    }
+  }
+}
+
+// Up to kFused requests: every workgroup scans them all (their lengths come
+// from the caches) and writes one tile of the outputs, in one launch.
+constexpr int kFused = 2048;
+
+__global__ __launch_bounds__(kThreads) void plan_fused_kernel(PlanArgs a, int64_t token_tiles) {
+  __shared__ uint32_t ends[3][kFused];
+  const int n = (int)a.n;
+  const int per = (n + kThreads - 1) / kThreads;
+  const int r0 = (int)threadIdx.x * per;
+  const int r1 = r0 + per < n ? r0 + per : n;
+  int32_t bad = 0, len;
+  Counts sum = {0u, 0u, 0u};
+  for (int r = r0; r < r1; ++r) sum = sum + request(a, r, &len, &bad);
+  Counts total;
+  const Counts end = group_scan<kThreads>(sum, &total);
+  // walk back from the inclusive end: saturated sums are past every capacity
+  Counts at = {0u, 0u, 0u};
+  {
+    __shared__ Counts prev[kThreads];
+    prev[threadIdx.x] = end;
+    __syncthreads();
+    if (threadIdx.x > 0) at = prev[threadIdx.x - 1];
+  }
+  const bool first = blockIdx.x == 0;
+  for (int r = r0; r < r1; ++r) {
+    if (first) a.q_offsets[r] = at.tokens;
+    at = at + request(a, r, &len, &bad);
+    ends[0][r] = at.tokens;
+    ends[1][r] = at.taken;
+    ends[2][r] = at.given;
+    if (first) a.lens[r] = len;
+  }
+  __syncthreads();
+  const Ends e = {ends[0], ends[1], ends[2]};
+  if (first) {
+    if (threadIdx.x == 0) a.q_offsets[n] = total.tokens;
+    if (bad) raise_status(a.d_status, bad);
+    plan_totals(a, e, total);
+  }
+  plan_outputs(a, e, total, blockIdx.x, token_tiles);
+}
+
+// More requests: a first launch writes the scans' ends to the workspace.  Each
+// of its workgroups owns kScan requests and sums the ones before them itself,
+// which at 9 bytes a request is less than a second pass would wait for.
+constexpr int kScan = 1024;
+
+__global__ __launch_bounds__(kScan) void plan_scan_kernel(PlanArgs a, uint32_t* ends) {
+  const int64_t r0 = (int64_t)blockIdx.x * kScan;
+  int32_t bad = 0, other = 0, len;
+  Counts sum = {0u, 0u, 0u};
+  for (int64_t r = threadIdx.x; r < r0; r += kScan) sum = sum + request(a, r, &len, &other);
+  Counts before, total;
+  group_scan<kScan>(sum, &before);
+  const int64_t r = r0 + threadIdx.x;
+  Counts mine = {0u, 0u, 0u};
+  if (r < a.n) mine = request(a, r, &len, &bad);
+  const Counts end = before + group_scan<kScan>(mine, &total);
+  if (r < a.n) {
+    ends[r] = end.tokens;
+    ends[a.n + r] = end.taken;
+    ends[2 * a.n + r] = end.given;
+    a.q_offsets[r + 1] = end.tokens;
+    a.lens[r] = len;
+    if (r == 0) a.q_offsets[0] = 0;
+  }
+  if (bad) raise_status(a.d_status, bad);
+}
+
+__global__ __launch_bounds__(kThreads) void plan_write_kernel(PlanArgs a, const uint32_t* ends,
+                                                              int64_t token_tiles) {
+  const Ends e = {ends, ends + a.n, ends + 2 * a.n};
+  const Counts total = {e.tokens[a.n - 1], e.taken[a.n - 1], e.given[a.n - 1]};
+  if (blockIdx.x == 0) plan_totals(a, e, total);
+  plan_outputs(a, e, total, blockIdx.x, token_tiles);
+}
+
+// ------------------------------------------------------------------ store --
+// A copy of 16-byte pieces: piece i of the call is piece i % per_token of
+// token i / per_token, the keys' pieces before the values'.
+constexpr int kStorePieces = 4;   // in flight per lane
+
+struct StoreArgs {
+  const unsigned char* src[2];
+  unsigned char* dst[2];
+  int64_t token_bytes, head_in_bytes;
+  int64_t page_bytes, slot_bytes, head_bytes;
+  FastDiv page, per_token, per_head;
+  uint32_t half;              // pieces of a token's keys
+  int64_t slots_total;
+  const int64_t* slots;
+  int64_t tokens;
+  int32_t* d_status;
+};
+
+__global__ __launch_bounds__(kThreads) void cache_store_kernel(StoreArgs a, int tokens_per_group) {
+  const int64_t t0 = (int64_t)blockIdx.x * tokens_per_group;
+  const int64_t left = a.tokens - t0;
+  const uint32_t n =
+      (uint32_t)(left < tokens_per_group ? left : tokens_per_group) * a.per_token.d;
+  for (uint32_t i0 = threadIdx.x; i0 < n; i0 += kThreads * kStorePieces) {
+    u32x4_t v[kStorePieces];
+    unsigned char* to[kStorePieces];
+#pragma unroll
+    for (int s = 0; s < kStorePieces; ++s) {
+      const uint32_t i = i0 + s * kThreads;
+      to[s] = nullptr;
+      if (i < n) {
+        const uint32_t tok = div_by(i, a.per_token);
+        uint32_t c = i - tok * a.per_token.d;
+        const int64_t slot = a.slots[t0 + tok];
+        const bool value = c >= a.half;
+        if (value) c -= a.half;
+        const uint32_t h = div_by(c, a.per_head);
+        const uint32_t d = (c - h * a.per_head.d) * 16u;
+        if (slot >= a.slots_total) {
+          raise_status(a.d_status, PAIR_ST_PAGES);
+        } else if (slot >= 0) {
+          const uint32_t pg = div_by((uint32_t)slot, a.page);
+          const uint32_t at = (uint32_t)slot - pg * a.page.d;
+          to[s] = (value ? a.dst[1] : a.dst[0]) + pg * a.page_bytes + at * a.slot_bytes +
+                  h * a.head_bytes + d;
+          v[s] = *reinterpret_cast<const u32x4_t*>((value ? a.src[1] : a.src[0]) +
+                                                   (t0 + tok) * a.token_bytes +
+                                                   h * a.head_in_bytes + d);
+        }
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < kStorePieces; ++s)
+      if (to[s] != nullptr) *reinterpret_cast<u32x4_t*>(to[s]) = v[s];
+  }
+}
+
+}  // namespace
+
+size_t page_plan_workspace_bytes(int64_t n) {
+  return ((size_t)n * 3 * sizeof(uint32_t) + 255) / 256 * 256;
+}
+
+int launch_page_plan(int64_t n, const int32_t* cached, const int32_t* fresh, const uint8_t* mask,
+                     int32_t page, int32_t* table, int64_t ldt, int64_t capacity,
+                     const int32_t* free_pages, const int64_t* free_count, int64_t max_tokens,
+                     int64_t* q_offsets, int32_t* lens, int64_t* slots, int32_t* positions,
+                     int32_t* free_out, int64_t* free_count_out, void* workspace,
+                     int32_t* d_status, hipStream_t stream) {
+  const PlanArgs a = {n,         cached,     fresh,          mask,       fast_div((uint32_t)page),
+                      table,     ldt,        (int32_t)capacity, free_pages, free_count,
+                      (int32_t)max_tokens, q_offsets, lens,   slots,      positions,
+                      free_out,  free_count_out, d_status};
+  const int64_t token_tiles = (max_tokens + kTile - 1) / kTile;
+  const int64_t tiles = token_tiles + (capacity + kTile - 1) / kTile;
+  const unsigned grid = (unsigned)(tiles > 0 ? tiles : 1);
+  if (n <= kFused) {
+    hipLaunchKernelGGL(plan_fused_kernel, dim3(grid), dim3(kThreads), 0, stream, a, token_tiles);
+  } else {
+    uint32_t* ends = static_cast<uint32_t*>(workspace);
+    hipLaunchKernelGGL(plan_scan_kernel, dim3((unsigned)((n + kScan - 1) / kScan)), dim3(kScan), 0,
+                       stream, a, ends);
+    if (hipGetLastError() != hipSuccess) return PAIR_EHIP;
+    hipLaunchKernelGGL(plan_write_kernel, dim3(grid), dim3(kThreads), 0, stream, a, ends,
+                       token_tiles);
+  }
+  return hipGetLastError() == hipSuccess ? PAIR_OK : PAIR_EHIP;
+}
+
+int launch_cache_store(int64_t tokens, int32_t kv_heads, int32_t dim, const void* k, const void* v,
+                       int64_t token_stride, int64_t new_head_stride, void* k_cache,
+                       void* v_cache, const PagedCache& cache, const int64_t* slots,
+                       int32_t* d_status, hipStream_t stream) {
+  StoreArgs a;
+  a.src[0] = static_cast<const unsigned char*>(k);
+  a.src[1] = static_cast<const unsigned char*>(v);
+  a.dst[0] = static_cast<unsigned char*>(k_cache);
+  a.dst[1] = static_cast<unsigned char*>(v_cache);
+  a.token_bytes = token_stride * 2;
+  a.head_in_bytes = new_head_stride * 2;
+  a.page_bytes = cache.page_stride * 2;
+  a.slot_bytes = cache.slot_stride * 2;
+  a.head_bytes = cache.head_stride * 2;
+  a.page = fast_div((uint32_t)cache.page);
+  const uint32_t per_head = (uint32_t)dim / 8;
+  a.per_head = fast_div(per_head);
+  a.half = (uint32_t)kv_heads * per_head;
+  a.per_token = fast_div(2 * a.half);
+  a.slots_total = cache.n_pages * cache.page;
+  a.slots = slots;
+  a.tokens = tokens;
+  a.d_status = d_status;
+  // About four pieces a lane, at least one token a workgroup.
+  int per_group = (int)(kThreads * kStorePieces / a.per_token.d);
+  if (per_group < 1) per_group = 1;
+  const int64_t grid = (tokens + per_group - 1) / per_group;
+  hipLaunchKernelGGL(cache_store_kernel, dim3((unsigned)grid), dim3(kThreads), 0, stream, a,
+                     per_group);
+  return hipGetLastError() == hipSuccess ? PAIR_OK : PAIR_EHIP;
+}
+
+}  // namespace pair
