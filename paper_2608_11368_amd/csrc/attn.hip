@@ -6,9 +6,7 @@
 //
 // One wave per token and query head: the lanes take 64 keys at a time, one
 // score each, then add the 64 value rows with a lane for every second element.
-#include <math.h>
-
-#include "paged.hpp"
+#include "attn.hpp"
 
 namespace pair {
 
@@ -107,11 +105,14 @@ __global__ __launch_bounds__(kWave) void attention_row_kernel(AttnCall a, FastDi
 
 }  // namespace
 
-size_t attention_workspace_bytes(int64_t, int64_t, int32_t, int32_t, int32_t, int32_t, int32_t) {
-  return 256;
+size_t attention_workspace_bytes(int64_t n, int64_t, int32_t q_heads, int32_t kv_heads,
+                                 int32_t dim, int32_t max_q, int32_t max_len) {
+  return attention_rows_workspace(n, q_heads, kv_heads, dim, max_q, max_len);
 }
 
-int launch_attention(const AttnCall& a, void*, hipStream_t stream) {
+int launch_attention(const AttnCall& a, void* workspace, hipStream_t stream) {
+  if ((int64_t)a.max_q * (a.q_heads / a.kv_heads) <= kRowsMost)
+    return launch_attention_rows(a, workspace, stream);
   const FastDiv page = fast_div((uint32_t)a.cache.page);
   const dim3 grid((unsigned)a.tokens, (unsigned)a.q_heads);
 #define PAIR_ATTN(BF, D_) \
