@@ -1,0 +1,533 @@
+// Attention of a chunk of new tokens (prompts, chunks of prompts): tiles of 128
+// rows -- a row is one query head of one token, and all rows of a tile share a
+// key/value head -- against steps of 64 keys.  Bound by the matrix cores.
+//
+// A workgroup's four waves own 32 rows each.  Keys and values of a step go
+// through LDS, two steps deep: while one is multiplied, the next is on its way
+// from memory in registers, and one barrier a step suffices.
+//   scores   S^T = K Q^T, so that a lane holds scores of one row only (keys
+//            8 b + 4 h + e of a tile of 32, lane = row + 32 h): the row's maximum
+//            and sum need one exchange between two lanes, and
+//   weights  are, rounded, already the lane's entries of the B operand of
+//   output   O^T += V^T P^T with the product's k index in that order.  The A
+//            operand, four keys of one dim twice, is what the transposing LDS
+//            read returns.
+// LDS rows are stored with their 16-byte pieces permuted by the row number, so
+// that neither the reads of K (32 rows at one place) nor those of V (four rows
+// at two neighbouring places) meet in a bank.
+// The maximum is raised only when a score exceeds it by 2^8 (attn_rows.hip does
+// the same), and steps that every row of a wave sees whole skip the masks.
+//
+// When the tiles are too few for the card, each tile's keys are split and a
+// second launch joins the parts.
+#include "attn.hpp"
+
+namespace pair {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+constexpr int kRows = 32 * kWaves;          // of a tile
+constexpr int kKeys = 64;                   // of a step
+constexpr float kLazy = 8.0f;
+constexpr int kInline = kThreads;           // requests that a workgroup scans itself
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+struct TileArgs {
+  AttnCall a;
+  FastDiv page, group;
+  float scale_log2;
+  int32_t least;        // requests of fewer rows are left to the other kernel
+  int32_t splits;
+  int32_t* starts;      // [n + 1] tiles before each request, if n > kInline
+  float* part_o;        // [tokens][q_heads][splits][dim]
+  float* part_ml;       // [tokens][q_heads][splits][2]
+};
+
+__device__ __forceinline__ int tiles_of(const TileArgs& s, int64_t r, int32_t* bad) {
+  Request q;
+  if (!attention_request(s.a, s.page.d, r, &q, bad)) return 0;
+  const int64_t rows = (int64_t)q.tokens * s.group.d;
+  return rows < s.least ? 0 : (int)((rows + kRows - 1) / kRows);
+}
+
+// Tiles before each request, for the calls of many requests.
+__global__ __launch_bounds__(1024) void tile_starts_kernel(TileArgs s) {
+  __shared__ int32_t ends[1024 / kWave];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  int32_t carry = 0, bad = 0;
+  for (int64_t r0 = 0; r0 < s.a.n; r0 += 1024) {
+    const int64_t r = r0 + threadIdx.x;
+    int32_t scan = r < s.a.n ? tiles_of(s, r, &bad) : 0;
+#pragma unroll
+    for (int by = 1; by < kWave; by <<= 1) {
+      const int32_t v = __shfl_up(scan, by, kWave);
+      if (lane >= by) scan += v;
+    }
+    if (lane == kWave - 1) ends[wave] = scan;
+    __syncthreads();
+    int32_t all = 0;
+#pragma unroll
+    for (int w = 0; w < 1024 / kWave; ++w) {
+      if (w < wave) scan += ends[w];
+      all += ends[w];
+    }
+    if (r < s.a.n) s.starts[r + 1] = carry + scan;
+    carry += all;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) s.starts[0] = 0;
+  if (bad) raise_status(s.a.d_status, bad);
+}
+
+// The request of tile `back` from the end, and the tile's number in it; false
+// past the first tile.  The last tiles of a request see the most keys, so the
+// order starts with them.
+__device__ __forceinline__ bool find_tile(const TileArgs& s, int64_t back, int64_t* request,
+                                          int* tile) {
+  __shared__ int32_t start[kInline + 1];
+  __shared__ int32_t ends[kWaves];
+  const int n = (int)s.a.n, lane = threadIdx.x & (kWave - 1);
+  if (n <= kInline) {
+    int32_t bad = 0;
+    const int32_t mine = (int)threadIdx.x < n ? tiles_of(s, threadIdx.x, &bad) : 0;
+    if (bad && blockIdx.x == 0) raise_status(s.a.d_status, bad);
+    int32_t scan = mine;
+#pragma unroll
+    for (int by = 1; by < kWave; by <<= 1) {
+      const int32_t v = __shfl_up(scan, by, kWave);
+      if (lane >= by) scan += v;
+    }
+    if (lane == kWave - 1) ends[threadIdx.x / kWave] = scan;
+    if (threadIdx.x == 0) start[0] = 0;
+    __syncthreads();
+    for (int w = 0; w < (int)threadIdx.x / kWave; ++w) scan += ends[w];
+    start[threadIdx.x + 1] = scan;
+    __syncthreads();
+    const int64_t t = start[kInline] - 1 - back;
+    if (t < 0) return false;
+    const int r = __syncthreads_count(start[threadIdx.x + 1] <= t);
+    *request = r;
+    *tile = uniform((int)t - start[r]);
+    return true;
+  }
+  const int64_t t = (int64_t)s.starts[n] - 1 - back;
+  if (t < 0) return false;
+  int lo = 0, hi = n;                       // starts[lo] <= t < starts[hi]
+  while (hi - lo > 1) {
+    const int step = (hi - lo + kThreads - 1) / kThreads;
+    const int at = lo + ((int)threadIdx.x + 1) * step;
+    const int below = __syncthreads_count(at < hi && s.starts[at] <= t);
+    const int top = lo + (below + 1) * step;
+    lo += below * step;
+    hi = top < hi ? top : hi;
+  }
+  *request = uniform(lo);
+  *tile = uniform((int)(t - s.starts[lo]));
+  return true;
+}
+
+// 16-byte piece `c` of LDS row `row` of a step's keys, and of its values.
+template <int DIM>
+__device__ __forceinline__ int key_piece(int row, int c) {
+  return row * (DIM * 2) + ((c ^ (row & (DIM / 8 - 1))) << 4);
+}
+template <int DIM>
+__device__ __forceinline__ int value_piece(int row, int c) {
+  const int f = DIM == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2;
+  return row * (DIM * 2) + ((c ^ f) << 4);
+}
+
+// A step whose values are not all finite, and not all seen by every row: a
+// weight of zero would not keep a NaN or an infinity out of the matrix
+// product.  The weights go through LDS (over the keys, which are done with)
+// and each row adds the values that it sees, one key at a time.
+template <bool BF16, int DIM>
+__device__ __forceinline__ void add_odd_step(unsigned char* keys, const unsigned char* values,
+                                             const u32x4_t (&pf)[4], int kb, int limit,
+                                             f32x16_t (*acc)[DIM / 32]) {
+  const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
+  const int x = lane & 31, h = lane >> 5;
+  uint32_t* weights = reinterpret_cast<uint32_t*>(keys) + (wave * 32 + x) * (kKeys / 2);
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) weights[8 * u + 4 * (w >> 1) + 2 * h + (w & 1)] = pf[u][w];
+  __syncthreads();
+#pragma unroll 1
+  for (int k = 0; k < kKeys; ++k) {
+    const float p = half_value<BF16>((weights[k >> 1] >> (16 * (k & 1))) & 0xffffu);
+    const bool seen = kb + k <= limit;
+#pragma unroll
+    for (int d = 0; d < DIM / 32; ++d)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const u32x2_t v = *reinterpret_cast<const u32x2_t*>(
+            values + value_piece<DIM>(k, 4 * d + b) + 8 * h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (seen)
+            (*acc)[d][4 * b + e] = __builtin_fmaf(
+                p, half_value<BF16>((v[e >> 1] >> (16 * (e & 1))) & 0xffffu), (*acc)[d][4 * b + e]);
+      }
+  }
+  __syncthreads();
+}
+
+template <bool BF16, int DIM, bool ALIGNED>
+__global__ __launch_bounds__(kThreads, 2) void attention_tiles_kernel(TileArgs s) {
+  constexpr int NC = DIM / 16;              // k pieces of a score product
+  constexpr int ND = DIM / 32;              // dim tiles of the output
+  constexpr int kPer = DIM / 8;             // 16-byte pieces of a row
+  constexpr int kStage = kKeys * kPer / kThreads;   // pieces of a lane per step
+  constexpr int kStep = kThreads / kPer;    // rows between a lane's pieces
+  // add_odd_step lays 16 KiB of weights over both key steps
+  static_assert(kRows * kKeys * 2 <= 2 * kKeys * DIM * 2, "weights of a step");
+  __shared__ __align__(16) unsigned char kt[2][kKeys * DIM * 2];
+  __shared__ __align__(16) unsigned char vt[2][kKeys * DIM * 2];
+
+  // heads fastest: consecutive workgroups go to the XCDs in turn, so that with
+  // 8 (4, 2) key heads each XCD's cache holds one (two, four) of them
+  const int64_t heads = s.a.kv_heads;
+  const int kvh = (int)(blockIdx.x % heads);
+  const int split = (int)((blockIdx.x / heads) % s.splits);
+  int64_t r;
+  int tile;
+  if (!find_tile(s, blockIdx.x / (heads * s.splits), &r, &tile)) return;
+  Request q;
+  int32_t bad = 0;
+  if (!attention_request(s.a, s.page.d, r, &q, &bad)) return;
+  const int rows = q.tokens * (int)s.group.d;
+  const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
+  const int x = lane & 31, h = lane >> 5;
+
+  // this lane's row, and the keys that the wave and the tile see
+  const int i = tile * kRows + wave * 32 + x;
+  const int tok = (int)div_by((uint32_t)i, s.group);
+  const int qh = kvh * (int)s.group.d + i - tok * (int)s.group.d;
+  const int limit = i < rows ? limit_of(q, tok) : -1;
+  const int i_first = tile * kRows + wave * 32;
+  const int first_limit = limit_of(q, (int)div_by((uint32_t)i_first, s.group));
+  int i_last = tile * kRows + kRows - 1;
+  if (i_last >= rows) i_last = rows - 1;
+  int keys = limit_of(q, (int)div_by((uint32_t)i_last, s.group)) + 1;
+  if (keys < 0) keys = 0;
+  int k0 = 0, k1 = keys;
+  if (s.splits > 1) {
+    const int part = ((keys + s.splits - 1) / s.splits + kKeys - 1) / kKeys * kKeys;
+    k0 = split * part < keys ? split * part : keys;
+    k1 = k0 + part < keys ? k0 + part : keys;
+  }
+
+  u32x4_t qf[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) qf[c] = u32x4_t{0u, 0u, 0u, 0u};
+  if (i < rows) {
+    const uint16_t* p = static_cast<const uint16_t*>(s.a.q) + (q.q0 + tok) * s.a.q_token +
+                        qh * s.a.q_head + h * 8;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) qf[c] = *reinterpret_cast<const u32x4_t*>(p + c * 16);
+  }
+  f32x16_t acc[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[d][e] = 0.0f;
+  float m = -INFINITY, l = 0.0f;            // l: this lane's keys only
+
+  const int64_t head = kvh * s.a.cache.head_stride * 2;
+  const unsigned char* kbase = static_cast<const unsigned char*>(s.a.k_cache) + head;
+  const unsigned char* vbase = static_cast<const unsigned char*>(s.a.v_cache) + head;
+  const int64_t slot_bytes = s.a.cache.slot_stride * 2, page_bytes = s.a.cache.page_stride * 2;
+  const int32_t* table = s.a.table + r * s.a.ldt;
+  const int my_row = (int)threadIdx.x / kPer, my_piece = (int)threadIdx.x % kPer;
+  constexpr int kWaveRows = kWave / kPer;   // rows of a wave's load, in one page
+
+  u32x4_t ks[kStage], vs[kStage];
+  auto fetch = [&](int kb) {
+#pragma unroll
+    for (int p = 0; p < kStage; ++p) {
+      int64_t at;
+      if (ALIGNED) {
+        // a run of 16 keys lies in one page; one past the end repeats the last
+        int key = kb + p * kStep + wave * kWaveRows;
+        if (key >= q.len) key = ((q.len - 1) & ~15) + (key & 15);
+        const uint32_t pg = div_by((uint32_t)key, s.page);
+        at = checked_page(s.a, table[pg]) * page_bytes +
+             (int64_t)((uint32_t)key - pg * s.page.d) * slot_bytes +
+             (lane / kPer) * slot_bytes;
+      } else {
+        int key = kb + p * kStep + my_row;
+        if (key >= q.len) key = q.len - 1;
+        const uint32_t pg = div_by((uint32_t)key, s.page);
+        at = checked_page(s.a, table[pg]) * page_bytes +
+             (int64_t)((uint32_t)key - pg * s.page.d) * slot_bytes;
+      }
+      ks[p] = *reinterpret_cast<const u32x4_t*>(kbase + at + my_piece * 16);
+      vs[p] = *reinterpret_cast<const u32x4_t*>(vbase + at + my_piece * 16);
+    }
+  };
+  // Into LDS, and a barrier; whether a step that some row does not see whole
+  // holds a value that is not finite.
+  const int tile_limit = limit_of(q, (int)div_by((uint32_t)(tile * kRows), s.group));
+  auto park = [&](int kb, int buf) {
+    const bool edge = kb + kKeys - 1 > tile_limit;
+    uint32_t bad = 0;
+#pragma unroll
+    for (int p = 0; p < kStage; ++p) {
+      const int row = p * kStep + my_row;
+      if (edge) {
+        if (kb + row >= q.len) vs[p] = u32x4_t{0u, 0u, 0u, 0u};   // no value at all
+#pragma unroll
+        for (int w = 0; w < 4; ++w) bad |= not_finite<BF16>(vs[p][w]) ? 1u : 0u;
+      }
+      *reinterpret_cast<u32x4_t*>(kt[buf] + key_piece<DIM>(row, my_piece)) = ks[p];
+      *reinterpret_cast<u32x4_t*>(vt[buf] + value_piece<DIM>(row, my_piece)) = vs[p];
+    }
+    if (edge) return __syncthreads_or((int)bad) != 0;
+    __syncthreads();
+    return false;
+  };
+
+  if (k0 < k1) fetch(k0);
+  for (int kb = k0, buf = 0; kb < k1; kb += kKeys, buf ^= 1) {
+    const bool odd = park(kb, buf);
+    if (kb + kKeys < k1) fetch(kb + kKeys);
+
+    f32x16_t sc[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[t][e] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const u32x4_t kf =
+            *reinterpret_cast<const u32x4_t*>(kt[buf] + key_piece<DIM>(32 * t + x, 2 * c + h));
+        sc[t] = mma32<BF16>(kf, qf[c], sc[t]);
+      }
+    }
+    const bool masked = kb + kKeys - 1 > first_limit;
+    if (masked) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (kb + 32 * t + 8 * (e >> 2) + 4 * h + (e & 3) > limit) sc[t][e] = -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[t][e]);
+    top *= s.scale_log2;
+    if (__any(top > m + kLazy)) {
+      top = fmaxf(top, __shfl_xor(top, 32, kWave));
+      const float mn = fmaxf(m, top);
+      const float keep = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= keep;
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[d][e] *= keep;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;
+    u32x4_t pf[4];
+    float part = 0.0f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        const float a =
+            __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][2 * w], s.scale_log2, -base));
+        const float b =
+            __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][2 * w + 1], s.scale_log2, -base));
+        part += a + b;
+        pf[2 * t + (w >> 2)][w & 3] = pack2<BF16>(a, b);
+      }
+    l += part;
+
+    if (odd) {
+      add_odd_step<BF16, DIM>(kt[0], vt[buf], pf, kb, limit, &acc);
+      continue;
+    }
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {         // 16 keys at a time
+        u32x4_t vf;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int row = 16 * u + 8 * half + 4 * h + ((lane & 15) >> 2);
+          const int at = value_piece<DIM>(row, 4 * d + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) +
+                         (lane & 1) * 8;
+          const s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) s16x4_t*)(vt[buf] + at));
+          const u32x2_t b = __builtin_bit_cast(u32x2_t, v);
+          vf[2 * half] = b[0];
+          vf[2 * half + 1] = b[1];
+        }
+        acc[d] = mma32<BF16>(vf, pf[u], acc[d]);
+      }
+  }
+
+  if (i >= rows) return;
+  l += __shfl_xor(l, 32, kWave);
+  const int64_t row = (q.q0 + tok) * s.a.q_heads + qh;
+  if (s.splits > 1) {
+    const int64_t at = row * s.splits + split;
+    if (h == 0) {
+      s.part_ml[2 * at] = m;
+      s.part_ml[2 * at + 1] = l;
+    }
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        *reinterpret_cast<f32x4_t*>(s.part_o + at * DIM + 32 * d + 8 * b + 4 * h) =
+            f32x4_t{acc[d][4 * b], acc[d][4 * b + 1], acc[d][4 * b + 2], acc[d][4 * b + 3]};
+    return;
+  }
+  const bool none = limit < 0;
+  const float inv = 1.0f / l;
+  uint16_t* o = static_cast<uint16_t*>(s.a.out) + (q.q0 + tok) * s.a.out_token + qh * s.a.out_head;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      u32x2_t w;
+      w[0] = none ? 0u : pack2<BF16>(acc[d][4 * b] * inv, acc[d][4 * b + 1] * inv);
+      w[1] = none ? 0u : pack2<BF16>(acc[d][4 * b + 2] * inv, acc[d][4 * b + 3] * inv);
+      *reinterpret_cast<u32x2_t*>(o + 32 * d + 8 * b + 4 * h) = w;
+    }
+  if (s.a.lse != nullptr && h == 0)
+    s.a.lse[row] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718056f;
+}
+
+// Joins a row's parts: one wave a row.
+template <bool BF16, int DIM>
+__global__ __launch_bounds__(kThreads) void join_tiles_kernel(TileArgs s) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const int64_t row = (int64_t)blockIdx.x * kWaves + uniform(threadIdx.x / kWave);
+  const int64_t t = row / s.a.q_heads;
+  const int qh = (int)(row - t * s.a.q_heads);
+  if (t >= s.a.tokens) return;
+  int64_t lo = 0, hi = s.a.n - 1;           // the token's request
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (s.a.q_offsets[mid + 1] > t)
+      hi = mid;
+    else
+      lo = mid + 1;
+  }
+  Request q;
+  int32_t bad = 0;
+  if (!attention_request(s.a, s.page.d, lo, &q, &bad)) return;
+  if (t < q.q0 || t >= q.q0 + q.tokens || (int64_t)q.tokens * s.group.d < s.least) return;
+  constexpr int PER = DIM / kWave;
+  const int64_t at = row * s.splits;
+  float m = -INFINITY;
+  for (int p = 0; p < s.splits; ++p) m = fmaxf(m, s.part_ml[2 * (at + p)]);
+  const float base = m == -INFINITY ? 0.0f : m;
+  float l = 0.0f, o[PER];
+#pragma unroll
+  for (int e = 0; e < PER; ++e) o[e] = 0.0f;
+  for (int p = 0; p < s.splits; ++p) {
+    const float mp = s.part_ml[2 * (at + p)], lp = s.part_ml[2 * (at + p) + 1];
+    if (mp == -INFINITY && lp == 0.0f) continue;          // saw no key
+    const float f = __builtin_amdgcn_exp2f(mp - base);
+    l = __builtin_fmaf(lp, f, l);
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+      o[e] = __builtin_fmaf(s.part_o[(at + p) * DIM + lane * PER + e], f, o[e]);
+  }
+  const bool none = limit_of(q, (int)(t - q.q0)) < 0;
+  const float inv = 1.0f / l;
+  uint16_t* to = static_cast<uint16_t*>(s.a.out) + t * s.a.out_token + qh * s.a.out_head;
+  if (PER == 2) {
+    *reinterpret_cast<uint32_t*>(to + 2 * lane) =
+        none ? 0u : pack2<BF16>(o[0] * inv, o[PER - 1] * inv);
+  } else {
+    to[lane] = none ? (uint16_t)0 : (uint16_t)pack2<BF16>(o[0] * inv, 0.0f);
+  }
+  if (s.a.lse != nullptr && lane == 0)
+    s.a.lse[row] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718056f;
+}
+
+struct Plan {
+  int64_t tiles;        // bound on the tiles of one head
+  int32_t splits;
+  size_t starts, ml, total;
+};
+
+Plan plan_tiles(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads, int32_t dim,
+                int32_t max_len) {
+  Plan p;
+  p.tiles = tokens * (q_heads / kv_heads) / kRows + (n < tokens ? n : tokens);
+  // Two workgroups fit a compute unit.  Fewer tiles than that are split along
+  // the keys, down to eight steps a part.
+  const int64_t slots = 2 * (int64_t)device_cu_count();
+  int64_t split = slots / (p.tiles * kv_heads > 0 ? p.tiles * kv_heads : 1);
+  const int64_t most = ((int64_t)max_len + 8 * kKeys - 1) / (8 * kKeys);
+  if (split > most) split = most;
+  if (split > 32) split = 32;
+  p.splits = (int32_t)(split < 1 ? 1 : split);
+  p.starts = n > kInline ? ((size_t)(n + 1) * 4 + 255) / 256 * 256 : 0;
+  const size_t parts = p.splits > 1 ? (size_t)tokens * q_heads * p.splits : 0;
+  p.ml = (parts * 8 + 255) / 256 * 256;
+  p.total = p.starts + p.ml + parts * dim * 4 + 256;
+  return p;
+}
+
+template <bool BF16, int DIM>
+int launch(const TileArgs& s, const Plan& p, hipStream_t stream) {
+  const int64_t grid = p.tiles * s.a.kv_heads * p.splits;
+  if (grid > 0x7fffffffLL) return PAIR_ERANGE;
+  if (s.a.n > kInline) {
+    hipLaunchKernelGGL(tile_starts_kernel, dim3(1), dim3(1024), 0, stream, s);
+    if (hipGetLastError() != hipSuccess) return PAIR_EHIP;
+  }
+  if (s.page.d % 16 == 0)
+    hipLaunchKernelGGL((attention_tiles_kernel<BF16, DIM, true>), dim3((unsigned)grid),
+                       dim3(kThreads), 0, stream, s);
+  else
+    hipLaunchKernelGGL((attention_tiles_kernel<BF16, DIM, false>), dim3((unsigned)grid),
+                       dim3(kThreads), 0, stream, s);
+  if (hipGetLastError() != hipSuccess) return PAIR_EHIP;
+  if (p.splits > 1) {
+    const int64_t rows = s.a.tokens * s.a.q_heads;
+    hipLaunchKernelGGL((join_tiles_kernel<BF16, DIM>), dim3((unsigned)((rows + kWaves - 1) / kWaves)),
+                       dim3(kThreads), 0, stream, s);
+  }
+  return hipGetLastError() == hipSuccess ? PAIR_OK : PAIR_EHIP;
+}
+
+}  // namespace
+
+size_t attention_tiles_workspace(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads,
+                                 int32_t dim, int32_t max_len) {
+  return plan_tiles(n, tokens, q_heads, kv_heads, dim, max_len).total;
+}
+
+int launch_attention_tiles(const AttnCall& a, int32_t least_rows, void* workspace,
+                           hipStream_t stream) {
+  const Plan p = plan_tiles(a.n, a.tokens, a.q_heads, a.kv_heads, a.dim, a.max_len);
+  TileArgs s;
+  s.a = a;
+  s.page = fast_div((uint32_t)a.cache.page);
+  s.group = fast_div((uint32_t)(a.q_heads / a.kv_heads));
+  s.scale_log2 = a.scale * 1.44269504089f;
+  s.least = least_rows;
+  s.splits = p.splits;
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  s.starts = reinterpret_cast<int32_t*>(ws);
+  s.part_ml = reinterpret_cast<float*>(ws + p.starts);
+  s.part_o = reinterpret_cast<float*>(ws + p.starts + p.ml);
+  if (a.dim == 64) return a.bf16 ? launch<true, 64>(s, p, stream) : launch<false, 64>(s, p, stream);
+  return a.bf16 ? launch<true, 128>(s, p, stream) : launch<false, 128>(s, p, stream);
+}
+
+}  // namespace pair
