@@ -92,14 +92,19 @@ __device__ __forceinline__ int limit_of(const Request& q, int token) {
   return q.len - q.tokens + token;
 }
 
-// A page id that may be used as an index: one outside the cache is reported and
-// replaced by page 0 (the request's results are then unspecified).
-__device__ __forceinline__ int32_t checked_page(const AttnCall& a, int32_t id) {
-  if ((uint32_t)id >= (uint32_t)a.cache.n_pages) {
-    raise_status(a.d_status, PAIR_ST_PAGES);
-    return 0;
-  }
-  return id;
+// Entry `i` (wave-uniform) of a table row, by a scalar load: nothing that runs
+// beside the attention writes the table.
+__device__ __forceinline__ int32_t table_entry(const int32_t* row, uint32_t i) {
+  typedef const __attribute__((address_space(4))) int32_t* scalar_ptr;
+  return ((scalar_ptr)(uintptr_t)row)[i];
+}
+
+// A page id that may be used as an index: one outside the cache is counted in
+// *bad and replaced by page 0 (the request's results are then unspecified).
+__device__ __forceinline__ int32_t checked_page(const AttnCall& a, int32_t id, int32_t* bad) {
+  const bool ok = (uint32_t)id < (uint32_t)a.cache.n_pages;
+  *bad |= ok ? 0 : PAIR_ST_PAGES;
+  return ok ? id : 0;
 }
 
 // The launches of attn_rows.hip (requests of at most kRowsMost rows, a row being

@@ -86,6 +86,7 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
   const int64_t koff = x * slot_bytes + g * 16;
   const int64_t voff = 4 * g * slot_bytes + x * (DIM / 8);
 
+  int32_t bad_page = 0;
   for (int kb = k0; kb < k1; kb += kUnit) {
     // where the keys lie
     u32x4_t kf[2][NC];
@@ -97,7 +98,7 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
         int key = kb + 16 * t;
         if (key >= len) key = (len - 1) & ~15;
         const uint32_t pg = div_by((uint32_t)key, s.page);
-        const int64_t at = checked_page(s.a, row[pg]) * page_bytes +
+        const int64_t at = checked_page(s.a, table_entry(row, pg), &bad_page) * page_bytes +
                            (int64_t)((uint32_t)key - pg * s.page.d) * slot_bytes;
         const unsigned char* kp = kbase + at + koff;
 #pragma unroll
@@ -121,7 +122,7 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
           int key = kb + 16 * t + (i < 0 ? x : 4 * g + i);
           if (key >= len) key = len - 1;
           const uint32_t pg = div_by((uint32_t)key, s.page);
-          const int64_t at = checked_page(s.a, row[pg]) * page_bytes +
+          const int64_t at = checked_page(s.a, row[pg], &bad_page) * page_bytes +
                              (int64_t)((uint32_t)key - pg * s.page.d) * slot_bytes;
           if (i < 0) {
             const unsigned char* kp = kbase + at + g * 16;
@@ -245,6 +246,7 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
       for (int nt = 0; nt < NT; ++nt) st->acc[nt][j] = mma16<BF16>(vt, pf[nt], st->acc[nt][j]);
     }
   }
+  if (bad_page) raise_status(s.a.d_status, bad_page);
 }
 
 // Keys [k0, k1) of one request and head (k0 a multiple of kUnit): the waves'

@@ -145,7 +145,7 @@ __device__ __forceinline__ int value_piece(int row, int c) {
 // product.  The weights go through LDS (over the keys, which are done with)
 // and each row adds the values that it sees, one key at a time.
 template <bool BF16, int DIM>
-__device__ __forceinline__ void add_odd_step(unsigned char* keys, const unsigned char* values,
+__device__ __forceinline__ void add_odd_step(unsigned char* keys, unsigned char* values,
                                              const u32x4_t (&pf)[4], int kb, int limit,
                                              f32x16_t (*acc)[DIM / 32]) {
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
@@ -174,6 +174,9 @@ __device__ __forceinline__ void add_odd_step(unsigned char* keys, const unsigned
                 p, half_value<BF16>((v[e >> 1] >> (16 * (e & 1))) & 0xffffu), (*acc)[d][4 * b + e]);
       }
   }
+  __syncthreads();
+  for (int b = threadIdx.x * 16; b < kKeys * DIM * 2; b += kThreads * 16)
+    *reinterpret_cast<u32x4_t*>(values + b) = u32x4_t{0u, 0u, 0u, 0u};
   __syncthreads();
 }
 
@@ -246,28 +249,36 @@ __global__ __launch_bounds__(kThreads, 2) void attention_tiles_kernel(TileArgs s
   const int my_row = (int)threadIdx.x / kPer, my_piece = (int)threadIdx.x % kPer;
   constexpr int kWaveRows = kWave / kPer;   // rows of a wave's load, in one page
 
+  // The pages of a step are looked up a step before its keys are fetched.
   u32x4_t ks[kStage], vs[kStage];
+  int32_t id[kStage];
+  int32_t bad_page = 0;
+  const int64_t lane_off = my_piece * 16 + (ALIGNED ? (lane / kPer) * slot_bytes : 0);
+  auto key_of = [&](int kb, int p) {
+    if (ALIGNED) {
+      // a run of 16 keys lies in one page; one past the end repeats the last
+      const int key = kb + p * kStep + wave * kWaveRows;
+      return uniform(key < q.len ? key : ((q.len - 1) & ~15) + (key & 15));
+    }
+    const int key = kb + p * kStep + my_row;
+    return key < q.len ? key : q.len - 1;
+  };
+  auto lookup = [&](int kb) {
+#pragma unroll
+    for (int p = 0; p < kStage; ++p) {
+      const uint32_t pg = div_by((uint32_t)key_of(kb, p), s.page);
+      id[p] = ALIGNED ? table_entry(table, pg) : table[pg];
+    }
+  };
   auto fetch = [&](int kb) {
 #pragma unroll
     for (int p = 0; p < kStage; ++p) {
-      int64_t at;
-      if (ALIGNED) {
-        // a run of 16 keys lies in one page; one past the end repeats the last
-        int key = kb + p * kStep + wave * kWaveRows;
-        if (key >= q.len) key = ((q.len - 1) & ~15) + (key & 15);
-        const uint32_t pg = div_by((uint32_t)key, s.page);
-        at = checked_page(s.a, table[pg]) * page_bytes +
-             (int64_t)((uint32_t)key - pg * s.page.d) * slot_bytes +
-             (lane / kPer) * slot_bytes;
-      } else {
-        int key = kb + p * kStep + my_row;
-        if (key >= q.len) key = q.len - 1;
-        const uint32_t pg = div_by((uint32_t)key, s.page);
-        at = checked_page(s.a, table[pg]) * page_bytes +
-             (int64_t)((uint32_t)key - pg * s.page.d) * slot_bytes;
-      }
-      ks[p] = *reinterpret_cast<const u32x4_t*>(kbase + at + my_piece * 16);
-      vs[p] = *reinterpret_cast<const u32x4_t*>(vbase + at + my_piece * 16);
+      const uint32_t key = (uint32_t)key_of(kb, p);
+      const uint32_t at_page = key - div_by(key, s.page) * s.page.d;
+      const int64_t at =
+          checked_page(s.a, id[p], &bad_page) * page_bytes + at_page * slot_bytes;
+      ks[p] = *reinterpret_cast<const u32x4_t*>(kbase + at + lane_off);
+      vs[p] = *reinterpret_cast<const u32x4_t*>(vbase + at + lane_off);
     }
   };
   // Into LDS, and a barrier; whether a step that some row does not see whole
@@ -292,10 +303,17 @@ __global__ __launch_bounds__(kThreads, 2) void attention_tiles_kernel(TileArgs s
     return false;
   };
 
-  if (k0 < k1) fetch(k0);
+  if (k0 < k1) {
+    lookup(k0);
+    fetch(k0);
+    lookup(k0 + kKeys);
+  }
   for (int kb = k0, buf = 0; kb < k1; kb += kKeys, buf ^= 1) {
     const bool odd = park(kb, buf);
-    if (kb + kKeys < k1) fetch(kb + kKeys);
+    if (kb + kKeys < k1) {
+      fetch(kb + kKeys);
+      lookup(kb + 2 * kKeys);
+    }
 
     f32x16_t sc[2];
 #pragma unroll
@@ -315,7 +333,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_tiles_kernel(TileArgs s
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (kb + 32 * t + 8 * (e >> 2) + 4 * h + (e & 3) > limit) sc[t][e] = -INFINITY;
+          sc[t][e] = kb + 32 * t + 8 * (e >> 2) + 4 * h + (e & 3) > limit ? -INFINITY : sc[t][e];
     }
     float top = -INFINITY;
 #pragma unroll
@@ -350,14 +368,11 @@ __global__ __launch_bounds__(kThreads, 2) void attention_tiles_kernel(TileArgs s
       }
     l += part;
 
-    if (odd) {
-      add_odd_step<BF16, DIM>(kt[0], vt[buf], pf, kb, limit, &acc);
-      continue;
-    }
+    if (odd) add_odd_step<BF16, DIM>(kt[0], vt[buf], pf, kb, limit, &acc);
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+    for (int u = 0; u < 4; ++u)             // 16 keys at a time
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {         // 16 keys at a time
+      for (int d = 0; d < ND; ++d) {
         u32x4_t vf;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -374,8 +389,9 @@ __global__ __launch_bounds__(kThreads, 2) void attention_tiles_kernel(TileArgs s
       }
   }
 
-  if (i >= rows) return;
+  if (bad_page) raise_status(s.a.d_status, bad_page);
   l += __shfl_xor(l, 32, kWave);
+  if (i >= rows) return;
   const int64_t row = (q.q0 + tok) * s.a.q_heads + qh;
   if (s.splits > 1) {
     const int64_t at = row * s.splits + split;
