@@ -2,8 +2,8 @@
 // rows of a key/value head -- a row is one query head of one token -- fit one
 // or two tiles of 16, and the time goes into reading the cache once.
 //
-// Layout.  A wave takes 32 keys at a time straight from memory into registers;
-// nothing goes through LDS in the loop.
+// Layout.  A wave takes 32 keys at a time from memory into registers, whole rows
+// at a time; keys then pass through the wave's own LDS, values do not.
 //   scores   S^T = K Q^T: a key row is 16-byte pieces of the A operand, and lane
 //            (x, g) ends up with row x's scores of keys 4 g + i and 16 + 4 g + i;
 //   weights  exactly those are its eight entries of the B operand of
@@ -13,12 +13,13 @@
 // The rows' running maximum is raised (and the sums rescaled) only when a score
 // exceeds it by 2^8, so most steps need no exchange between lanes.
 //
-// Work split.  The keys of all requests and heads form one line of units of
-// kUnit keys; it is cut into equal runs, one per workgroup, whatever the
-// lengths (the lengths are scanned by every workgroup: they are a few cached
-// kilobytes).  A head whose run is cut leaves partial sums that a second launch
-// joins.  The four waves of a workgroup take the 32-key blocks in turn and are
-// joined through LDS.
+// Work split.  The keys of all requests form one line of units of kUnit keys; it
+// is cut into equal runs whatever the lengths (the lengths are scanned by every
+// workgroup: they are a few cached kilobytes), and a run has one workgroup for
+// each key head.  Those walk it side by side, so that the heads of a slot, which
+// lie together in memory, are read at about the same time.  A request that is
+// cut leaves partial sums that a second launch joins.  The four waves of a
+// workgroup take the 32-key blocks in turn and are joined through LDS.
 #include "attn.hpp"
 
 namespace pair {
@@ -31,17 +32,18 @@ constexpr int kBlock = 32;                  // keys of a wave's step
 constexpr int kUnit = kBlock * kWaves;      // keys of a workgroup's step
 // Requests whose lengths a workgroup scans; more of them fill the card with
 // one workgroup per request and head.
-constexpr int kMostScanned = 4096;
+constexpr int kMostScanned = 2048;
+constexpr int kMostRuns = 1024;
 constexpr float kLazy = 8.0f;
 
 struct RowArgs {
   AttnCall a;
   FastDiv page, group;
   float scale_log2;
-  int32_t groups;       // workgroups; 0: one per request and head
+  int32_t runs;         // most runs; 0: one workgroup per request and head
   int32_t* starts;      // [n + 1] units before each request (workspace)
-  float* part_o;        // [2 groups][rows][dim]
-  float* part_ml;       // [2 groups][rows][2]
+  float* part_o;        // [2 runs][kv_heads][rows][dim]
+  float* part_ml;       // [2 runs][kv_heads][rows][2]
 };
 
 __device__ __forceinline__ int units_of(const RowArgs& s, int64_t r, int32_t* bad) {
@@ -51,10 +53,10 @@ __device__ __forceinline__ int units_of(const RowArgs& s, int64_t r, int32_t* ba
   return q.len <= kUnit ? 1 : (q.len + kUnit - 1) / kUnit;
 }
 
-// Workgroups that get a run: no more than there are units, so that none of
-// those between two of a head is without one.
+// No more runs than there are units, so that none of those between two of a
+// request is empty.
 __device__ __forceinline__ int64_t runs_of(const RowArgs& s, int64_t units) {
-  return units < s.groups ? units : s.groups;
+  return units < s.runs ? units : s.runs;
 }
 
 // First unit of run w of `runs` on a line of `units`.
@@ -69,11 +71,94 @@ struct State {
   f32x4_t acc[NT][DIM / 16];         // O^T: dims (4 g + i) * (DIM / 16) + j of row x
 };
 
+// LDS of one wave: a block's keys, the values and weights of an odd one, or the
+// wave's sums.
+// A lane's sixteenth of a key or value row.  Each is read once: the loads are
+// non-temporal, and each instruction covers whole cache lines.
+template <int DIM>
+struct Piece {
+  uint32_t w[DIM / 32];
+  __device__ __forceinline__ void load(const unsigned char* p) {
+    if (DIM == 128) {
+      const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
+#pragma unroll
+      for (int i = 0; i < DIM / 32; ++i) w[i] = v[i];
+    } else {
+      const u32x2_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(p));
+#pragma unroll
+      for (int i = 0; i < DIM / 32; ++i) w[i] = v[i];
+    }
+  }
+  __device__ __forceinline__ void store(unsigned char* p) const {
+#pragma unroll
+    for (int i = 0; i < DIM / 32; ++i) reinterpret_cast<uint32_t*>(p)[i] = w[i];
+  }
+};
+
+// Byte `b` of LDS row `row` of a block's keys: 16-byte pieces permuted by the
+// row, so that neither 16 lanes on one row nor 16 rows at one place meet in a
+// bank.
+template <int DIM>
+__device__ __forceinline__ int key_place(int row, int b) {
+  return row * (DIM * 2) + ((((b >> 4) ^ row) & (DIM / 8 - 1)) << 4) + (b & 15);
+}
+
+template <int DIM, int NT>
+struct WaveLds {
+  union {
+    float sum[16][DIM + 4];
+    unsigned char key[kBlock * DIM * 2];
+    uint16_t value[kBlock][DIM];
+  };
+  uint32_t weight[NT][16][kBlock / 2];
+  float stat[16][2];
+};
+
+// A block whose values are not all finite and not all seen by every row: each
+// row adds the values that it sees, one key at a time, and the values are
+// cleared so that the matrix product adds nothing.
+template <bool BF16, int DIM, int NT>
+__device__ __forceinline__ void add_odd_block(WaveLds<DIM, NT>* lds, const u32x4_t (&pf)[NT],
+                                              int kb, const int (&limit)[NT],
+                                              Piece<DIM> (*vr)[8], State<DIM, NT>* st) {
+  constexpr int ND = DIM / 16;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int x = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+#pragma unroll
+    for (int w = 0; w < ND / 2; ++w) {
+      uint32_t* to = reinterpret_cast<uint32_t*>(lds->value[16 * (e >> 2) + 4 * g + (e & 3)]);
+      to[x * (ND / 2) + w] = (*vr)[e].w[w];
+      (*vr)[e].w[w] = 0u;
+    }
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) lds->weight[nt][x][8 * (w >> 1) + 2 * g + (w & 1)] = pf[nt][w];
+  wave_lds_order();
+#pragma unroll 1
+  for (int k = 0; k < kBlock; ++k) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const float p = half_value<BF16>((lds->weight[nt][x][k >> 1] >> (16 * (k & 1))) & 0xffffu);
+      if (kb + k > limit[nt]) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < ND; ++j)
+          st->acc[nt][j][i] = __builtin_fmaf(
+              p, half_value<BF16>(lds->value[k][(4 * g + i) * ND + j]), st->acc[nt][j][i]);
+    }
+  }
+  wave_lds_order();
+}
+
 template <bool BF16, int DIM, int NT, bool ALIGNED>
 __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[NT][DIM / 32],
                                          const int (&limit)[NT], int first_limit, int64_t r,
                                          int64_t kvh, int len, int k0, int k1,
-                                         State<DIM, NT>* st) {
+                                         WaveLds<DIM, NT>* lds, State<DIM, NT>* st) {
   constexpr int NC = DIM / 32;       // 32-dim pieces of a key row
   constexpr int ND = DIM / 16;       // dims of a lane's piece of a value row
   const int lane = threadIdx.x & (kWave - 1);
@@ -83,81 +168,77 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
   const unsigned char* vbase = static_cast<const unsigned char*>(s.a.v_cache) + head;
   const int64_t slot_bytes = s.a.cache.slot_stride * 2, page_bytes = s.a.cache.page_stride * 2;
   const int32_t* row = s.a.table + r * s.a.ldt;
-  const int64_t koff = x * slot_bytes + g * 16;
-  const int64_t voff = 4 * g * slot_bytes + x * (DIM / 8);
+  const int64_t lane_off = x * (DIM / 8) + (ALIGNED ? 4 * g * slot_bytes : 0);
 
+  // A lane reads piece x of eight rows, the same of keys and values.  Pages are
+  // looked up a step before: one per tile of 16 keys where pages are multiples
+  // of 16 (by scalar loads), else one per row.
+  constexpr int kIds = ALIGNED ? 2 : 8;
+  int32_t id[kIds];
   int32_t bad_page = 0;
-  for (int kb = k0; kb < k1; kb += kUnit) {
-    // where the keys lie
-    u32x4_t kf[2][NC];
-    uint32_t vr[8][ND / 2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      if (ALIGNED) {
-        // a tile of 16 keys lies in one page; one past the end repeats the last
-        int key = kb + 16 * t;
-        if (key >= len) key = (len - 1) & ~15;
-        const uint32_t pg = div_by((uint32_t)key, s.page);
-        const int64_t at = checked_page(s.a, table_entry(row, pg), &bad_page) * page_bytes +
-                           (int64_t)((uint32_t)key - pg * s.page.d) * slot_bytes;
-        const unsigned char* kp = kbase + at + koff;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) kf[t][c] = *reinterpret_cast<const u32x4_t*>(kp + c * 64);
-        const unsigned char* vp = vbase + at + voff;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (DIM == 128) {
-            const u32x4_t w = *reinterpret_cast<const u32x4_t*>(vp + i * slot_bytes);
-#pragma unroll
-            for (int e = 0; e < ND / 2; ++e) vr[4 * t + i][e] = w[e];
-          } else {
-            const u32x2_t w = *reinterpret_cast<const u32x2_t*>(vp + i * slot_bytes);
-#pragma unroll
-            for (int e = 0; e < ND / 2; ++e) vr[4 * t + i][e] = w[e];
-          }
-        }
-      } else {
-#pragma unroll
-        for (int i = -1; i < 4; ++i) {     // the key row, then four value rows
-          int key = kb + 16 * t + (i < 0 ? x : 4 * g + i);
-          if (key >= len) key = len - 1;
-          const uint32_t pg = div_by((uint32_t)key, s.page);
-          const int64_t at = checked_page(s.a, row[pg], &bad_page) * page_bytes +
-                             (int64_t)((uint32_t)key - pg * s.page.d) * slot_bytes;
-          if (i < 0) {
-            const unsigned char* kp = kbase + at + g * 16;
-#pragma unroll
-            for (int c = 0; c < NC; ++c) kf[t][c] = *reinterpret_cast<const u32x4_t*>(kp + c * 64);
-          } else {
-            const unsigned char* vp = vbase + at + x * (DIM / 8);
-            const int e0 = 4 * t + (i < 0 ? 0 : i);
-            if (DIM == 128) {
-              const u32x4_t w = *reinterpret_cast<const u32x4_t*>(vp);
-#pragma unroll
-              for (int e = 0; e < ND / 2; ++e) vr[e0][e] = w[e];
-            } else {
-              const u32x2_t w = *reinterpret_cast<const u32x2_t*>(vp);
-#pragma unroll
-              for (int e = 0; e < ND / 2; ++e) vr[e0][e] = w[e];
-            }
-          }
-        }
-      }
+  auto key_of = [&](int kb, int n) {
+    if (ALIGNED) {                       // a tile past the end repeats the last
+      const int key = kb + 16 * n;
+      return uniform(key < len ? key : (len - 1) & ~15);
     }
+    const int key = kb + 16 * (n >> 2) + 4 * g + (n & 3);
+    return key < len ? key : len - 1;
+  };
+  auto lookup = [&](int kb) {
+#pragma unroll
+    for (int n = 0; n < kIds; ++n) {
+      const uint32_t pg = div_by((uint32_t)key_of(kb, n), s.page);
+      id[n] = ALIGNED ? table_entry(row, pg) : row[pg];
+    }
+  };
+  if (k0 < k1) lookup(k0);
+  for (int kb = k0; kb < k1; kb += kUnit) {
+    Piece<DIM> kr[8], vr[8];
+    int64_t at[kIds];
+#pragma unroll
+    for (int n = 0; n < kIds; ++n) {
+      const uint32_t key = (uint32_t)key_of(kb, n);
+      at[n] = checked_page(s.a, id[n], &bad_page) * page_bytes +
+              (int64_t)(key - div_by(key, s.page) * s.page.d) * slot_bytes + lane_off;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      kr[e].load(kbase + at[ALIGNED ? e >> 2 : e] + (ALIGNED ? (e & 3) * slot_bytes : 0));
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      vr[e].load(vbase + at[ALIGNED ? e >> 2 : e] + (ALIGNED ? (e & 3) * slot_bytes : 0));
+    if (kb + kUnit < k1) lookup(kb + kUnit);
+
+    // keys through LDS: whole rows come from memory, the product wants a row's
+    // piece from every lane
+    wave_lds_order();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int y = 16 * (e >> 2) + 4 * g + (e & 3);
+      kr[e].store(lds->key + key_place<DIM>(y, x * (DIM / 8)));
+    }
+    wave_lds_order();
+    f32x4_t sc[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) sc[nt][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const u32x4_t kf = *reinterpret_cast<const u32x4_t*>(
+            lds->key + key_place<DIM>(16 * t + x, 64 * c + 16 * g));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) sc[nt][t] = mma16<BF16>(kf, qf[nt][c], sc[nt][t]);
+      }
 
     float p[NT][8];
     const bool masked = kb + kBlock - 1 > first_limit;   // some row does not see some key
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      f32x4_t sc[2];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        sc[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int c = 0; c < NC; ++c) sc[t] = mma16<BF16>(kf[t][c], qf[nt][c], sc[t]);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[nt][e] = sc[e >> 2][e & 3] * s.scale_log2;
+      for (int e = 0; e < 8; ++e) p[nt][e] = sc[nt][e >> 2][e & 3] * s.scale_log2;
       if (masked) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -184,11 +265,14 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
       }
     }
 
+    u32x4_t pf[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) pf[nt][w] = pack2<BF16>(p[nt][2 * w], p[nt][2 * w + 1]);
     // Values that some row must not see: past the end they are no values at
     // all, and within the chunk a weight of zero does not hide a NaN or an
-    // infinity from the matrix product.  Those are taken out of it here and
-    // added below, one by one, to the rows that see them.
-    uint64_t odd = 0;
+    // infinity from the matrix product.
     if (masked) {
       uint32_t bad = 0;
 #pragma unroll
@@ -196,51 +280,19 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
         const int key = kb + 16 * (e >> 2) + 4 * g + (e & 3);
 #pragma unroll
         for (int w = 0; w < ND / 2; ++w) {
-          if (key >= len) vr[e][w] = 0u;
-          bad |= not_finite<BF16>(vr[e][w]) ? 1u : 0u;
+          if (key >= len) vr[e].w[w] = 0u;
+          bad |= not_finite<BF16>(vr[e].w[w]) ? 1u : 0u;
         }
       }
-      odd = __ballot(bad != 0u);
-    }
-    if (odd != 0) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-#pragma unroll
-        for (int j = 0; j < ND; ++j) {
-          const uint32_t bits = (vr[e][j >> 1] >> (16 * (j & 1))) & 0xffffu;
-          uint64_t where = __ballot(not_finite<BF16>(bits));
-          if (not_finite<BF16>(bits)) vr[e][j >> 1] &= (j & 1) ? 0x0000ffffu : 0xffff0000u;
-          while (where != 0) {
-            const int src = __ffsll((unsigned long long)where) - 1;
-            where &= where - 1;
-            const float v = half_value<BF16>((uint32_t)__builtin_amdgcn_readlane((int)bits, src));
-            const int key = kb + 16 * (e >> 2) + 4 * (src >> 4) + (e & 3);
-            const int m = src & 15;                 // dim m * ND + j
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              const float pv = __shfl(p[nt][e], x + 16 * (src >> 4), kWave);
-              if (key <= limit[nt] && g == (m >> 2)) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  if (i == (m & 3)) st->acc[nt][j][i] = __builtin_fmaf(pv, v, st->acc[nt][j][i]);
-              }
-            }
-          }
-        }
-      }
+      if (__any(bad != 0u)) add_odd_block<BF16, DIM, NT>(lds, pf, kb, limit, &vr, st);
     }
 
-    u32x4_t pf[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) pf[nt][w] = pack2<BF16>(p[nt][2 * w], p[nt][2 * w + 1]);
 #pragma unroll
     for (int j = 0; j < ND; ++j) {
       u32x4_t vt;                                   // dim j of this lane's eight keys
 #pragma unroll
       for (int w = 0; w < 4; ++w)
-        vt[w] = __builtin_amdgcn_perm(vr[2 * w + 1][j >> 1], vr[2 * w][j >> 1],
+        vt[w] = __builtin_amdgcn_perm(vr[2 * w + 1].w[j >> 1], vr[2 * w].w[j >> 1],
                                       (j & 1) ? 0x07060302u : 0x05040100u);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) st->acc[nt][j] = mma16<BF16>(vt, pf[nt], st->acc[nt][j]);
@@ -253,11 +305,8 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
 // sums, joined, either as results (slot < 0) or as partial sums.
 template <bool BF16, int DIM, int NT, bool ALIGNED>
 __device__ __forceinline__ void attend(const RowArgs& s, int64_t r, int kvh, int k0, int k1,
-                                       int64_t slot) {
+                                       int64_t slot, WaveLds<DIM, NT>* lds) {
   constexpr int ND = DIM / 16;
-  constexpr int kRow = DIM + 4;
-  __shared__ float sum[kWaves][16][kRow];
-  __shared__ float stat[kWaves][16][2];
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
   const int x = lane & 15, g = lane >> 4;
   Request q;
@@ -289,7 +338,7 @@ __device__ __forceinline__ void attend(const RowArgs& s, int64_t r, int kvh, int
   // it does for the first token
   const int end = k1 < q.len ? k1 : q.len;
   add_keys<BF16, DIM, NT, ALIGNED>(s, qf, limit, q.len - q.tokens, r, kvh, q.len,
-                                   k0 + kBlock * wave, end, &st);
+                                   k0 + kBlock * wave, end, lds + wave, &st);
 
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -297,30 +346,31 @@ __device__ __forceinline__ void attend(const RowArgs& s, int64_t r, int kvh, int
     l += __shfl_xor(l, 16, kWave);
     l += __shfl_xor(l, 32, kWave);
     if (g == 0) {
-      stat[wave][x][0] = st.m[nt];
-      stat[wave][x][1] = l;
+      lds[wave].stat[x][0] = st.m[nt];
+      lds[wave].stat[x][1] = l;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < ND; ++j) sum[wave][x][(4 * g + i) * ND + j] = st.acc[nt][j][i];
+      for (int j = 0; j < ND; ++j) lds[wave].sum[x][(4 * g + i) * ND + j] = st.acc[nt][j][i];
     __syncthreads();
     for (int e = threadIdx.x; e < 16 * DIM / 8; e += kThreads) {
       const int y = e / (DIM / 8), d = (e - y * (DIM / 8)) * 8;
       const int i = 16 * nt + y;
       if (i < rows) {
-        float m = stat[0][y][0];
+        float m = lds[0].stat[y][0];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, stat[w][y][0]);
+        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, lds[w].stat[y][0]);
         const float base = m == -INFINITY ? 0.0f : m;
         float tot = 0.0f, o[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-          const float f = __builtin_amdgcn_exp2f(stat[w][y][0] - base);
-          if (stat[w][y][0] == -INFINITY && stat[w][y][1] == 0.0f) continue;   // saw no key
-          tot = __builtin_fmaf(f, stat[w][y][1], tot);
+          const float mw = lds[w].stat[y][0], lw = lds[w].stat[y][1];
+          if (mw == -INFINITY && lw == 0.0f) continue;   // saw no key
+          const float f = __builtin_amdgcn_exp2f(mw - base);
+          tot = __builtin_fmaf(f, lw, tot);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) o[k] = __builtin_fmaf(f, sum[w][y][d + k], o[k]);
+          for (int k = 0; k < 8; ++k) o[k] = __builtin_fmaf(f, lds[w].sum[y][d + k], o[k]);
         }
         if (slot >= 0) {
           float* to = s.part_o + (slot * (16 * NT) + i) * DIM + d;
@@ -351,21 +401,9 @@ __device__ __forceinline__ void attend(const RowArgs& s, int64_t r, int kvh, int
   }
 }
 
-template <bool BF16, int DIM, int NT, bool ALIGNED>
-__global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(RowArgs s) {
-  const int64_t heads = s.a.kv_heads;
-  if (s.groups == 0) {
-    const int64_t r = blockIdx.x / heads;
-    int32_t bad = 0;
-    const int units = units_of(s, r, &bad);
-    if (bad && threadIdx.x == 0) raise_status(s.a.d_status, bad);
-    if (units == 0) return;
-    attend<BF16, DIM, NT, ALIGNED>(s, r, (int)(blockIdx.x - r * heads), 0, units * kUnit, -1);
-    return;
-  }
-  // units before each request, in every workgroup
-  __shared__ int32_t start[kMostScanned + 1];
-  __shared__ int32_t wave_sum_of[kWaves];
+// Units before each request, in every workgroup; the first leaves them to the
+// launch that joins.
+__device__ __forceinline__ void scan_units(const RowArgs& s, int32_t* start, int32_t* wave_sums) {
   const int n = (int)s.a.n, lane = threadIdx.x & (kWave - 1);
   const int per = (n + kThreads - 1) / kThreads;
   const int r0 = (int)threadIdx.x * per, r1 = r0 + per < n ? r0 + per : n;
@@ -382,11 +420,11 @@ __global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(RowArgs s) 
     const int32_t v = __shfl_up(scan, by, kWave);
     if (lane >= by) scan += v;
   }
-  if (lane == kWave - 1) wave_sum_of[threadIdx.x / kWave] = scan;
+  if (lane == kWave - 1) wave_sums[threadIdx.x / kWave] = scan;
   if (threadIdx.x == 0) start[0] = 0;
   __syncthreads();
   int32_t at = scan - mine;
-  for (int w = 0; w < (int)threadIdx.x / kWave; ++w) at += wave_sum_of[w];
+  for (int w = 0; w < (int)threadIdx.x / kWave; ++w) at += wave_sums[w];
   for (int r = r0; r < r1; ++r) {
     at += start[r + 1];
     start[r + 1] = at;
@@ -394,46 +432,72 @@ __global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(RowArgs s) 
   __syncthreads();
   if (blockIdx.x == 0)
     for (int r = threadIdx.x; r <= n; r += kThreads) s.starts[r] = start[r];
-  const int64_t units = start[n] * heads;
-  const int64_t runs = runs_of(s, units);
-  if (blockIdx.x >= runs) return;
-  int64_t u = uniform64(run_start(units, runs, blockIdx.x));
-  const int64_t end = uniform64(run_start(units, runs, blockIdx.x + 1));
-  int64_t slot = 2 * (int64_t)blockIdx.x;
+}
+
+template <bool BF16, int DIM, int NT, bool ALIGNED>
+__global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(RowArgs s) {
+  __shared__ WaveLds<DIM, NT> lds[kWaves];
+  __shared__ int32_t start[kMostScanned + 1];
+  __shared__ int32_t wave_sum_of[kWaves];
+  const int64_t heads = s.a.kv_heads;
+  const bool direct = s.runs == 0;          // one workgroup per request and head
+  const int64_t run = blockIdx.x / heads;   // or the request
+  const int h = (int)(blockIdx.x - run * heads);
+  const int n = (int)s.a.n;
+  int64_t u = 0, end = 0;
+  if (direct) {
+    int32_t bad = 0;
+    const int units = units_of(s, run, &bad);
+    if (bad && threadIdx.x == 0) raise_status(s.a.d_status, bad);
+    end = uniform(units);
+  } else {
+    scan_units(s, start, wave_sum_of);
+    const int64_t units = start[n];
+    const int64_t runs = runs_of(s, units);
+    if (run >= runs) return;
+    u = uniform64(run_start(units, runs, run));
+    end = uniform64(run_start(units, runs, run + 1));
+  }
+  int64_t part = 2 * run;
   while (u < end) {
-    int lo = 0, hi = n - 1;                         // the request of unit u
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (uniform(start[mid + 1]) * heads > u)
-        hi = mid;
-      else
-        lo = mid + 1;
+    int64_t r = run;
+    int c0 = 0, c1 = (int)end;
+    bool whole = true;
+    if (!direct) {
+      int lo = 0, hi = n - 1;               // the request of unit u
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (uniform(start[mid + 1]) > u)
+          hi = mid;
+        else
+          lo = mid + 1;
+      }
+      r = lo;
+      const int first = uniform(start[lo]), count = uniform(start[lo + 1]) - first;
+      c0 = (int)u - first;
+      c1 = count - c0 < end - u ? count : c0 + (int)(end - u);
+      whole = c0 == 0 && c1 == count;
     }
-    const int first = uniform(start[lo]), count = uniform(start[lo + 1]) - first;
-    const int x = (int)(u - first * heads);
-    const int h = x / count, c0 = x - h * count;
-    const int c1 = count - c0 < end - u ? count : c0 + (int)(end - u);
-    const bool whole = c0 == 0 && c1 == count;
-    attend<BF16, DIM, NT, ALIGNED>(s, lo, h, c0 * kUnit, c1 * kUnit, whole ? -1 : slot);
-    slot = 2 * (int64_t)blockIdx.x + 1;
+    attend<BF16, DIM, NT, ALIGNED>(s, r, h, c0 * kUnit, c1 * kUnit,
+                                   whole ? -1 : part * heads + h, lds);
+    part = 2 * run + 1;
     u += c1 - c0;
   }
 }
 
-// Joins the partial sums of the heads that were cut: one workgroup per request,
-// head and row, its waves taking the parts in turn.
+// Joins the partial sums of the requests that were cut: one workgroup per
+// request, head and row.  The parts' maxima first, a lane each, then their sums
+// with several parts' loads in flight.
 template <bool BF16, int DIM>
 __global__ __launch_bounds__(kThreads) void join_rows_kernel(RowArgs s, int rows_slot) {
   const int64_t heads = s.a.kv_heads;
   const int64_t r = blockIdx.x / heads;
   const int kvh = (int)(blockIdx.x - r * heads);
   const int i = blockIdx.y;
-  const int64_t first = s.starts[r] * heads, count = s.starts[r + 1] - s.starts[r];
-  if (count == 0) return;
-  const int64_t units = s.starts[s.a.n] * heads;
-  const int64_t u0 = first + kvh * count, u1 = u0 + count;
-  // workgroup of unit u: the last whose run starts at or before it
-  const int64_t runs = runs_of(s, units);
+  const int64_t u0 = s.starts[r], u1 = s.starts[r + 1];
+  if (u0 == u1) return;
+  const int64_t units = s.starts[s.a.n], runs = runs_of(s, units);
+  // run of unit u: the last that starts at or before it
   const int64_t w0 = ((u0 + 1) * runs - 1) / units, w1 = (u1 * runs - 1) / units;
   if (w0 == w1) return;
   Request q;
@@ -442,51 +506,50 @@ __global__ __launch_bounds__(kThreads) void join_rows_kernel(RowArgs s, int rows
   if (i >= q.tokens * (int)s.group.d) return;
   const int tok = (int)div_by((uint32_t)i, s.group);
   const int h = kvh * (int)s.group.d + i - tok * (int)s.group.d;
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
   constexpr int PER = DIM / kWave;
-  float m = -INFINITY, l = 0.0f, o[PER];
+  __shared__ float weight[kMostRuns], sum[kWaves][DIM];
+  const int parts = (int)(w1 - w0) + 1;
+  // a request that starts inside a run is in the run's second part
+  const int64_t first = 2 * w0 + (run_start(units, runs, w0) != u0 ? 1 : 0);
+  auto place = [&](int p) {
+    return ((p == 0 ? first : 2 * (w0 + p)) * heads + kvh) * rows_slot + i;
+  };
+  float m = -INFINITY;
+  for (int p = lane; p < parts; p += kWave) m = fmaxf(m, s.part_ml[place(p) * 2]);
+#pragma unroll
+  for (int by = 1; by < kWave; by <<= 1) m = fmaxf(m, __shfl_xor(m, by, kWave));
+  const float base = m == -INFINITY ? 0.0f : m;
+  float l = 0.0f;
+  for (int p = lane; p < parts; p += kWave) {
+    const float mp = s.part_ml[place(p) * 2], lp = s.part_ml[place(p) * 2 + 1];
+    const bool none = mp == -INFINITY && lp == 0.0f;       // saw no key
+    const float f = none ? 0.0f : __builtin_amdgcn_exp2f(mp - base);
+    l += none ? 0.0f : lp * f;
+    if (wave == 0) weight[p] = f;
+  }
+  l = wave_sum(l);
+  __syncthreads();
+  float o[PER];
 #pragma unroll
   for (int e = 0; e < PER; ++e) o[e] = 0.0f;
-  for (int64_t w = w0 + wave; w <= w1; w += kWaves) {
-    // a head that starts inside a workgroup's run is in its second slot
-    const int64_t slot = 2 * w + (w == w0 && run_start(units, runs, w) != u0 ? 1 : 0);
-    const int64_t at = slot * rows_slot + i;
-    const float mw = s.part_ml[at * 2], lw = s.part_ml[at * 2 + 1];
-    float ow[PER];
+#pragma unroll 4
+  for (int p = wave; p < parts; p += kWaves) {
+    const float f = weight[p];
+    const float* from = s.part_o + place(p) * DIM;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) ow[e] = s.part_o[at * DIM + e * kWave + lane];
-    if (mw == -INFINITY && lw == 0.0f) continue;
-    const float mn = fmaxf(m, mw);
-    const float base = mn == -INFINITY ? 0.0f : mn;
-    const float a = __builtin_amdgcn_exp2f(m - base), b = __builtin_amdgcn_exp2f(mw - base);
-    l = l * a + lw * b;
-#pragma unroll
-    for (int e = 0; e < PER; ++e) o[e] = o[e] * a + ow[e] * b;
-    m = mn;
+    for (int e = 0; e < PER; ++e) o[e] = __builtin_fmaf(from[e * kWave + lane], f, o[e]);
   }
-  __shared__ float sum[kWaves][DIM], stat[kWaves][2];
 #pragma unroll
   for (int e = 0; e < PER; ++e) sum[wave][e * kWave + lane] = o[e];
-  if (lane == 0) {
-    stat[wave][0] = m;
-    stat[wave][1] = l;
-  }
   __syncthreads();
   if (threadIdx.x >= DIM / 2) return;
-  m = stat[0][0];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) m = fmaxf(m, stat[w][0]);
-  const float base = m == -INFINITY ? 0.0f : m;
-  l = 0.0f;
-  float a = 0.0f, b = 0.0f;
   const int d = threadIdx.x * 2;
+  float a = 0.0f, b = 0.0f;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    if (stat[w][0] == -INFINITY && stat[w][1] == 0.0f) continue;
-    const float f = __builtin_amdgcn_exp2f(stat[w][0] - base);
-    l += stat[w][1] * f;
-    a += sum[w][d] * f;
-    b += sum[w][d + 1] * f;
+    a += sum[w][d];
+    b += sum[w][d + 1];
   }
   const bool none = limit_of(q, tok) < 0;
   const float inv = 1.0f / l;
@@ -500,7 +563,7 @@ __global__ __launch_bounds__(kThreads) void join_rows_kernel(RowArgs s, int rows
 struct Plan {
   int tiles;            // of 16 rows
   int rows;             // bound on a request's rows
-  int32_t groups;
+  int32_t runs;
   size_t starts, ml, total;   // workspace: bytes of the parts
 };
 
@@ -512,20 +575,23 @@ Plan plan_rows(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim, int32_
   p.tiles = p.rows <= 16 ? 1 : 2;
   // Cut into equal runs unless every head is a step or two anyway, or the
   // requests are so many that they fill the card by themselves.
-  const int64_t most = n * kv_heads * ((max_len + kUnit - 1) / kUnit);
-  const int64_t slots = 2 * (int64_t)device_cu_count();
-  p.groups = n > kMostScanned || max_len <= 2 * kUnit ? 0 : (int32_t)(most < slots ? most : slots);
-  const size_t parts = 2 * (size_t)p.groups * 16 * p.tiles;
+  const int64_t most = n * ((max_len + kUnit - 1) / kUnit);
+  int64_t runs = 2 * (int64_t)device_cu_count() / kv_heads;   // two workgroups fit a compute unit
+  if (runs > most) runs = most;
+  if (runs > kMostRuns) runs = kMostRuns;
+  if (runs < 1) runs = 1;
+  p.runs = n > kMostScanned || max_len <= 2 * kUnit ? 0 : (int32_t)runs;
+  const size_t parts = 2 * (size_t)p.runs * kv_heads * 16 * p.tiles;
   p.starts = ((size_t)(n + 1) * 4 + 255) / 256 * 256;
   p.ml = (parts * 8 + 255) / 256 * 256;
-  p.total = p.groups == 0 ? 256 : p.starts + p.ml + parts * dim * 4;
+  p.total = p.runs == 0 ? 256 : p.starts + p.ml + parts * dim * 4;
   return p;
 }
 
 template <bool BF16, int DIM>
 int launch(const RowArgs& s, const Plan& p, hipStream_t stream) {
-  const int64_t grid = p.groups != 0 ? p.groups : s.a.n * s.a.kv_heads;
-  if (grid > 0x7fffffffLL || s.a.n * s.a.kv_heads > 0x7fffffffLL) return PAIR_ERANGE;
+  const int64_t grid = (p.runs != 0 ? p.runs : s.a.n) * s.a.kv_heads;
+  if (s.a.n * s.a.kv_heads > 0x7fffffffLL) return PAIR_ERANGE;
   const bool aligned = s.page.d % 16 == 0;
 #define PAIR_ROWS(NT, AL)                                                                        \
   hipLaunchKernelGGL((attention_rows_kernel<BF16, DIM, NT, AL>), dim3((unsigned)grid),            \
@@ -537,7 +603,7 @@ int launch(const RowArgs& s, const Plan& p, hipStream_t stream) {
   }
 #undef PAIR_ROWS
   if (hipGetLastError() != hipSuccess) return PAIR_EHIP;
-  if (p.groups != 0)
+  if (p.runs != 0)
     hipLaunchKernelGGL((join_rows_kernel<BF16, DIM>),
                        dim3((unsigned)(s.a.n * s.a.kv_heads), (unsigned)p.rows), dim3(kThreads), 0,
                        stream, s, 16 * p.tiles);
@@ -558,7 +624,7 @@ int launch_attention_rows(const AttnCall& a, void* workspace, hipStream_t stream
   s.page = fast_div((uint32_t)a.cache.page);
   s.group = fast_div((uint32_t)(a.q_heads / a.kv_heads));
   s.scale_log2 = a.scale * 1.44269504089f;
-  s.groups = p.groups;
+  s.runs = p.runs;
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   s.starts = reinterpret_cast<int32_t*>(ws);
   s.part_ml = reinterpret_cast<float*>(ws + p.starts);
