@@ -18,6 +18,7 @@ workspace to later work only behind them.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import functools
 import inspect
@@ -177,8 +178,17 @@ def _dev(t, name, dtype, numel=None, allow_none=False):
     return t.data_ptr()   # the declared argument type makes the pointer
 
 
+# The current stream's handle without a Stream object, where torch has the call
+# (0.2 us against 2.8 us, of a call that takes 15 to 30 in all).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device())
 
 
 def _scores_arg(scores):
@@ -486,33 +496,38 @@ def pair_clip_grads_workspace_bytes(count) -> int:
     return int(lib().pair_clip_grads_workspace_bytes(count))
 
 
-def _grad_table(grads, name):
-    """Host arrays of the tensors' addresses and types for one call."""
-    ptr, size, code = [], [], []
-    for t in grads:
-        if not (t.is_cuda and t.is_contiguous()):
-            raise ValueError(f"{name} must be contiguous CUDA (HIP) tensors")
-        if t.dtype not in _DTYPE_CODE:
-            raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
-        ptr.append(t.data_ptr())
-        size.append(t.numel())
-        code.append(_DTYPE_CODE[t.dtype])
-    n = len(ptr)
-    return ((ctypes.c_void_p * n)(*ptr), (ctypes.c_int64 * n)(*size), (ctypes.c_int32 * n)(*code),
-            size)
+def _grad_table(tensors, name):
+    """Host arrays of the tensors' addresses, sizes and types for one call; a
+    model has hundreds, so each property is gathered in one go."""
+    T = torch.Tensor
+    if not all(isinstance(t, T) for t in tensors):
+        raise ValueError(f"{name} must be tensors")
+    devices = set(map(T.get_device, tensors))
+    if len(devices) > 1 or -1 in devices or not all(map(T.is_contiguous, tensors)):
+        raise ValueError(f"{name} must be contiguous CUDA (HIP) tensors of one device")
+    try:
+        code = array.array("i", map(_DTYPE_CODE.__getitem__, map(T.dtype.__get__, tensors)))
+    except KeyError as e:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {e.args[0]}") from None
+    return (array.array("Q", map(T.data_ptr, tensors)), array.array("q", map(T.numel, tensors)), code)
+
+
+def _address(a):
+    return None if a is None else a.buffer_info()[0]
 
 
 def pair_clip_grads(grads, max_norm, norm, coef, workspace, out=None, d_status=None, stream=None):
     """`out`: None clips in place, else a list of tensors of the gradients'
     sizes, each of its gradient's type or float32."""
-    gp, sizes, codes, numel = _grad_table(grads, "grads")
-    op = ocodes = None
+    ptrs, sizes, codes = _grad_table(grads, "grads")
+    optrs = ocodes = None
     if out is not None:
-        op, _, ocodes, onumel = _grad_table(out, "out")
-        if onumel != numel:
+        optrs, osizes, ocodes = _grad_table(out, "out")
+        if osizes != sizes:
             raise ValueError("out must hold a tensor of each gradient's size")
     _rc(lib().pair_clip_grads(
-        len(numel), gp, op, sizes, codes, ocodes, float(max_norm),
+        len(sizes), _address(ptrs), _address(optrs), _address(sizes), _address(codes),
+        _address(ocodes), float(max_norm),
         _dev(norm, "norm", torch.float32, 1), _dev(coef, "coef", torch.float32, 1),
         _dev(workspace, "workspace", torch.uint8), workspace.numel(),
         _dev(d_status, "d_status", torch.int32, 1, True), _stream(stream)), "pair_clip_grads")
