@@ -20,6 +20,8 @@
 //
 // When the tiles are too few for the card, each tile's keys are split and a
 // second launch joins the parts.
+#include <type_traits>
+
 #include "attn.hpp"
 
 namespace pair {
@@ -32,6 +34,9 @@ constexpr int kRows = 32 * kWaves;          // of a tile
 constexpr int kKeys = 64;                   // of a step
 constexpr float kLazy = 8.0f;
 constexpr int kInline = kThreads;           // requests that a workgroup scans itself
+
+// kinds of instructions in a scheduling group
+constexpr int kMfma = 0x8, kDsRead = 0x100;
 
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
@@ -247,93 +252,125 @@ __global__ __launch_bounds__(kThreads, 2) void attention_tiles_kernel(TileArgs s
   const int64_t slot_bytes = s.a.cache.slot_stride * 2, page_bytes = s.a.cache.page_stride * 2;
   const int32_t* table = s.a.table + r * s.a.ldt;
   const int my_row = (int)threadIdx.x / kPer, my_piece = (int)threadIdx.x % kPer;
-  constexpr int kWaveRows = kWave / kPer;   // rows of a wave's load, in one page
-
-  // The pages of a step are looked up a step before its keys are fetched.
-  u32x4_t ks[kStage], vs[kStage];
-  int32_t id[kStage];
+  constexpr int kWaveRows = kWave / kPer;   // rows of a wave's load: within 16 aligned ones
   int32_t bad_page = 0;
-  const int64_t lane_off = my_piece * 16 + (ALIGNED ? (lane / kPer) * slot_bytes : 0);
-  auto key_of = [&](int kb, int p) {
-    if (ALIGNED) {
-      // a run of 16 keys lies in one page; one past the end repeats the last
-      const int key = kb + p * kStep + wave * kWaveRows;
-      return uniform(key < q.len ? key : ((q.len - 1) & ~15) + (key & 15));
-    }
-    const int key = kb + p * kStep + my_row;
-    return key < q.len ? key : q.len - 1;
+  auto place = [&](int key, int32_t id) {   // byte offset of a key
+    const uint32_t pg = div_by((uint32_t)key, s.page);
+    return checked_page(s.a, id, &bad_page) * page_bytes +
+           (int64_t)((uint32_t)key - pg * s.page.d) * slot_bytes;
+  };
+
+  // Where the keys lie.  ALIGNED (pages of a multiple of 16 keys): 16 aligned
+  // keys share a page, and lane x of the wave holds the place of 16-key group x
+  // of a window of 1024 keys; a fetch reads it from the lane, and the loads take
+  // a scalar base.  The next window's pages are loaded a window ahead.  Else
+  // each lane looks its rows up a step ahead.
+  constexpr int kWindow = 16 * kWave;
+  u32x4_t ks[kStage], vs[kStage];
+  int32_t id[ALIGNED ? 1 : kStage];
+  int64_t group_at = 0;
+  int window = k0;
+  const uint32_t lane_off =
+      my_piece * 16 + (ALIGNED ? (uint32_t)((my_row & 15) * slot_bytes) : 0u);
+  auto row_key = [&](int kb, int p) {       // one past the end repeats the last
+    const int key = ALIGNED ? kb + 16 * lane : kb + p * kStep + my_row;
+    return key < q.len ? key : (ALIGNED ? (q.len - 1) & ~15 : q.len - 1);
   };
   auto lookup = [&](int kb) {
 #pragma unroll
-    for (int p = 0; p < kStage; ++p) {
-      const uint32_t pg = div_by((uint32_t)key_of(kb, p), s.page);
-      id[p] = ALIGNED ? table_entry(table, pg) : table[pg];
-    }
+    for (int p = 0; p < (ALIGNED ? 1 : kStage); ++p)
+      id[p] = table[div_by((uint32_t)row_key(kb, p), s.page)];
   };
   auto fetch = [&](int kb) {
+    if (ALIGNED && kb - window == kWindow) {
+      window = kb;
+      group_at = place(row_key(kb, 0), id[0]);
+      lookup(kb + kWindow);
+    }
 #pragma unroll
     for (int p = 0; p < kStage; ++p) {
-      const uint32_t key = (uint32_t)key_of(kb, p);
-      const uint32_t at_page = key - div_by(key, s.page) * s.page.d;
-      const int64_t at =
-          checked_page(s.a, id[p], &bad_page) * page_bytes + at_page * slot_bytes;
+      int64_t at;
+      if (ALIGNED) {
+        const int x16 = ((kb - window) >> 4) + ((p * kStep + wave * kWaveRows) >> 4);
+        const uint32_t lo =
+            (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)group_at, x16);
+        const uint32_t hi =
+            (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)group_at >> 32), x16);
+        at = (int64_t)(((uint64_t)hi << 32) | lo);
+      } else {
+        at = place(row_key(kb, p), id[ALIGNED ? 0 : p]);
+      }
       ks[p] = *reinterpret_cast<const u32x4_t*>(kbase + at + lane_off);
       vs[p] = *reinterpret_cast<const u32x4_t*>(vbase + at + lane_off);
     }
+    if (!ALIGNED) lookup(kb + kKeys);
   };
-  // Into LDS, and a barrier; whether a step that some row does not see whole
-  // holds a value that is not finite.
-  const int tile_limit = limit_of(q, (int)div_by((uint32_t)(tile * kRows), s.group));
-  auto park = [&](int kb, int buf) {
-    const bool edge = kb + kKeys - 1 > tile_limit;
-    uint32_t bad = 0;
+
+  // Offsets in LDS; a step's buffer and the rows' higher parts are constants.
+  int k_in, v_in, k_out[NC], v_out[ND];
+  k_in = key_piece<DIM>(my_row, my_piece);
+  v_in = value_piece<DIM>(my_row, my_piece);
 #pragma unroll
-    for (int p = 0; p < kStage; ++p) {
-      const int row = p * kStep + my_row;
-      if (edge) {
-        if (kb + row >= q.len) vs[p] = u32x4_t{0u, 0u, 0u, 0u};   // no value at all
+  for (int c = 0; c < NC; ++c) k_out[c] = key_piece<DIM>(x, 2 * c + h);
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+    v_out[d] = value_piece<DIM>(4 * h + ((lane & 15) >> 2),
+                                4 * d + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) +
+               (lane & 1) * 8;
+
+  const int tile_limit = limit_of(q, (int)div_by((uint32_t)(tile * kRows), s.group));
+  auto step = [&](int kb, auto buffer) {
+    constexpr int buf = decltype(buffer)::value;
+    // Into LDS, and a barrier.  `odd`: a step that some row of the tile does not
+    // see whole holds a value that is not finite.
+    const bool edge = kb + kKeys - 1 > tile_limit;
+    bool odd = false;
+    if (edge) {
+      uint32_t bad = 0;
+#pragma unroll
+      for (int p = 0; p < kStage; ++p) {
+        if (kb + p * kStep + my_row >= q.len) vs[p] = u32x4_t{0u, 0u, 0u, 0u};   // no value at all
 #pragma unroll
         for (int w = 0; w < 4; ++w) bad |= not_finite<BF16>(vs[p][w]) ? 1u : 0u;
       }
-      *reinterpret_cast<u32x4_t*>(kt[buf] + key_piece<DIM>(row, my_piece)) = ks[p];
-      *reinterpret_cast<u32x4_t*>(vt[buf] + value_piece<DIM>(row, my_piece)) = vs[p];
+      odd = __syncthreads_or((int)bad) != 0;
     }
-    if (edge) return __syncthreads_or((int)bad) != 0;
+#pragma unroll
+    for (int p = 0; p < kStage; ++p) {
+      *reinterpret_cast<u32x4_t*>(kt[buf] + p * kStep * DIM * 2 + k_in) = ks[p];
+      *reinterpret_cast<u32x4_t*>(vt[buf] + p * kStep * DIM * 2 + v_in) = vs[p];
+    }
     __syncthreads();
-    return false;
-  };
-
-  if (k0 < k1) {
-    lookup(k0);
-    fetch(k0);
-    lookup(k0 + kKeys);
-  }
-  for (int kb = k0, buf = 0; kb < k1; kb += kKeys, buf ^= 1) {
-    const bool odd = park(kb, buf);
-    if (kb + kKeys < k1) {
-      fetch(kb + kKeys);
-      lookup(kb + 2 * kKeys);
-    }
+    if (kb + kKeys < k1) fetch(kb + kKeys);
 
     f32x16_t sc[2];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) sc[t][e] = 0.0f;
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
         const u32x4_t kf =
-            *reinterpret_cast<const u32x4_t*>(kt[buf] + key_piece<DIM>(32 * t + x, 2 * c + h));
+            *reinterpret_cast<const u32x4_t*>(kt[buf] + 32 * t * DIM * 2 + k_out[c]);
         sc[t] = mma32<BF16>(kf, qf[c], sc[t]);
       }
+    // four reads ahead of the products
+    __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
+#pragma unroll
+    for (int i = 0; i < 2 * NC - 4; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
     }
-    const bool masked = kb + kKeys - 1 > first_limit;
-    if (masked) {
+    __builtin_amdgcn_sched_group_barrier(kMfma, 4, 0);
+    if (kb + kKeys - 1 > first_limit) {
+      const int last = limit - kb - 4 * h;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          sc[t][e] = kb + 32 * t + 8 * (e >> 2) + 4 * h + (e & 3) > limit ? -INFINITY : sc[t][e];
+          sc[t][e] = 32 * t + 8 * (e >> 2) + (e & 3) > last ? -INFINITY : sc[t][e];
     }
     float top = -INFINITY;
 #pragma unroll
@@ -367,7 +404,6 @@ __global__ __launch_bounds__(kThreads, 2) void attention_tiles_kernel(TileArgs s
         pf[2 * t + (w >> 2)][w & 3] = pack2<BF16>(a, b);
       }
     l += part;
-
     if (odd) add_odd_step<BF16, DIM>(kt[0], vt[buf], pf, kb, limit, &acc);
 #pragma unroll
     for (int u = 0; u < 4; ++u)             // 16 keys at a time
@@ -376,17 +412,36 @@ __global__ __launch_bounds__(kThreads, 2) void attention_tiles_kernel(TileArgs s
         u32x4_t vf;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          const int row = 16 * u + 8 * half + 4 * h + ((lane & 15) >> 2);
-          const int at = value_piece<DIM>(row, 4 * d + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) +
-                         (lane & 1) * 8;
           const s16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) s16x4_t*)(vt[buf] + at));
+              (__attribute__((address_space(3))) s16x4_t*)(vt[buf] +
+                                                            (16 * u + 8 * half) * DIM * 2 +
+                                                            v_out[d]));
           const u32x2_t b = __builtin_bit_cast(u32x2_t, v);
           vf[2 * half] = b[0];
           vf[2 * half + 1] = b[1];
         }
         acc[d] = mma32<BF16>(vf, pf[u], acc[d]);
       }
+    __builtin_amdgcn_sched_group_barrier(kDsRead, 8, 0);
+#pragma unroll
+    for (int i = 0; i < 4 * ND - 4; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kMfma, 4, 0);
+  };
+
+  if (k0 < k1) {
+    lookup(k0);
+    if (ALIGNED) {
+      group_at = place(row_key(k0, 0), id[0]);
+      lookup(k0 + kWindow);
+    }
+    fetch(k0);
+  }
+  for (int kb = k0; kb < k1; kb += 2 * kKeys) {
+    step(kb, std::integral_constant<int, 0>());
+    if (kb + kKeys < k1) step(kb + kKeys, std::integral_constant<int, 1>());
   }
 
   if (bad_page) raise_status(s.a.d_status, bad_page);
@@ -506,7 +561,8 @@ int launch(const TileArgs& s, const Plan& p, hipStream_t stream) {
     hipLaunchKernelGGL(tile_starts_kernel, dim3(1), dim3(1024), 0, stream, s);
     if (hipGetLastError() != hipSuccess) return PAIR_EHIP;
   }
-  if (s.page.d % 16 == 0)
+  // 16 slots within 32 bits of offset: any sensible layout
+  if (s.page.d % 16 == 0 && s.a.cache.slot_stride < ((int64_t)1 << 26))
     hipLaunchKernelGGL((attention_tiles_kernel<BF16, DIM, true>), dim3((unsigned)grid),
                        dim3(kThreads), 0, stream, s);
   else
