@@ -500,15 +500,17 @@ def _grad_table(tensors, name):
     """Host arrays of the tensors' addresses, sizes and types for one call; a
     model has hundreds, so each property is gathered in one go."""
     T = torch.Tensor
-    if not all(isinstance(t, T) for t in tensors):
+    if not all(issubclass(t, T) for t in set(map(type, tensors))):
         raise ValueError(f"{name} must be tensors")
     devices = set(map(T.get_device, tensors))
     if len(devices) > 1 or -1 in devices or not all(map(T.is_contiguous, tensors)):
         raise ValueError(f"{name} must be contiguous CUDA (HIP) tensors of one device")
-    try:
-        code = array.array("i", map(_DTYPE_CODE.__getitem__, map(T.dtype.__get__, tensors)))
-    except KeyError as e:
-        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {e.args[0]}") from None
+    dtypes = list(map(T.dtype.__get__, tensors))
+    kinds = set(dtypes)
+    for t in kinds - _DTYPE_CODE.keys():
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t}")
+    code = (array.array("i", [_DTYPE_CODE[dtypes[0]]]) * len(dtypes) if len(kinds) == 1
+            else array.array("i", map(_DTYPE_CODE.__getitem__, dtypes)))
     return (array.array("Q", map(T.data_ptr, tensors)), array.array("q", map(T.numel, tensors)), code)
 
 
@@ -752,6 +754,30 @@ def cps_draw(offsets, w, n, seed, rep0, R, gmax, nv=None, stream=None):
     return out
 
 
+_status_words = {}
+
+
+def _status(device):
+    """A zeroed status word of the current stream.  Words are cleared 256 at a
+    time by one fill on the stream that will use them (a fill for every call
+    took 5 us of the 15 to 30 that the small calls take); under graph capture
+    each call records its own fill, so that every replay clears its word."""
+    if torch.cuda.is_current_stream_capturing():
+        return torch.zeros(1, dtype=torch.int32, device=device)
+    key = (device, _stream(None))
+    words = _status_words.get(key)
+    if not words:
+        with torch.inference_mode(False):
+            words = list(torch.zeros(256, dtype=torch.int32, device=device).split(1))
+        _status_words[key] = words
+    return words.pop()
+
+
+@functools.lru_cache(maxsize=256)
+def _attention_workspace(*sizes):
+    return pair_paged_attention_workspace_bytes(*sizes)
+
+
 @_allocating
 def page_plan(cached, fresh, table, free_pages, free_count, page, max_tokens, mask=None,
               stream=None):
@@ -761,21 +787,20 @@ def page_plan(cached, fresh, table, free_pages, free_count, page, max_tokens, ma
     place; `free_pages` int32 lists the pool's pages, the first `free_count`
     (int64 [1], on the GPU) of them free, and the new list and count come back
     as `free_pages` and `free_count`.  `max_tokens` bounds the new tokens."""
-    n, dev = cached.numel(), cached.device
-    out = {
-        "q_offsets": torch.empty(n + 1, dtype=torch.int64, device=dev),
-        "lens": torch.empty(n, dtype=torch.int32, device=dev),
-        "slots": torch.empty(max_tokens, dtype=torch.int64, device=dev),
-        "positions": torch.empty(max_tokens, dtype=torch.int32, device=dev),
-        "table": table,
-        "free_pages": torch.empty_like(free_pages),
-        "free_count": torch.empty(1, dtype=torch.int64, device=dev),
-        "status": torch.zeros(1, dtype=torch.int32, device=dev),
-    }
-    ws = torch.empty(pair_page_plan_workspace_bytes(n), dtype=torch.uint8, device=dev)
+    n, dev, cap = cached.numel(), cached.device, free_pages.numel()
+    # two allocations; the workspace, which must be aligned, comes first
+    scratch = pair_page_plan_workspace_bytes(n) // 4
+    ws, lens, positions, new_free = torch.empty(
+        scratch + n + max_tokens + cap, dtype=torch.int32, device=dev).split(
+            [scratch, n, max_tokens, cap])
+    q_offsets, slots, new_count = torch.empty(
+        n + 1 + max_tokens + 1, dtype=torch.int64, device=dev).split([n + 1, max_tokens, 1])
+    out = {"q_offsets": q_offsets, "lens": lens, "slots": slots, "positions": positions,
+           "table": table, "free_pages": new_free, "free_count": new_count,
+           "status": _status(dev)}
     pair_page_plan(n, cached, fresh, mask, page, table, free_pages, free_count, max_tokens,
                    out["q_offsets"], out["lens"], out["slots"], out["positions"],
-                   out["free_pages"], out["free_count"], ws, out["status"], stream)
+                   out["free_pages"], out["free_count"], ws.view(torch.uint8), out["status"], stream)
     return out
 
 
@@ -783,7 +808,7 @@ def page_plan(cached, fresh, table, free_pages, free_count, page, max_tokens, ma
 def cache_store(k, v, slots, k_cache, v_cache, stream=None):
     """New keys and values [tokens][kv_heads][dim] into their slots of the
     caches [pages][page][kv_heads][dim]; negative slots are skipped."""
-    st = torch.zeros(1, dtype=torch.int32, device=k_cache.device)
+    st = _status(k_cache.device)
     pair_cache_store(k, v, slots, k_cache, v_cache, st, stream)
     return {"k_cache": k_cache, "v_cache": v_cache, "status": st}
 
@@ -800,11 +825,10 @@ def paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max_len,
     if out is None:
         out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=dev)
     lse = torch.empty((tokens, heads), dtype=torch.float32, device=dev) if want_lse else None
-    need = pair_paged_attention_workspace_bytes(lens.numel(), tokens, heads, k_cache.shape[2], dim,
-                                                max_q, max_len)
+    need = _attention_workspace(lens.numel(), tokens, heads, k_cache.shape[2], dim, max_q, max_len)
     if workspace is None or workspace.numel() < need:
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    st = torch.zeros(1, dtype=torch.int32, device=dev)
+    st = _status(dev)
     pair_paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max_len,
                          dim ** -0.5 if scale is None else scale, out, lse, workspace, st, stream)
     return {"out": out, "lse": lse, "status": st}
@@ -822,7 +846,7 @@ def clip_grads(grads, max_norm, out=None, stream=None):
     dev = grads[0].device
     norm = torch.empty(1, dtype=torch.float32, device=dev)
     coef = torch.empty(1, dtype=torch.float32, device=dev)
-    st = torch.zeros(1, dtype=torch.int32, device=dev)
+    st = _status(dev)
     ws = torch.empty(pair_clip_grads_workspace_bytes(len(grads)), dtype=torch.uint8, device=dev)
     pair_clip_grads(grads, max_norm, norm, coef, ws, out, st, stream)
     return {"norm": norm, "coef": coef, "out": grads if out is None else out, "status": st}

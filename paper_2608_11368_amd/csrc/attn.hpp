@@ -12,6 +12,7 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
 // D[m][n] += sum_k A[m][k] B[k][n] over one wave.  16x16x32: lane (x = lane & 15,
@@ -43,8 +44,8 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const f32x2_t v = {a, b};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
   }
-  const uint32_t lo = __builtin_bit_cast(uint16_t, (_Float16)a);
-  return lo | ((uint32_t)__builtin_bit_cast(uint16_t, (_Float16)b) << 16);
+  const f32x2_t v = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2_t));
 }
 
 template <bool BF16>

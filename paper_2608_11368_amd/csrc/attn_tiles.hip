@@ -186,7 +186,7 @@ __device__ __forceinline__ void add_odd_step(unsigned char* keys, unsigned char*
 }
 
 template <bool BF16, int DIM, bool ALIGNED>
-__global__ __launch_bounds__(kThreads, 2) void attention_tiles_kernel(TileArgs s) {
+__global__ __launch_bounds__(kThreads, DIM == 64 ? 3 : 2) void attention_tiles_kernel(TileArgs s) {
   constexpr int NC = DIM / 16;              // k pieces of a score product
   constexpr int ND = DIM / 32;              // dim tiles of the output
   constexpr int kPer = DIM / 8;             // 16-byte pieces of a row
@@ -344,6 +344,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_tiles_kernel(TileArgs s
     if (kb + kKeys < k1) fetch(kb + kKeys);
 
     f32x16_t sc[2];
+    __builtin_amdgcn_s_setprio(1);          // over a wave that is at its softmax
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -364,6 +365,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_tiles_kernel(TileArgs s
       __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
     }
     __builtin_amdgcn_sched_group_barrier(kMfma, 4, 0);
+    __builtin_amdgcn_s_setprio(0);
     if (kb + kKeys - 1 > first_limit) {
       const int last = limit - kb - 4 * h;
 #pragma unroll
@@ -405,6 +407,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_tiles_kernel(TileArgs s
       }
     l += part;
     if (odd) add_odd_step<BF16, DIM>(kt[0], vt[buf], pf, kb, limit, &acc);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int u = 0; u < 4; ++u)             // 16 keys at a time
 #pragma unroll
@@ -429,6 +432,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_tiles_kernel(TileArgs s
       __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
     }
     __builtin_amdgcn_sched_group_barrier(kMfma, 4, 0);
+    __builtin_amdgcn_s_setprio(0);
   };
 
   if (k0 < k1) {
