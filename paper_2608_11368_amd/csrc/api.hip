@@ -408,6 +408,8 @@ static int check_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t k
       q_heads / kv_heads > 64)
     return PAIR_ERANGE;
   if (dim != 64 && dim != 128) return PAIR_ERANGE;
+  // rows and key positions are counted in 31 bits, with room for a window ahead
+  if (tokens > kMaxSlots / q_heads || max_len > kMaxSlots / 2) return PAIR_ERANGE;
   if (max_q < 0 || max_len < 0 || (tokens > 0 && max_q < 1)) return PAIR_ERANGE;
   return PAIR_OK;
 }

@@ -33,7 +33,8 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kRows = 32 * kWaves;          // of a tile
 constexpr int kKeys = 64;                   // of a step
 constexpr float kLazy = 8.0f;
-constexpr int kInline = kThreads;           // requests that a workgroup scans itself
+constexpr int kClasses = 8;                 // of work, in the order of the tiles
+constexpr int kInline = 256;                // requests that a workgroup orders itself
 
 // kinds of instructions in a scheduling group
 constexpr int kMfma = 0x8, kDsRead = 0x100;
@@ -87,37 +88,98 @@ __global__ __launch_bounds__(1024) void tile_starts_kernel(TileArgs s) {
   if (bad) raise_status(s.a.d_status, bad);
 }
 
-// The request of tile `back` from the end, and the tile's number in it; false
-// past the first tile.  The last tiles of a request see the most keys, so the
-// order starts with them.
-__device__ __forceinline__ bool find_tile(const TileArgs& s, int64_t back, int64_t* request,
-                                          int* tile) {
-  __shared__ int32_t start[kInline + 1];
-  __shared__ int32_t ends[kWaves];
+__device__ __forceinline__ int wave_sum_i(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, false);
+  return __builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16) +
+         __builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48);
+}
+
+// Tile `at` of the call: the request, and the tile's number in it; false past the
+// last.  Every wave holds the requests in its lanes, SETS each.  The order is by
+// falling work, so that the last workgroups to start are the shortest, but only
+// in kClasses classes of the keys seen: within a class request by request, so
+// that the workgroups that run at one time share a request's keys in their
+// caches.  (8 prompts of 300 to 4096 tokens at width 64: 157 us in the order of
+// the requests, 147 us strictly by work, 151 us so.  8 chunks of 2048 tokens over
+// 8192 keys, 16 heads of width 128: 1441 us strictly by work, 1300 us so.)  The
+// tiles of more than w steps are counted request by request in closed form.
+template <int SETS>
+__device__ __forceinline__ bool find_ordered(const TileArgs& s, int64_t at, Request* q,
+                                             int64_t* request, int* tile) {
   const int n = (int)s.a.n, lane = threadIdx.x & (kWave - 1);
-  if (n <= kInline) {
-    int32_t bad = 0;
-    const int32_t mine = (int)threadIdx.x < n ? tiles_of(s, threadIdx.x, &bad) : 0;
-    if (bad && blockIdx.x == 0) raise_status(s.a.d_status, bad);
-    int32_t scan = mine;
+  Request own[SETS];
+  int tiles[SETS];
+  int32_t bad = 0;
+#pragma unroll
+  for (int i = 0; i < SETS; ++i) {
+    const int r = i * kWave + lane;
+    own[i] = Request{0, 0, 0};
+    tiles[i] = 0;
+    if (r < n && attention_request(s.a, s.page.d, r, &own[i], &bad)) {
+      const int rows = own[i].tokens * (int)s.group.d;
+      if (rows >= s.least) tiles[i] = (rows + kRows - 1) / kRows;
+    }
+  }
+  if (bad && blockIdx.x == 0 && threadIdx.x < kWave) raise_status(s.a.d_status, bad);
+  auto longer = [&](int i, int w) {         // tiles of set i's request of more than w steps
+    if (w < 0) return tiles[i];
+    int64_t token = (int64_t)w * kKeys - (own[i].len - own[i].tokens);   // first that sees more
+    if (token < 0) token = 0;
+    if (token >= own[i].tokens) return 0;
+    return tiles[i] - (int)token * (int)s.group.d / kRows;
+  };
+  auto total = [&](int w) {
+    int v = 0;
+#pragma unroll
+    for (int i = 0; i < SETS; ++i) v += tiles[i] > 0 ? longer(i, w) : 0;
+    return wave_sum_i(v);
+  };
+  if (at >= total(-1)) return false;
+  const int steps = (s.a.max_len + kKeys - 1) / kKeys;
+  const int each = (steps + kClasses - 1) / kClasses;
+  int hi = kClasses * each, lo = hi - each;     // until total(lo) > at >= total(hi)
+  while (lo > 0 && total(lo) <= at) {
+    hi = lo;
+    lo -= each;
+  }
+  if (lo <= 0) lo = -1;                         // tiles that see nothing, too
+  int left = (int)(at - total(hi));
+#pragma unroll
+  for (int i = 0; i < SETS; ++i) {
+    const int mine = tiles[i] > 0 ? longer(i, lo) - longer(i, hi) : 0;
+    int scan = mine;
 #pragma unroll
     for (int by = 1; by < kWave; by <<= 1) {
-      const int32_t v = __shfl_up(scan, by, kWave);
+      const int v = __shfl_up(scan, by, kWave);
       if (lane >= by) scan += v;
     }
-    if (lane == kWave - 1) ends[threadIdx.x / kWave] = scan;
-    if (threadIdx.x == 0) start[0] = 0;
-    __syncthreads();
-    for (int w = 0; w < (int)threadIdx.x / kWave; ++w) scan += ends[w];
-    start[threadIdx.x + 1] = scan;
-    __syncthreads();
-    const int64_t t = start[kInline] - 1 - back;
-    if (t < 0) return false;
-    const int r = __syncthreads_count(start[threadIdx.x + 1] <= t);
-    *request = r;
-    *tile = uniform((int)t - start[r]);
+    const int all = __builtin_amdgcn_readlane(scan, kWave - 1);
+    if (left >= all) {
+      left -= all;
+      continue;
+    }
+    const int x = uniform(__popcll(__ballot(scan <= left)));
+    *request = i * kWave + x;
+    *tile = __builtin_amdgcn_readlane(tiles[i] > 0 ? tiles[i] - longer(i, hi) - 1 + scan - mine : 0,
+                                      x) - left;
+    q->tokens = __builtin_amdgcn_readlane(own[i].tokens, x);
+    q->len = __builtin_amdgcn_readlane(own[i].len, x);
+    q->q0 = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane(
+                           (int)(uint32_t)((uint64_t)own[i].q0 >> 32), x) << 32) |
+                      (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)own[i].q0, x));
     return true;
   }
+  return false;
+}
+
+// The same for more requests, from the tiles counted before each, and only in
+// the order of the last tile first: with so many of them the ends even out.
+__device__ __forceinline__ bool find_counted(const TileArgs& s, int64_t back, Request* q,
+                                             int64_t* request, int* tile) {
+  const int n = (int)s.a.n;
   const int64_t t = (int64_t)s.starts[n] - 1 - back;
   if (t < 0) return false;
   int lo = 0, hi = n;                       // starts[lo] <= t < starts[hi]
@@ -131,7 +193,8 @@ __device__ __forceinline__ bool find_tile(const TileArgs& s, int64_t back, int64
   }
   *request = uniform(lo);
   *tile = uniform((int)(t - s.starts[lo]));
-  return true;
+  int32_t bad = 0;
+  return attention_request(s.a, s.page.d, lo, q, &bad);
 }
 
 // 16-byte piece `c` of LDS row `row` of a step's keys, and of its values.
@@ -204,10 +267,15 @@ __global__ __launch_bounds__(kThreads, DIM == 64 ? 3 : 2) void attention_tiles_k
   const int split = (int)((blockIdx.x / heads) % s.splits);
   int64_t r;
   int tile;
-  if (!find_tile(s, blockIdx.x / (heads * s.splits), &r, &tile)) return;
   Request q;
-  int32_t bad = 0;
-  if (!attention_request(s.a, s.page.d, r, &q, &bad)) return;
+  const int64_t place_in_order = blockIdx.x / (heads * s.splits);
+  if (s.a.n <= kWave) {
+    if (!find_ordered<1>(s, place_in_order, &q, &r, &tile)) return;
+  } else if (s.a.n <= kInline) {
+    if (!find_ordered<kInline / kWave>(s, place_in_order, &q, &r, &tile)) return;
+  } else if (!find_counted(s, place_in_order, &q, &r, &tile)) {
+    return;
+  }
   const int rows = q.tokens * (int)s.group.d;
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
   const int x = lane & 31, h = lane >> 5;
