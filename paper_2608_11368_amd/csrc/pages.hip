@@ -54,31 +54,24 @@ __device__ __forceinline__ uint32_t pages_of(uint32_t tokens, const FastDiv& pag
   return tokens == 0 ? 0u : div_by(tokens - 1, page) + 1;
 }
 
-// What request r takes and gives; its length after the step in *len.
+// What a request takes and gives, and its length after the step in *len (no
+// branches: the loads before it are then in flight together).
+__device__ __forceinline__ Counts counts_of(const PlanArgs& a, int32_t c, int32_t f, bool live,
+                                            int32_t* len, int32_t* bad) {
+  const bool sane = (c | f) >= 0 && (uint32_t)c + (uint32_t)f <= 0x7fffffffu;
+  const uint32_t cached = sane ? (uint32_t)c : 0u, fresh = sane ? (uint32_t)f : 0u;
+  const uint32_t held = pages_of(cached, a.page);
+  const uint32_t all = live ? pages_of(cached + fresh, a.page) : held;
+  const bool fits = (int64_t)all <= a.ldt;
+  *bad |= sane ? (fits ? 0 : PAIR_ST_PAGES) : PAIR_ST_LENGTH;
+  const bool goes = sane && fits && live;
+  *len = goes ? (int32_t)(cached + fresh) : 0;
+  return Counts{goes ? fresh : 0u, goes ? all - held : 0u, sane && fits && !live ? held : 0u};
+}
+
 __device__ __forceinline__ Counts request(const PlanArgs& a, int64_t r, int32_t* len,
                                           int32_t* bad) {
-  const int32_t c = a.cached[r], f = a.fresh[r];
-  const bool live = a.mask == nullptr || a.mask[r] != 0;
-  Counts k = {0u, 0u, 0u};
-  *len = 0;
-  if (c < 0 || f < 0 || (int64_t)c + f > 0x7fffffff) {
-    *bad |= PAIR_ST_LENGTH;
-    return k;
-  }
-  const uint32_t held = pages_of((uint32_t)c, a.page);
-  const uint32_t all = live ? pages_of((uint32_t)c + (uint32_t)f, a.page) : held;
-  if ((int64_t)all > a.ldt) {
-    *bad |= PAIR_ST_PAGES;
-    return k;
-  }
-  if (live) {
-    k.tokens = (uint32_t)f;
-    k.taken = all - held;
-    *len = c + f;
-  } else {
-    k.given = held;
-  }
-  return k;
+  return counts_of(a, a.cached[r], a.fresh[r], a.mask == nullptr || a.mask[r] != 0, len, bad);
 }
 
 __device__ __forceinline__ Counts shfl_up(const Counts& v, int by) {
@@ -129,14 +122,28 @@ __device__ __forceinline__ int owner(const uint32_t* ends, uint32_t x, int lo, i
   return lo;
 }
 
-// Entry j of the pool: the free list, then the released requests' pages.
-__device__ __forceinline__ int32_t pool_entry(const PlanArgs& a, const Ends& e, uint32_t j,
-                                              uint32_t free, int lo, int hi) {
-  if (j < free) return a.free_pages[j];
-  const uint32_t x = j - free;
-  const int r = owner(e.given, x, lo, hi);
-  const uint32_t at = x - (r > 0 ? e.given[r - 1] : 0u);
-  return a.table[(int64_t)r * a.ldt + at];
+// The same for two numbers by a whole wave, 64 probes of each at a time.
+__device__ __forceinline__ void wave_owners(const uint32_t* ends, uint32_t x, uint32_t y, int last,
+                                            int32_t* out) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int lo[2] = {0, 0}, hi[2] = {last, last};
+  const uint32_t want[2] = {x, y};
+  while (lo[0] < hi[0] || lo[1] < hi[1]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int step = (hi[k] - lo[k] + kWave - 1) / kWave;
+      const int i = lo[k] + lane * step;
+      const int below = __popcll(__ballot(i < hi[k] && ends[i < hi[k] ? i : 0] <= want[k]));
+      if (below == 0) {
+        hi[k] = lo[k];
+      } else {
+        const int top = lo[k] + below * step;
+        lo[k] += (below - 1) * step + 1;
+        hi[k] = top < hi[k] ? top : hi[k];
+      }
+    }
+  }
+  if (lane < 2) out[lane] = lane == 0 ? lo[0] : lo[1];
 }
 
 __device__ __forceinline__ uint32_t free_pages_of(const PlanArgs& a) {
@@ -145,33 +152,97 @@ __device__ __forceinline__ uint32_t free_pages_of(const PlanArgs& a) {
 }
 
 constexpr int kTile = 4 * kThreads;   // outputs of a workgroup
+constexpr int kNear = 512;            // requests that a tile keeps in LDS
+
+// A scan's ends over the requests [lo, hi] that a tile needs: in LDS where they
+// fit, else where they were.
+struct Near {
+  const uint32_t* ends;
+  int lo, hi;        // requests
+  int base;          // request of ends[0]
+  uint32_t before;   // end of request lo - 1
+};
+
+__device__ __forceinline__ void find(const Near& n, uint32_t x, int* r, uint32_t* start) {
+  const int i = owner(n.ends, x, n.lo - n.base, n.hi - n.base);
+  *r = i + n.base;
+  *start = *r > n.lo ? n.ends[i - 1] : n.before;
+}
 
 // Outputs [tile * kTile, ...) of the tokens, then of the pages (the taken ones
-// into the table, the rest into the new list).
-__device__ void plan_outputs(const PlanArgs& a, const Ends& e, const Counts& total,
-                             int64_t tile, int64_t token_tiles) {
+// into the table, the rest into the new list).  NARROW: the ends are in memory;
+// the tile's first and last owners are found first, by a wave each, and what
+// lies between them is fetched at one go, so that an output costs two loads in
+// turn and not one for every halving.
+template <bool NARROW>
+__device__ __forceinline__ void plan_outputs(const PlanArgs& a, const Ends& e,
+                                             const Counts& total, int64_t tile,
+                                             int64_t token_tiles) {
+  __shared__ int32_t bound[6];
+  __shared__ uint32_t near[3][NARROW ? kNear : 1];
   const int last = (int)a.n - 1;
+  const int wave = uniform(threadIdx.x / kWave);
   const uint32_t free = free_pages_of(a);
   const uint32_t avail = sat_add(free, total.given);
+  auto locate = [&](int i, const uint32_t* ends, uint32_t x, uint32_t y) {
+    if (NARROW && wave == i) wave_owners(ends, x, y, last, bound + 2 * i);
+  };
+  auto stage = [&](int i, const uint32_t* ends) {          // after the bounds are known
+    Near n = {ends, 0, last, 0, 0u};
+    if (!NARROW) return n;
+    n.lo = bound[2 * i];
+    n.hi = bound[2 * i + 1];
+    n.before = n.lo > 0 ? ends[n.lo - 1] : 0u;
+    if (n.hi - n.lo < kNear) {
+      for (int k = threadIdx.x; k <= n.hi - n.lo; k += kThreads) near[i][k] = ends[n.lo + k];
+      n.ends = near[i];
+      n.base = n.lo;
+    }
+    return n;
+  };
+  auto pool_entry = [&](const Near& given, uint32_t j) {   // the free list, then the released
+    if (j < free) return a.free_pages[j];
+    int r;
+    uint32_t start;
+    find(given, j - free, &r, &start);
+    return a.table[(int64_t)r * a.ldt + (j - free - start)];
+  };
   if (tile < token_tiles) {
     const int64_t t0 = tile * kTile;
+    locate(0, e.tokens, (uint32_t)t0, (uint32_t)(t0 + kTile - 1));
+    if (NARROW) __syncthreads();
+    const Near owners = stage(0, e.tokens);
+    const bool staged = NARROW && owners.ends == near[0];
+    if (staged) {
+      for (int k = threadIdx.x; k <= owners.hi - owners.lo; k += kThreads) {
+        const int r = owners.lo + k;
+        near[1][k] = (uint32_t)a.cached[r];
+        near[2][k] = r > 0 ? e.taken[r - 1] : 0u;
+      }
+    }
+    if (NARROW) __syncthreads();
+    const Near anyone = {e.given, 0, last, 0, 0u};
+#pragma unroll
     for (int s = 0; s < kTile / kThreads; ++s) {
       const int64_t t = t0 + s * kThreads + threadIdx.x;
       if (t >= a.max_tokens) break;
       int64_t slot = -1;
       int32_t pos = -1;
       if ((uint32_t)t < total.tokens) {
-        const int r = owner(e.tokens, (uint32_t)t, 0, last);
-        const uint32_t c = (uint32_t)a.cached[r];
-        const uint32_t x = c + (uint32_t)t - (r > 0 ? e.tokens[r - 1] : 0u);
+        int r;
+        uint32_t start;
+        find(owners, (uint32_t)t, &r, &start);
+        const uint32_t c = staged ? near[1][r - owners.lo] : (uint32_t)a.cached[r];
+        const uint32_t x = c + (uint32_t)t - start;
         const uint32_t held = pages_of(c, a.page);
         const uint32_t pg = div_by(x, a.page);
         int32_t id;
         if (pg < held) {
           id = a.table[(int64_t)r * a.ldt + pg];
         } else {
-          const uint32_t j = (r > 0 ? e.taken[r - 1] : 0u) + (pg - held);
-          id = j < avail ? pool_entry(a, e, j, free, 0, last) : -1;
+          const uint32_t first = staged ? near[2][r - owners.lo] : (r > 0 ? e.taken[r - 1] : 0u);
+          const uint32_t j = first + (pg - held);
+          id = j < avail ? pool_entry(anyone, j) : -1;
         }
         pos = (int32_t)x;
         if (id >= 0) slot = (int64_t)id * a.page.d + (x - pg * a.page.d);
@@ -183,16 +254,26 @@ __device__ void plan_outputs(const PlanArgs& a, const Ends& e, const Counts& tot
   }
   const int64_t j0 = (tile - token_tiles) * kTile;
   const uint32_t used = total.taken < avail ? total.taken : avail;
+  const uint32_t first = (uint32_t)j0, final = (uint32_t)j0 + kTile - 1;
+  auto released = [&](uint32_t j) { return j > free ? j - free : 0u; };
+  locate(0, e.taken, first, final);
+  locate(1, e.given, released(first), released(final));
+  locate(2, e.given, released(used + first), released(used + final));
+  if (NARROW) __syncthreads();
+  const Near takers = stage(0, e.taken), givers = stage(1, e.given), later = stage(2, e.given);
+  if (NARROW) __syncthreads();
+#pragma unroll
   for (int s = 0; s < kTile / kThreads; ++s) {
     const int64_t j = j0 + s * kThreads + threadIdx.x;
     if (j >= a.capacity) break;
     const uint32_t from = used + (uint32_t)j;
-    a.free_out[j] = from < avail ? pool_entry(a, e, from, free, 0, last) : -1;
+    a.free_out[j] = from < avail ? pool_entry(later, from) : -1;
     if ((uint32_t)j < used) {
-      const int r = owner(e.taken, (uint32_t)j, 0, last);
+      int r;
+      uint32_t start;
+      find(takers, (uint32_t)j, &r, &start);
       const uint32_t held = pages_of((uint32_t)a.cached[r], a.page);
-      const uint32_t at = held + (uint32_t)j - (r > 0 ? e.taken[r - 1] : 0u);
-      a.table[(int64_t)r * a.ldt + at] = pool_entry(a, e, (uint32_t)j, free, 0, last);
+      a.table[(int64_t)r * a.ldt + held + ((uint32_t)j - start)] = pool_entry(givers, (uint32_t)j);
     }
   }
 }
@@ -258,7 +339,7 @@ __global__ __launch_bounds__(kThreads) void plan_fused_kernel(PlanArgs a, int64_
     if (bad) raise_status(a.d_status, bad);
     plan_totals(a, e, total);
   }
-  plan_outputs(a, e, total, blockIdx.x, token_tiles);
+  plan_outputs<false>(a, e, total, blockIdx.x, token_tiles);
 }
 
 // More requests: a first launch writes the scans' ends to the workspace.  Each
@@ -270,7 +351,19 @@ __global__ __launch_bounds__(kScan) void plan_scan_kernel(PlanArgs a, uint32_t* 
   const int64_t r0 = (int64_t)blockIdx.x * kScan;
   int32_t bad = 0, other = 0, len;
   Counts sum = {0u, 0u, 0u};
-  for (int64_t r = threadIdx.x; r < r0; r += kScan) sum = sum + request(a, r, &len, &other);
+  // r0 is a multiple of kScan: four requests of a lane at a time
+  for (int64_t r = 4 * threadIdx.x; r < r0; r += 4 * kScan) {
+    typedef u32x4_t u32x4_a4 __attribute__((aligned(4)));
+    typedef uint32_t u32_a1 __attribute__((aligned(1)));
+    const u32x4_t cached = *reinterpret_cast<const u32x4_a4*>(a.cached + r);
+    const u32x4_t fresh = *reinterpret_cast<const u32x4_a4*>(a.fresh + r);
+    const uint32_t live =
+        a.mask != nullptr ? *reinterpret_cast<const u32_a1*>(a.mask + r) : 0x01010101u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      sum = sum + counts_of(a, (int32_t)cached[i], (int32_t)fresh[i],
+                            ((live >> (8 * i)) & 0xffu) != 0, &len, &other);
+  }
   Counts before, total;
   group_scan<kScan>(sum, &before);
   const int64_t r = r0 + threadIdx.x;
@@ -293,7 +386,7 @@ __global__ __launch_bounds__(kThreads) void plan_write_kernel(PlanArgs a, const 
   const Ends e = {ends, ends + a.n, ends + 2 * a.n};
   const Counts total = {e.tokens[a.n - 1], e.taken[a.n - 1], e.given[a.n - 1]};
   if (blockIdx.x == 0) plan_totals(a, e, total);
-  plan_outputs(a, e, total, blockIdx.x, token_tiles);
+  plan_outputs<true>(a, e, total, blockIdx.x, token_tiles);
 }
 
 // ------------------------------------------------------------------ store --
