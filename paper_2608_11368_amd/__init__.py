@@ -181,6 +181,7 @@ def _dev(t, name, dtype, numel=None, allow_none=False):
 # The current stream's handle without a Stream object, where torch has the call
 # (0.2 us against 2.8 us, of a call that takes 15 to 30 in all).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device_index = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream):
@@ -188,7 +189,7 @@ def _stream(stream):
         return stream.cuda_stream
     if _raw_stream is None:
         return torch.cuda.current_stream().cuda_stream
-    return _raw_stream(torch.cuda.current_device())
+    return _raw_stream(_device_index())
 
 
 def _scores_arg(scores):
@@ -424,7 +425,13 @@ def pair_page_plan(n, cached, fresh, mask, page, table, free_pages, free_count, 
 
 
 def _cache_arg(k_cache, v_cache):
-    """Pointers, element type and layout of a key and a value cache."""
+    """Pointers, element type, layout and shape of a key and a value cache."""
+    if isinstance(k_cache, torch.Tensor) and isinstance(v_cache, torch.Tensor):
+        shape, strides, dtype = k_cache.shape, k_cache.stride(), k_cache.dtype
+        if (v_cache.shape == shape and v_cache.stride() == strides and v_cache.dtype is dtype
+                and len(shape) == 4 and strides[3] == 1 and k_cache.is_cuda and v_cache.is_cuda
+                and (dtype is torch.bfloat16 or dtype is torch.float16)):
+            return k_cache.data_ptr(), v_cache.data_ptr(), dtype, strides, shape
     for name, c in (("k_cache", k_cache), ("v_cache", v_cache)):
         if not isinstance(c, torch.Tensor) or not c.is_cuda or c.dim() != 4:
             raise ValueError(f"{name} must be a 4-D CUDA tensor [pages][page][kv_heads][dim]")
@@ -432,34 +439,34 @@ def _cache_arg(k_cache, v_cache):
         raise TypeError("the caches must be bfloat16 or float16")
     if v_cache.dtype != k_cache.dtype or v_cache.shape != k_cache.shape:
         raise ValueError("k_cache and v_cache must have the same type and shape")
-    if v_cache.stride() != k_cache.stride() or k_cache.stride(3) != 1:
-        raise ValueError("k_cache and v_cache must have the same strides and contiguous rows")
-    return k_cache.data_ptr(), v_cache.data_ptr(), _DTYPE_CODE[k_cache.dtype], k_cache.stride()
+    raise ValueError("k_cache and v_cache must have the same strides and contiguous rows")
 
 
 def _rows_arg(t, name, dtype, heads, dim):
-    """Pointer and strides of rows [tokens][heads][dim]."""
+    """Pointer, strides and shape of rows [tokens][heads][dim]."""
+    if isinstance(t, torch.Tensor):
+        shape, strides = t.shape, t.stride()
+        if (len(shape) == 3 and t.dtype is dtype and t.is_cuda and shape[2] == dim
+                and strides[2] == 1 and (heads is None or shape[1] == heads)):
+            return t.data_ptr(), strides[0], strides[1], shape
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 3:
         raise ValueError(f"{name} must be a 3-D CUDA tensor [tokens][heads][dim]")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, needs {heads} heads of {dim}")
-    if t.stride(2) != 1:
-        raise ValueError(f"{name} rows must be contiguous")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    raise ValueError(f"{name} rows must be contiguous")
 
 
 def pair_cache_store(k, v, slots, k_cache, v_cache, d_status=None, stream=None):
-    kc, vc, code, st = _cache_arg(k_cache, v_cache)
-    pages, page, heads, dim = k_cache.shape
-    kp, tok, head = _rows_arg(k, "k", k_cache.dtype, heads, dim)
-    vp, vtok, vhead = _rows_arg(v, "v", k_cache.dtype, heads, dim)
-    if (vtok, vhead) != (tok, head) or v.shape != k.shape:
+    kc, vc, dtype, st, (pages, page, heads, dim) = _cache_arg(k_cache, v_cache)
+    kp, tok, head, shape = _rows_arg(k, "k", dtype, heads, dim)
+    vp, vtok, vhead, vshape = _rows_arg(v, "v", dtype, heads, dim)
+    if vtok != tok or vhead != head or vshape != shape:
         raise ValueError("k and v must have the same shape and strides")
-    tokens = k.shape[0]
+    tokens = shape[0]
     _rc(lib().pair_cache_store(
-        tokens, heads, dim, code, kp, vp, tok, head, kc, vc, st[0], st[1], st[2], page, pages,
+        tokens, heads, dim, _DTYPE_CODE[dtype], kp, vp, tok, head, kc, vc, st[0], st[1], st[2], page, pages,
         _dev(slots, "slots", torch.int64, tokens), _dev(d_status, "d_status", torch.int32, 1, True),
         _stream(stream)), "pair_cache_store")
 
@@ -471,18 +478,16 @@ def pair_paged_attention_workspace_bytes(n, tokens, q_heads, kv_heads, dim, max_
 
 def pair_paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max_len, scale, out,
                          lse, workspace, d_status=None, stream=None):
-    kc, vc, code, st = _cache_arg(k_cache, v_cache)
-    pages, page, kv_heads, dim = k_cache.shape
-    qp, qt, qh = _rows_arg(q, "q", k_cache.dtype, None, dim)
-    tokens, heads = q.shape[0], q.shape[1]
-    op, ot, oh = _rows_arg(out, "out", k_cache.dtype, heads, dim)
+    kc, vc, dtype, st, (pages, page, kv_heads, dim) = _cache_arg(k_cache, v_cache)
+    qp, qt, qh, (tokens, heads, _) = _rows_arg(q, "q", dtype, None, dim)
+    op, ot, oh, oshape = _rows_arg(out, "out", dtype, heads, dim)
     n = lens.numel()
     if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[0] < n:
         raise ValueError("table must be a 2-D tensor with a row for each request")
-    if out.shape[0] < tokens:
-        raise ValueError(f"out holds {out.shape[0]} tokens, needs {tokens}")
+    if oshape[0] < tokens:
+        raise ValueError(f"out holds {oshape[0]} tokens, needs {tokens}")
     _rc(lib().pair_paged_attention(
-        n, tokens, heads, kv_heads, dim, code, qp, qt, qh, kc, vc, st[0], st[1], st[2], page,
+        n, tokens, heads, kv_heads, dim, _DTYPE_CODE[dtype], qp, qt, qh, kc, vc, st[0], st[1], st[2], page,
         pages, _dev(table, "table", torch.int32), table.shape[1],
         _dev(q_offsets, "q_offsets", torch.int64, n + 1), _dev(lens, "lens", torch.int32, n),
         int(max_q), int(max_len), float(scale), op, ot, oh,
