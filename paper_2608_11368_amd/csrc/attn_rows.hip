@@ -573,14 +573,16 @@ Plan plan_rows(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim, int32_
   const int64_t rows = (int64_t)max_q * (q_heads / kv_heads);
   p.rows = (int)(rows < kRowsMost ? rows : kRowsMost);
   p.tiles = p.rows <= 16 ? 1 : 2;
-  // Cut into equal runs unless every head is a step or two anyway, or the
-  // requests are so many that they fill the card by themselves.
+  // Cut into equal runs unless the longest head is eight steps, which take less
+  // than the second launch would (4 requests of 700 keys: 10.9 us uncut, 16.5 us
+  // cut; of 1000: 14.3 and 16.4; of 2000: 24.7 and 16.7), or the requests are so
+  // many that they fill the card by themselves.
   const int64_t most = n * ((max_len + kUnit - 1) / kUnit);
   int64_t runs = 2 * (int64_t)device_cu_count() / kv_heads;   // two workgroups fit a compute unit
   if (runs > most) runs = most;
   if (runs > kMostRuns) runs = kMostRuns;
   if (runs < 1) runs = 1;
-  p.runs = n > kMostScanned || max_len <= 2 * kUnit ? 0 : (int32_t)runs;
+  p.runs = n > kMostScanned || max_len <= 8 * kUnit ? 0 : (int32_t)runs;
   const size_t parts = 2 * (size_t)p.runs * kv_heads * 16 * p.tiles;
   p.starts = ((size_t)(n + 1) * 4 + 255) / 256 * 256;
   p.ml = (parts * 8 + 255) / 256 * 256;
