@@ -629,7 +629,7 @@ size_t pair_paged_attention_workspace_bytes(int64_t n, int64_t tokens, int32_t q
  * effect on that token.  Scores, statistics and sums are fp32; exp(s_j - m)
  * is rounded to the type of v for the matrix cores.
  *
- *   n, tokens    requests and packed new tokens (rows of q and out)
+ *   n, tokens    requests, and rows of q and out
  *   q_heads      a multiple of kv_heads, at most 64 * kv_heads
  *   dim          head width: 64 or 128
  *   dtype        PAIR_BF16 or PAIR_F16, of q, the caches and out
@@ -637,7 +637,10 @@ size_t pair_paged_attention_workspace_bytes(int64_t n, int64_t tokens, int32_t q
  *                (strides multiples of 8; out likewise)
  *   table, ldt   int32 [n][ldt]; the first ceil(lens[r] / page) entries of row
  *                r are read
- *   q_offsets    int64 [n+1], q_offsets[0] = 0, q_offsets[n] = tokens
+ *   q_offsets    int64 [n+1], q_offsets[0] = 0, q_offsets[n] <= tokens: request
+ *                r has rows q_offsets[r] .. q_offsets[r+1] - 1; rows past the
+ *                last one's belong to no request and are not written, so that
+ *                a call may be made before the host knows how many continue
  *   lens         int32 [n]
  *   max_q, max_len  host bounds on Q_r and lens[r]
  *   lse          fp32 [tokens][q_heads] out                        (or NULL)

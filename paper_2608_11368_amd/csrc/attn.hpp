@@ -73,8 +73,7 @@ __device__ __forceinline__ bool attention_request(const AttnCall& a, uint32_t pa
                                                   Request* q, int32_t* bad) {
   const int64_t q0 = a.q_offsets[r], q1 = a.q_offsets[r + 1];
   const int32_t len = a.lens[r];
-  if ((r == 0 && q0 != 0) || (r == a.n - 1 && q1 != a.tokens)) *bad |= PAIR_ST_BAD_GROUP;
-  if (q0 < 0 || q1 < q0 || q1 > a.tokens) {
+  if (q0 < 0 || q1 < q0 || q1 > a.tokens || (r == 0 && q0 != 0)) {
     *bad |= PAIR_ST_BAD_GROUP;
     return false;
   }

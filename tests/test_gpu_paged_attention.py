@@ -255,6 +255,68 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(got["out"], want["out"]) and torch.equal(got["lse"], want["lse"])
 
 
+@pytest.mark.parametrize("new", [[2, 1], [60, 45]])
+def test_slots_far_apart(new):
+    """Slots 2^27 bytes apart, the pages' rows beside each other: offsets past
+    2^32 within a page, for few rows and for tiles."""
+    log(f"paged attention: slots 2^27 bytes apart, new {new}")
+    hkv, dim, page = 2, 64, 64
+    c = Cache([60, 50], new, 4, hkv, dim, page, "bf16", seed=11)
+    k, v = c.tensors()
+    slot = 1 << 26
+    wide = []
+    for x in (k, v):
+        base = torch.empty((page - 1) * slot + c.pages * hkv * dim, dtype=x.dtype, device=DEV)
+        y = base.as_strided(x.shape, (hkv * dim, slot, dim, 1))
+        y.copy_(x)
+        wide.append(y)
+    assert (page - 1) * slot * 2 > 1 << 32
+    got = pair.paged_attention(c.q, wide[0], wide[1], torch.from_numpy(c.table).to(DEV),
+                               torch.from_numpy(c.off).to(DEV),
+                               torch.from_numpy(c.lens.astype(np.int32)).to(DEV), max(new), 60,
+                               scale=c.scale, want_lse=True)
+    torch.cuda.synchronize()
+    c.check(got)
+
+
+@pytest.mark.parametrize("n,case", [(2100, "few"), (300, "few"), (300, "chunks"), (70, "chunks"),
+                                    (2100, "chunks")])
+def test_many_requests(n, case):
+    """Batches past what a workgroup scans or orders itself; requests of chunks
+    beside ones of a token, without tokens and without keys."""
+    log(f"paged attention: {n} requests, {case}")
+    rng = np.random.default_rng(n)
+    new = np.ones(n, dtype=np.int64)
+    lens = rng.integers(1, 60, n)
+    lens[5], lens[n - 2] = 1400, 1290
+    if case == "chunks":
+        new = rng.integers(0, 3, n)
+        new[[3, n // 2, n - 1]] = [40, 70, 33]
+    new[7], lens[9] = 0, 0
+    lens = np.maximum(lens, np.where(np.arange(n) == 9, 0, new))
+    c = Cache(lens, new, 4, 2, 64, 16, "bf16", seed=n)
+    c.check(c.call(), only=[0, 3, 5, 7, 8, 9, 63, 64, 65, n // 2, n - 2, n - 1])
+
+
+@pytest.mark.parametrize("new", [[1, 1, 0, 1], [70, 1, 0, 40]])
+def test_rows_past_the_last_request(new):
+    """More rows of q than the requests have: the others are not touched."""
+    log(f"paged attention: rows past the last request, new {new}")
+    c = Cache([90, 33, 20, 1100], new, 4, 2, 64, 16, "f16", seed=12)
+    t = int(c.off[-1])
+    q = torch.randn((t + 9, 4, 64), device=DEV).to(c.dtype)
+    q[:t] = c.q
+    out = torch.full_like(q, 3.0)
+    k, v = c.tensors()
+    r = pair.paged_attention(q, k, v, torch.from_numpy(c.table).to(DEV),
+                             torch.from_numpy(c.off).to(DEV),
+                             torch.from_numpy(c.lens.astype(np.int32)).to(DEV), max(new), 1100,
+                             scale=c.scale, want_lse=True, out=out)
+    torch.cuda.synchronize()
+    assert int(r["status"].item()) == 0 and bool((out[t:] == 3.0).all())
+    c.check({**r, "out": out[:t], "lse": r["lse"][:t]})
+
+
 def test_bounds_are_only_bounds():
     """max_q and max_len larger than the lengths: within the bar, and a call
     repeated gives the same bits."""
