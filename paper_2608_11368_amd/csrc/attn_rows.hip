@@ -573,7 +573,7 @@ Plan plan_rows(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim, int32_
   const int64_t rows = (int64_t)max_q * (q_heads / kv_heads);
   p.rows = (int)(rows < kRowsMost ? rows : kRowsMost);
   p.tiles = p.rows <= 16 ? 1 : 2;
-  // Cut into equal runs unless the longest head is eight steps, which take less
+  // Cut into equal runs (units are counted in 31 bits) unless the longest head is eight steps, which take less
   // than the second launch would (4 requests of 700 keys: 10.9 us uncut, 16.5 us
   // cut; of 1000: 14.3 and 16.4; of 2000: 24.7 and 16.7), or the requests are so
   // many that they fill the card by themselves.
@@ -582,7 +582,7 @@ Plan plan_rows(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim, int32_
   if (runs > most) runs = most;
   if (runs > kMostRuns) runs = kMostRuns;
   if (runs < 1) runs = 1;
-  p.runs = n > kMostScanned || max_len <= 8 * kUnit ? 0 : (int32_t)runs;
+  p.runs = n > kMostScanned || max_len <= 8 * kUnit || most > 0x7fffffff ? 0 : (int32_t)runs;
   const size_t parts = 2 * (size_t)p.runs * kv_heads * 16 * p.tiles;
   p.starts = ((size_t)(n + 1) * 4 + 255) / 256 * 256;
   p.ml = (parts * 8 + 255) / 256 * 256;

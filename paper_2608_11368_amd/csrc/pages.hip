@@ -344,25 +344,42 @@ __global__ __launch_bounds__(kThreads) void plan_fused_kernel(PlanArgs a, int64_
 
 // More requests: a first launch writes the scans' ends to the workspace.  Each
 // of its workgroups owns kScan requests and sums the ones before them itself,
-// which at 9 bytes a request is less than a second pass would wait for.
+// or, beyond kSelfSummed requests, takes the sums that a launch before it left.
+// (A call of 4,096 requests 23.4 us by itself, 26.2 us with that launch; 16,384:
+// 27.9 and 27.6; 65,536: 41.9 and 30.0; 2^20: 559 and 60.)
 constexpr int kScan = 1024;
+constexpr int64_t kSelfSummed = 1 << 14;
 
-__global__ __launch_bounds__(kScan) void plan_scan_kernel(PlanArgs a, uint32_t* ends) {
+__global__ __launch_bounds__(kScan) void plan_sums_kernel(PlanArgs a, Counts* sums) {
+  const int64_t r = (int64_t)blockIdx.x * kScan + threadIdx.x;
+  int32_t other = 0, len;
+  Counts mine = {0u, 0u, 0u}, total;
+  if (r < a.n) mine = request(a, r, &len, &other);
+  group_scan<kScan>(mine, &total);
+  if (threadIdx.x == 0) sums[blockIdx.x] = total;
+}
+
+__global__ __launch_bounds__(kScan) void plan_scan_kernel(PlanArgs a, uint32_t* ends,
+                                                          const Counts* sums) {
   const int64_t r0 = (int64_t)blockIdx.x * kScan;
   int32_t bad = 0, other = 0, len;
   Counts sum = {0u, 0u, 0u};
-  // r0 is a multiple of kScan: four requests of a lane at a time
-  for (int64_t r = 4 * threadIdx.x; r < r0; r += 4 * kScan) {
-    typedef u32x4_t u32x4_a4 __attribute__((aligned(4)));
-    typedef uint32_t u32_a1 __attribute__((aligned(1)));
-    const u32x4_t cached = *reinterpret_cast<const u32x4_a4*>(a.cached + r);
-    const u32x4_t fresh = *reinterpret_cast<const u32x4_a4*>(a.fresh + r);
-    const uint32_t live =
-        a.mask != nullptr ? *reinterpret_cast<const u32_a1*>(a.mask + r) : 0x01010101u;
+  if (sums != nullptr) {
+    for (int64_t b = threadIdx.x; b < blockIdx.x; b += kScan) sum = sum + sums[b];
+  } else {
+    // r0 is a multiple of kScan: four requests of a lane at a time
+    for (int64_t r = 4 * threadIdx.x; r < r0; r += 4 * kScan) {
+      typedef u32x4_t u32x4_a4 __attribute__((aligned(4)));
+      typedef uint32_t u32_a1 __attribute__((aligned(1)));
+      const u32x4_t cached = *reinterpret_cast<const u32x4_a4*>(a.cached + r);
+      const u32x4_t fresh = *reinterpret_cast<const u32x4_a4*>(a.fresh + r);
+      const uint32_t live =
+          a.mask != nullptr ? *reinterpret_cast<const u32_a1*>(a.mask + r) : 0x01010101u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      sum = sum + counts_of(a, (int32_t)cached[i], (int32_t)fresh[i],
-                            ((live >> (8 * i)) & 0xffu) != 0, &len, &other);
+      for (int i = 0; i < 4; ++i)
+        sum = sum + counts_of(a, (int32_t)cached[i], (int32_t)fresh[i],
+                              ((live >> (8 * i)) & 0xffu) != 0, &len, &other);
+    }
   }
   Counts before, total;
   group_scan<kScan>(sum, &before);
@@ -449,7 +466,8 @@ __global__ __launch_bounds__(kThreads) void cache_store_kernel(StoreArgs a, int 
 }  // namespace
 
 size_t page_plan_workspace_bytes(int64_t n) {
-  return ((size_t)n * 3 * sizeof(uint32_t) + 255) / 256 * 256;
+  return (((size_t)n * 3 * sizeof(uint32_t) + (size_t)(n + kScan - 1) / kScan * sizeof(Counts)) +
+          255) / 256 * 256;
 }
 
 int launch_page_plan(int64_t n, const int32_t* cached, const int32_t* fresh, const uint8_t* mask,
@@ -469,8 +487,14 @@ int launch_page_plan(int64_t n, const int32_t* cached, const int32_t* fresh, con
     hipLaunchKernelGGL(plan_fused_kernel, dim3(grid), dim3(kThreads), 0, stream, a, token_tiles);
   } else {
     uint32_t* ends = static_cast<uint32_t*>(workspace);
-    hipLaunchKernelGGL(plan_scan_kernel, dim3((unsigned)((n + kScan - 1) / kScan)), dim3(kScan), 0,
-                       stream, a, ends);
+    const dim3 groups((unsigned)((n + kScan - 1) / kScan));
+    Counts* sums = n > kSelfSummed ? reinterpret_cast<Counts*>(ends + 3 * n) : nullptr;
+    if (sums != nullptr) {
+      hipLaunchKernelGGL(plan_sums_kernel, groups, dim3(kScan), 0, stream, a, sums);
+      if (hipGetLastError() != hipSuccess) return PAIR_EHIP;
+    }
+    hipLaunchKernelGGL(plan_scan_kernel, groups, dim3(kScan), 0, stream, a, ends,
+                       (const Counts*)sums);
     if (hipGetLastError() != hipSuccess) return PAIR_EHIP;
     hipLaunchKernelGGL(plan_write_kernel, dim3(grid), dim3(kThreads), 0, stream, a, ends,
                        token_tiles);

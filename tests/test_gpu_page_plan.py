@@ -94,6 +94,16 @@ def test_plan_against_a_walk(n, page, most_cached, most_fresh, masked):
         same(got, walk(cached, fresh, mask, table, free, page, room, pool))
 
 
+@pytest.mark.parametrize("n", [16_384, 16_385, 70_001])
+def test_plan_of_many_against_a_walk(n):
+    log(f"page plan: n={n}")
+    cached, fresh, mask, table, free, pool = make(n, 8, 20, 2, True, n)
+    room = int(fresh.sum()) + 7
+    got = call(cached, fresh, mask, table, free, pool, 8, room)
+    assert int(got["status"].item()) == 0
+    same(got, walk(cached, fresh, mask, table, free, 8, room, pool))
+
+
 @pytest.mark.parametrize("n", [5, 2500])
 def test_all_released_and_none(n):
     log(f"page plan: all released, none released, n={n}")
