@@ -18,8 +18,9 @@
 // tensor table travels in the kernel's arguments, so nothing is copied to the
 // device or kept between calls.
 //
-// Measured: norm of 600M bf16 or 455M fp32 elements 189 and 269 us (6.3 and 6.8
-// TB/s); clipping 600M bf16 into fp32 900 us, into bf16 663 us, 455M fp32 998 us
+// Measured: 301 tensors of 40M bf16 elements into fp32, two launches for the norm
+// (11 us each) and three for the product, 77 us in all; norm of 600M bf16 or
+// 455M fp32 elements 187 and 269 us (6.4 and 6.8 TB/s); clipping 600M bf16 into fp32 900 us, into bf16 663 us, 455M fp32 998 us
 // (5.3 to 5.5 TB/s of two reads and a write).
 #include <math.h>
 
@@ -34,11 +35,13 @@ constexpr int kLaneBytes = 64;                      // of a lane per chunk: what
 constexpr int kChunkBytes = kThreads * kLaneBytes;
 constexpr int kNormBatch = 160;
 constexpr int kScaleBatch = 120;
-constexpr int kMaxGroups = 2048;                    // workgroups of a launch
+constexpr int kNormGroups = 1024;                   // most workgroups of a launch
+constexpr int kScaleGroups = 2048;
 constexpr int64_t kCached = (int64_t)192 << 20;     // of the 256 MiB memory-side cache
-// Partials that every workgroup of the second pass sums itself; more of them
-// (beyond about 2000 tensors) are summed once by a launch in between.
-constexpr int64_t kMaxOwnSum = 16384;
+// Partials that every workgroup of the second pass sums itself (2048 of them:
+// 1.1 us a launch more than reading one sum); more of them (beyond about 600
+// tensors, so six such launches) are summed once by a launch in between (2 us).
+constexpr int64_t kMaxOwnSum = 4096;
 
 template <int N>
 struct TensorTable {
@@ -239,7 +242,12 @@ __global__ __launch_bounds__(kThreads) void clip_norm_kernel(TensorTable<kNormBa
 
 __device__ __forceinline__ double sum_partials(const double* partial, int64_t n) {
   double s = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += kThreads) s += partial[i];
+  for (int64_t i0 = threadIdx.x; i0 < n; i0 += 4 * kThreads) {   // four loads in flight
+    double v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = i0 + e * kThreads < n ? partial[i0 + e * kThreads] : 0.0;
+    s += (v[0] + v[1]) + (v[2] + v[3]);
+  }
   return group_sum(s);
 }
 
@@ -327,8 +335,8 @@ uint32_t chunks_of(int64_t size, int32_t type) {
   return (uint32_t)((size * (type == PAIR_F32 ? 4 : 2) + kChunkBytes - 1) / kChunkBytes);
 }
 
-unsigned groups_of(uint32_t chunks) {
-  return chunks < (uint32_t)kMaxGroups ? (chunks ? chunks : 1u) : (unsigned)kMaxGroups;
+unsigned groups_of(uint32_t chunks, int most) {
+  return chunks < (uint32_t)most ? (chunks ? chunks : 1u) : (unsigned)most;
 }
 
 // Fills a table from tensor i0 on, skipping empty ones; returns the next tensor.
@@ -361,7 +369,7 @@ int64_t fill(TensorTable<N>* t, OutTable* o, int64_t i0, int64_t count, const vo
 // One partial per workgroup of the first pass, and one sum.
 size_t clip_workspace_bytes(int64_t count) {
   const int64_t batches = count / kNormBatch + 1;
-  return ((size_t)(batches * kMaxGroups + 1) * sizeof(double) + 255) / 256 * 256;
+  return ((size_t)(batches * kNormGroups + 1) * sizeof(double) + 255) / 256 * 256;
 }
 
 int launch_clip(int64_t count, const void* const* grads, void* const* outs, const int64_t* sizes,
@@ -377,7 +385,7 @@ int launch_clip(int64_t count, const void* const* grads, void* const* outs, cons
     TensorTable<kNormBatch> t;
     i = fill(&t, nullptr, i, count, grads, nullptr, sizes, dtypes, nullptr);
     if (t.count == 0) break;
-    const unsigned g = groups_of(t.first[t.count]);
+    const unsigned g = groups_of(t.first[t.count], kNormGroups);
     if (stream_past)
       hipLaunchKernelGGL(clip_norm_kernel<true>, dim3(g), dim3(kThreads), 0, stream, t, partial + n);
     else
@@ -398,7 +406,7 @@ int launch_clip(int64_t count, const void* const* grads, void* const* outs, cons
     OutTable o;
     i = fill(&t, &o, norm_only ? count : i, count, grads, outs, sizes, dtypes, out_dtypes);
     if (t.count == 0 && !report) break;
-    const unsigned g = groups_of(t.first[t.count]);
+    const unsigned g = groups_of(t.first[t.count], kScaleGroups);
     if (stream_past)
       hipLaunchKernelGGL(clip_scale_kernel<true>, dim3(g), dim3(kThreads), 0, stream, t, o, partial,
                          n, max_norm, outs == nullptr ? 1 : 0, report, norm, coef, d_status);
