@@ -20,6 +20,19 @@
 //
 // When the tiles are too few for the card, each tile's keys are split and a
 // second launch joins the parts.
+//
+// Measured, of 2 * 2 * rows * keys * width operations that the masks leave: 2048
+// new tokens each of 8 requests over 8192 keys, 32 heads of 128: 1030 TFLOP/s;
+// chunks of uneven length (16 requests, 594 GFLOP) 620 us, 960; prompts of
+// uneven length at width 64 (104 GFLOP) 150 us, 700.  A product of two 8192^2
+// matrices by the library runs at 1250.  At width 128 the products and their LDS
+// reads are what is left: a wave's 32 rows use each 1 KiB fragment once, and
+// four SIMDs taking one every 32 cycles ask for all of LDS's 128 bytes a cycle;
+// left alone (no weights, no loads) they take 80% of the time.  At width 64 the
+// exponentials (one per 256 operations instead of 512) take the larger part.
+// Eight waves in two groups that alternate between products and weights, one
+// workgroup a compute unit, reached 1050 to 1100 on the longest chunks and lost
+// 20 to 40% on 16 x 64 tokens and on single prompts, for which four stay.
 #include <type_traits>
 
 #include "attn.hpp"
@@ -97,6 +110,16 @@ __device__ __forceinline__ int wave_sum_i(int v) {
          __builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48);
 }
 
+__device__ __forceinline__ int wave_scan_i(int v) {   // inclusive
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // row_shr
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // row_bcast
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+
 // Tile `at` of the call: the request, and the tile's number in it; false past the
 // last.  Every wave holds the requests in its lanes, SETS each.  The order is by
 // falling work, so that the last workgroups to start are the shortest, but only
@@ -124,38 +147,38 @@ __device__ __forceinline__ bool find_ordered(const TileArgs& s, int64_t at, Requ
     }
   }
   if (bad && blockIdx.x == 0 && threadIdx.x < kWave) raise_status(s.a.d_status, bad);
-  auto longer = [&](int i, int w) {         // tiles of set i's request of more than w steps
-    if (w < 0) return tiles[i];
-    int64_t token = (int64_t)w * kKeys - (own[i].len - own[i].tokens);   // first that sees more
-    if (token < 0) token = 0;
-    if (token >= own[i].tokens) return 0;
-    return tiles[i] - (int)token * (int)s.group.d / kRows;
-  };
-  auto total = [&](int w) {
-    int v = 0;
-#pragma unroll
-    for (int i = 0; i < SETS; ++i) v += tiles[i] > 0 ? longer(i, w) : 0;
-    return wave_sum_i(v);
-  };
-  if (at >= total(-1)) return false;
   const int steps = (s.a.max_len + kKeys - 1) / kKeys;
   const int each = (steps + kClasses - 1) / kClasses;
-  int hi = kClasses * each, lo = hi - each;     // until total(lo) > at >= total(hi)
-  while (lo > 0 && total(lo) <= at) {
-    hi = lo;
-    lo -= each;
+  // tiles of set i's request of class c or a longer one (class 0: of any length)
+  auto from_class = [&](int i, int c) {
+    int token = c * each * kKeys - (own[i].len - own[i].tokens);   // first that sees more
+    if (token < 0 || c == 0) token = 0;
+    const int before = (token < own[i].tokens ? token : own[i].tokens) * (int)s.group.d / kRows;
+    return token < own[i].tokens ? tiles[i] - before : 0;
+  };
+  int totals[kClasses + 1];                 // side by side: each is a chain of lane exchanges
+#pragma unroll
+  for (int c = 0; c < kClasses; ++c) {
+    int v = 0;
+#pragma unroll
+    for (int i = 0; i < SETS; ++i) v += tiles[i] > 0 ? from_class(i, c) : 0;
+    totals[c] = wave_sum_i(v);
   }
-  if (lo <= 0) lo = -1;                         // tiles that see nothing, too
-  int left = (int)(at - total(hi));
+  totals[kClasses] = 0;
+  if (at >= totals[0]) return false;
+  int cls = 0, ahead = totals[1];           // tiles of longer classes
+#pragma unroll
+  for (int c = 1; c < kClasses; ++c)
+    if (at < totals[c]) {
+      cls = c;
+      ahead = totals[c + 1];
+    }
+  int left = (int)at - ahead;
 #pragma unroll
   for (int i = 0; i < SETS; ++i) {
-    const int mine = tiles[i] > 0 ? longer(i, lo) - longer(i, hi) : 0;
-    int scan = mine;
-#pragma unroll
-    for (int by = 1; by < kWave; by <<= 1) {
-      const int v = __shfl_up(scan, by, kWave);
-      if (lane >= by) scan += v;
-    }
+    const int longer = tiles[i] > 0 && cls + 1 < kClasses ? from_class(i, cls + 1) : 0;
+    const int mine = tiles[i] > 0 ? from_class(i, cls) - longer : 0;
+    const int scan = wave_scan_i(mine);
     const int all = __builtin_amdgcn_readlane(scan, kWave - 1);
     if (left >= all) {
       left -= all;
@@ -163,8 +186,7 @@ __device__ __forceinline__ bool find_ordered(const TileArgs& s, int64_t at, Requ
     }
     const int x = uniform(__popcll(__ballot(scan <= left)));
     *request = i * kWave + x;
-    *tile = __builtin_amdgcn_readlane(tiles[i] > 0 ? tiles[i] - longer(i, hi) - 1 + scan - mine : 0,
-                                      x) - left;
+    *tile = __builtin_amdgcn_readlane(tiles[i] - longer - 1 + scan - mine, x) - left;
     q->tokens = __builtin_amdgcn_readlane(own[i].tokens, x);
     q->len = __builtin_amdgcn_readlane(own[i].len, x);
     q->q0 = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane(
@@ -268,6 +290,7 @@ __global__ __launch_bounds__(kThreads, DIM == 64 ? 3 : 2) void attention_tiles_k
   int64_t r;
   int tile;
   Request q;
+  __builtin_amdgcn_s_setprio(2);            // until it takes its share of the work
   const int64_t place_in_order = blockIdx.x / (heads * s.splits);
   if (s.a.n <= kWave) {
     if (!find_ordered<1>(s, place_in_order, &q, &r, &tile)) return;
@@ -511,6 +534,7 @@ __global__ __launch_bounds__(kThreads, DIM == 64 ? 3 : 2) void attention_tiles_k
     }
     fetch(k0);
   }
+  __builtin_amdgcn_s_setprio(0);
   for (int kb = k0; kb < k1; kb += 2 * kKeys) {
     step(kb, std::integral_constant<int, 0>());
     if (kb + kKeys < k1) step(kb + kKeys, std::integral_constant<int, 1>());
