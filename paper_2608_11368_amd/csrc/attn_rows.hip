@@ -24,7 +24,7 @@
 // Bound by the cache's bytes.  Measured: one token for each of 256 requests of
 // 4000 keys on average, 8 heads of width 128, 4.1 GB: 649 us and 8 us for the
 // joins, 6.3 TB/s (a read of the same bytes with no work on them runs at 7.0);
-// four drafted tokens of 4 requests of 32,000 keys, 1.07 GB: 176 us, 6.1 TB/s.
+// five drafted tokens of 2 requests of 131,000 keys, 1.07 GB: 176 us, 6.1 TB/s.
 // What was measured on the first of these and decides the layout: K in 64-byte
 // pieces of a row straight into the products' operands 5.7 TB/s at any
 // occupancy or order, whole rows past the caches and through LDS 6.3; the heads

@@ -21,18 +21,20 @@
 // When the tiles are too few for the card, each tile's keys are split and a
 // second launch joins the parts.
 //
-// Measured, of 2 * 2 * rows * keys * width operations that the masks leave: 2048
-// new tokens each of 8 requests over 8192 keys, 32 heads of 128: 1030 TFLOP/s;
-// chunks of uneven length (16 requests, 594 GFLOP) 620 us, 960; prompts of
-// uneven length at width 64 (104 GFLOP) 150 us, 700.  A product of two 8192^2
-// matrices by the library runs at 1250.  At width 128 the products and their LDS
-// reads are what is left: a wave's 32 rows use each 1 KiB fragment once, and
-// four SIMDs taking one every 32 cycles ask for all of LDS's 128 bytes a cycle;
-// left alone (no weights, no loads) they take 80% of the time.  At width 64 the
-// exponentials (one per 256 operations instead of 512) take the larger part.
-// Eight waves in two groups that alternate between products and weights, one
-// workgroup a compute unit, reached 1050 to 1100 on the longest chunks and lost
-// 20 to 40% on 16 x 64 tokens and on single prompts, for which four stay.
+// Measured, in 4 * rows * keys * width operations that the masks leave: at width
+// 128 one prompt of 16,384 tokens 1030 TFLOP/s, 8 chunks of 2048 over 8192 keys
+// 1000, three uneven ones over 4000 to 8000 keys 945, 8 prompts of 4096 930, 16
+// chunks of 64 over 4000 keys 700; at width 64 the first two 810 and 795, 8
+// prompts of 301 to 4096 tokens 695.  A product of two 8192^2 matrices by the
+// library runs at 1250.  At width 128 the products and their LDS reads are what
+// is left: a wave's 32 rows use each 1 KiB fragment once, and four SIMDs taking
+// one every 32 cycles ask for all of LDS's 128 bytes a cycle; left alone (no
+// weights, no loads) they take 80% of the time, at clocks that the power limit
+// sets.  At width 64 the exponentials (one per 256 operations instead of 512)
+// take the larger part.  Eight waves in two groups that alternate between
+// products and weights, one workgroup a compute unit, reached 1050 to 1100 on the
+// longest chunks and lost 20 to 40% on 16 x 64 tokens and on single prompts, for
+// which four stay.
 #include <type_traits>
 
 #include "attn.hpp"
@@ -127,8 +129,9 @@ __device__ __forceinline__ int wave_scan_i(int v) {   // inclusive
 // that the workgroups that run at one time share a request's keys in their
 // caches.  (8 prompts of 300 to 4096 tokens at width 64: 157 us in the order of
 // the requests, 147 us strictly by work, 151 us so.  8 chunks of 2048 tokens over
-// 8192 keys, 16 heads of width 128: 1441 us strictly by work, 1300 us so.)  The
-// tiles of more than w steps are counted request by request in closed form.
+// 8192 keys, 16 heads of width 128: 1441 us strictly by work, 1300 us so; 4 or 16
+// classes differ from 8 by 1 to 3% either way.)  A request's tiles of a class are
+// counted in closed form.  A workgroup takes 2 us for this beside others' work.
 template <int SETS>
 __device__ __forceinline__ bool find_ordered(const TileArgs& s, int64_t at, Request* q,
                                              int64_t* request, int* tile) {

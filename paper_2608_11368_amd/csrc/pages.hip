@@ -15,9 +15,8 @@ constexpr int kThreads = 256;
 // by bisection of the scans' ends.  Bound by launches and by loads that wait for
 // each other, not by bytes: 64 requests 4.4 us; 16,896 requests with half of
 // them released, 1.1M tokens, 4 + 6 + 15 us (of 16 MB: 3 us at the rate of a
-// copy).  Sums saturate at 2^31 - 1, beyond every
-// capacity; saturating addition of counts is associative, so the scans may be
-// split anywhere.
+// copy).  Sums saturate at 2^31 - 1, beyond every capacity; saturating addition
+// of counts is associative, so the scans may be split anywhere.
 struct PlanArgs {
   int64_t n;
   const int32_t* cached;
