@@ -10,15 +10,14 @@ import of the library fails loudly (build it with
 ``python -m paper_2608_11368_amd.build``).
 
 The lower-case helpers (``design_inclusion``, ``edge_coeffs``,
-``weighted_grad``, ``audit``, ``page_plan``, ``paged_attention``, ...) allocate the outputs with torch and call the
-``pair_*`` functions.  Given an explicit ``stream``, a helper makes it torch's
+``weighted_grad``, ``audit``, ``page_plan``, ``paged_attention``, ...) allocate
+the outputs with torch and call the ``pair_*`` functions.  Given an explicit ``stream``, a helper makes it torch's
 current stream while it allocates, clears and launches, so the zero-fills are
 ordered before the kernels and the caching allocator hands a temporary
 workspace to later work only behind them.
 """
 from __future__ import annotations
 
-import array
 import ctypes
 import functools
 import inspect
@@ -501,40 +500,34 @@ def pair_clip_grads_workspace_bytes(count) -> int:
     return int(lib().pair_clip_grads_workspace_bytes(count))
 
 
-def _grad_table(tensors, name):
-    """Host arrays of the tensors' addresses, sizes and types for one call; a
-    model has hundreds, so each property is gathered in one go."""
-    T = torch.Tensor
-    if not all(issubclass(t, T) for t in set(map(type, tensors))):
-        raise ValueError(f"{name} must be tensors")
-    devices = set(map(T.get_device, tensors))
-    if len(devices) > 1 or -1 in devices or not all(map(T.is_contiguous, tensors)):
-        raise ValueError(f"{name} must be contiguous CUDA (HIP) tensors of one device")
-    dtypes = list(map(T.dtype.__get__, tensors))
-    kinds = set(dtypes)
-    for t in kinds - _DTYPE_CODE.keys():
-        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t}")
-    code = (array.array("i", [_DTYPE_CODE[dtypes[0]]]) * len(dtypes) if len(kinds) == 1
-            else array.array("i", map(_DTYPE_CODE.__getitem__, dtypes)))
-    return (array.array("Q", map(T.data_ptr, tensors)), array.array("q", map(T.numel, tensors)), code)
+_grad_table = None
 
 
-def _address(a):
-    return None if a is None else a.buffer_info()[0]
+def _load_grad_table():
+    """The native reader of tensor lists (raises if it has not been built)."""
+    global _grad_table
+    if _grad_table is None:
+        try:
+            from ._tensors import grad_table
+        except ImportError as e:
+            raise ImportError(f"{_HERE}/_tensors.so cannot be loaded ({e}): build it with "
+                              "`python -m paper_2608_11368_amd.build`") from e
+        _grad_table = grad_table
+    return _grad_table
 
 
 def pair_clip_grads(grads, max_norm, norm, coef, workspace, out=None, d_status=None, stream=None):
     """`out`: None clips in place, else a list of tensors of the gradients'
     sizes, each of its gradient's type or float32."""
-    ptrs, sizes, codes = _grad_table(grads, "grads")
+    table = _grad_table or _load_grad_table()
+    ptrs, sizes, codes = table(grads if type(grads) is list else list(grads), "grads")
     optrs = ocodes = None
     if out is not None:
-        optrs, osizes, ocodes = _grad_table(out, "out")
+        optrs, osizes, ocodes = table(out if type(out) is list else list(out), "out")
         if osizes != sizes:
             raise ValueError("out must hold a tensor of each gradient's size")
     _rc(lib().pair_clip_grads(
-        len(sizes), _address(ptrs), _address(optrs), _address(sizes), _address(codes),
-        _address(ocodes), float(max_norm),
+        len(sizes) // 8, ptrs, optrs, sizes, codes, ocodes, float(max_norm),
         _dev(norm, "norm", torch.float32, 1), _dev(coef, "coef", torch.float32, 1),
         _dev(workspace, "workspace", torch.uint8), workspace.numel(),
         _dev(d_status, "d_status", torch.int32, 1, True), _stream(stream)), "pair_clip_grads")
