@@ -177,6 +177,22 @@ def _dev(t, name, dtype, numel=None, allow_none=False):
     return t.data_ptr()   # the declared argument type makes the pointer
 
 
+_reader = None
+
+
+def _native():
+    """The native reader of tensor arguments (raises if it has not been built)."""
+    global _reader
+    if _reader is None:
+        try:
+            from . import _tensors
+        except ImportError as e:
+            raise ImportError(f"{_HERE}/_tensors.so cannot be loaded ({e}): build it with "
+                              "`python -m paper_2608_11368_amd.build`") from e
+        _reader = _tensors
+    return _reader
+
+
 # The current stream's handle without a Stream object, where torch has the call
 # (0.2 us against 2.8 us, of a call that takes 15 to 30 in all).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -408,19 +424,19 @@ def pair_page_plan(n, cached, fresh, mask, page, table, free_pages, free_count, 
                    d_status=None, stream=None):
     if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[0] < n:
         raise ValueError("table must be a 2-D tensor with a row for each request")
-    capacity = free_pages.numel()
+    at, capacity = _native().address, free_pages.numel()
     _rc(lib().pair_page_plan(
-        n, _dev(cached, "cached", torch.int32, n), _dev(fresh, "fresh", torch.int32, n),
-        _dev(mask, "mask", torch.uint8, n, True), int(page), _dev(table, "table", torch.int32),
-        table.shape[1], capacity, _dev(free_pages, "free_pages", torch.int32),
-        _dev(free_count, "free_count", torch.int64, 1), int(max_tokens),
-        _dev(q_offsets, "q_offsets", torch.int64, n + 1), _dev(lens, "lens", torch.int32, n),
-        _dev(slots, "slots", torch.int64, max_tokens),
-        _dev(positions, "positions", torch.int32, max_tokens, True),
-        _dev(free_out, "free_out", torch.int32, capacity),
-        _dev(free_count_out, "free_count_out", torch.int64, 1),
-        _dev(workspace, "workspace", torch.uint8), workspace.numel(),
-        _dev(d_status, "d_status", torch.int32, 1, True), _stream(stream)), "pair_page_plan")
+        n, at(cached, "cached", torch.int32, n), at(fresh, "fresh", torch.int32, n),
+        at(mask, "mask", torch.uint8, n, True), int(page), at(table, "table", torch.int32),
+        table.shape[1], capacity, at(free_pages, "free_pages", torch.int32),
+        at(free_count, "free_count", torch.int64, 1), int(max_tokens),
+        at(q_offsets, "q_offsets", torch.int64, n + 1), at(lens, "lens", torch.int32, n),
+        at(slots, "slots", torch.int64, max_tokens),
+        at(positions, "positions", torch.int32, max_tokens, True),
+        at(free_out, "free_out", torch.int32, capacity),
+        at(free_count_out, "free_count_out", torch.int64, 1),
+        at(workspace, "workspace", torch.uint8), workspace.numel(),
+        at(d_status, "d_status", torch.int32, 1, True), _stream(stream)), "pair_page_plan")
 
 
 def _cache_arg(k_cache, v_cache):
@@ -463,10 +479,10 @@ def pair_cache_store(k, v, slots, k_cache, v_cache, d_status=None, stream=None):
     vp, vtok, vhead, vshape = _rows_arg(v, "v", dtype, heads, dim)
     if vtok != tok or vhead != head or vshape != shape:
         raise ValueError("k and v must have the same shape and strides")
-    tokens = shape[0]
+    at, tokens = _native().address, shape[0]
     _rc(lib().pair_cache_store(
         tokens, heads, dim, _DTYPE_CODE[dtype], kp, vp, tok, head, kc, vc, st[0], st[1], st[2], page, pages,
-        _dev(slots, "slots", torch.int64, tokens), _dev(d_status, "d_status", torch.int32, 1, True),
+        at(slots, "slots", torch.int64, tokens), at(d_status, "d_status", torch.int32, 1, True),
         _stream(stream)), "pair_cache_store")
 
 
@@ -485,14 +501,15 @@ def pair_paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max
         raise ValueError("table must be a 2-D tensor with a row for each request")
     if oshape[0] < tokens:
         raise ValueError(f"out holds {oshape[0]} tokens, needs {tokens}")
+    at = _native().address
     _rc(lib().pair_paged_attention(
         n, tokens, heads, kv_heads, dim, _DTYPE_CODE[dtype], qp, qt, qh, kc, vc, st[0], st[1], st[2], page,
-        pages, _dev(table, "table", torch.int32), table.shape[1],
-        _dev(q_offsets, "q_offsets", torch.int64, n + 1), _dev(lens, "lens", torch.int32, n),
+        pages, at(table, "table", torch.int32), table.shape[1],
+        at(q_offsets, "q_offsets", torch.int64, n + 1), at(lens, "lens", torch.int32, n),
         int(max_q), int(max_len), float(scale), op, ot, oh,
-        _dev(lse, "lse", torch.float32, tokens * heads, True),
-        _dev(workspace, "workspace", torch.uint8), workspace.numel(),
-        _dev(d_status, "d_status", torch.int32, 1, True), _stream(stream)),
+        at(lse, "lse", torch.float32, tokens * heads, True),
+        at(workspace, "workspace", torch.uint8), workspace.numel(),
+        at(d_status, "d_status", torch.int32, 1, True), _stream(stream)),
         "pair_paged_attention")
 
 
@@ -500,26 +517,10 @@ def pair_clip_grads_workspace_bytes(count) -> int:
     return int(lib().pair_clip_grads_workspace_bytes(count))
 
 
-_grad_table = None
-
-
-def _load_grad_table():
-    """The native reader of tensor lists (raises if it has not been built)."""
-    global _grad_table
-    if _grad_table is None:
-        try:
-            from ._tensors import grad_table
-        except ImportError as e:
-            raise ImportError(f"{_HERE}/_tensors.so cannot be loaded ({e}): build it with "
-                              "`python -m paper_2608_11368_amd.build`") from e
-        _grad_table = grad_table
-    return _grad_table
-
-
 def pair_clip_grads(grads, max_norm, norm, coef, workspace, out=None, d_status=None, stream=None):
     """`out`: None clips in place, else a list of tensors of the gradients'
     sizes, each of its gradient's type or float32."""
-    table = _grad_table or _load_grad_table()
+    at, table = _native().address, _native().grad_table
     ptrs, sizes, codes = table(grads if type(grads) is list else list(grads), "grads")
     optrs = ocodes = None
     if out is not None:
@@ -528,9 +529,9 @@ def pair_clip_grads(grads, max_norm, norm, coef, workspace, out=None, d_status=N
             raise ValueError("out must hold a tensor of each gradient's size")
     _rc(lib().pair_clip_grads(
         len(sizes) // 8, ptrs, optrs, sizes, codes, ocodes, float(max_norm),
-        _dev(norm, "norm", torch.float32, 1), _dev(coef, "coef", torch.float32, 1),
-        _dev(workspace, "workspace", torch.uint8), workspace.numel(),
-        _dev(d_status, "d_status", torch.int32, 1, True), _stream(stream)), "pair_clip_grads")
+        at(norm, "norm", torch.float32, 1), at(coef, "coef", torch.float32, 1),
+        at(workspace, "workspace", torch.uint8), workspace.numel(),
+        at(d_status, "d_status", torch.int32, 1, True), _stream(stream)), "pair_clip_grads")
 
 
 # ------------------------------------------------ allocating helpers -------
