@@ -24,8 +24,8 @@
 // Measured, in 4 * rows * keys * width operations that the masks leave: at width
 // 128 one prompt of 16,384 tokens 1030 TFLOP/s, 8 chunks of 2048 over 8192 keys
 // 1000, three uneven ones over 4000 to 8000 keys 945, 8 prompts of 4096 930, 16
-// chunks of 64 over 4000 keys 700; at width 64 the first two 810 and 795, 8
-// prompts of 301 to 4096 tokens 695.  A product of two 8192^2 matrices by the
+// chunks of 64 over 4000 keys 700; at width 64 the first two 850 and 850, 8
+// prompts of 301 to 4096 tokens 725.  A product of two 8192^2 matrices by the
 // library runs at 1250.  At width 128 the products and their LDS reads are what
 // is left: a wave's 32 rows use each 1 KiB fragment once, and four SIMDs taking
 // one every 32 cycles ask for all of LDS's 128 bytes a cycle; left alone (no
@@ -225,7 +225,8 @@ __device__ __forceinline__ bool find_counted(const TileArgs& s, int64_t back, Re
 // 16-byte piece `c` of LDS row `row` of a step's keys, and of its values.
 template <int DIM>
 __device__ __forceinline__ int key_piece(int row, int c) {
-  return row * (DIM * 2) + ((c ^ (row & (DIM / 8 - 1))) << 4);
+  const int f = DIM == 128 ? row & 15 : (row >> 1) & 7;   // two rows of 64 fill the banks
+  return row * (DIM * 2) + ((c ^ f) << 4);
 }
 template <int DIM>
 __device__ __forceinline__ int value_piece(int row, int c) {
