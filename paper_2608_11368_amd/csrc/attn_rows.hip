@@ -68,9 +68,17 @@ __device__ __forceinline__ int64_t runs_of(const RowArgs& s, int64_t units) {
   return units < s.runs ? units : s.runs;
 }
 
+// a / b for 0 <= a < 2^42 and 0 < b < 2^31 with a / b < 2^31: the exact quotient is
+// an integer or further than 1 / b from the next one, which the rounding of the
+// double's (2^-53 of it) does not reach.  A division of 64-bit integers takes
+// some hundred instructions.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return (int64_t)((double)a / (double)b);
+}
+
 // First unit of run w of `runs` on a line of `units`.
 __device__ __forceinline__ int64_t run_start(int64_t units, int64_t runs, int64_t w) {
-  return units * w / runs;
+  return quotient(units * w, runs);
 }
 
 // One wave's running softmax over its keys: row x = lane & 15 of each tile.
@@ -450,7 +458,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(RowArgs s) 
   __shared__ int32_t wave_sum_of[kWaves];
   const int64_t heads = s.a.kv_heads;
   const bool direct = s.runs == 0;          // one workgroup per request and head
-  const int64_t run = blockIdx.x / heads;   // or the request
+  const int64_t run = blockIdx.x / (uint32_t)s.a.kv_heads;   // or the request
   const int h = (int)(blockIdx.x - run * heads);
   const int n = (int)s.a.n;
   int64_t u = 0, end = 0;
@@ -500,14 +508,14 @@ __global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(RowArgs s) 
 template <bool BF16, int DIM>
 __global__ __launch_bounds__(kThreads) void join_rows_kernel(RowArgs s, int rows_slot) {
   const int64_t heads = s.a.kv_heads;
-  const int64_t r = blockIdx.x / heads;
+  const int64_t r = blockIdx.x / (uint32_t)s.a.kv_heads;
   const int kvh = (int)(blockIdx.x - r * heads);
   const int i = blockIdx.y;
   const int64_t u0 = s.starts[r], u1 = s.starts[r + 1];
   if (u0 == u1) return;
   const int64_t units = s.starts[s.a.n], runs = runs_of(s, units);
   // run of unit u: the last that starts at or before it
-  const int64_t w0 = ((u0 + 1) * runs - 1) / units, w1 = (u1 * runs - 1) / units;
+  const int64_t w0 = quotient((u0 + 1) * runs - 1, units), w1 = quotient(u1 * runs - 1, units);
   if (w0 == w1) return;
   Request q;
   int32_t bad = 0;
