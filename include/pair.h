@@ -4,16 +4,17 @@
  *
  * Conventions shared by every entry point
  * ---------------------------------------
- *  - Every array argument is a DEVICE pointer owned by the caller.  The library
- *    never allocates, frees or retains caller memory; scratch space is passed
- *    in explicitly (the audits' workspaces).
+ *  - Every array argument is a DEVICE pointer owned by the caller (but for the
+ *    tensor lists of pair_clip_grads, which say so).  The library never
+ *    allocates, frees or retains caller memory; scratch space is passed in
+ *    explicitly (the workspaces).
  *  - `stream` is a hipStream_t passed as void* (NULL = the default stream).
  *    All work is enqueued asynchronously on it; nothing blocks the host.
  *  - Host-detectable argument errors return a negative PAIR_E* code and
  *    enqueue nothing.  A failed launch returns PAIR_EHIP.
  *  - Data-dependent errors found on the device are OR-ed into *d_status
  *    (device int32, optional: NULL disables reporting) as PAIR_ST_* bits; the
- *    outputs of the affected prompt are then unspecified.  Callers that pass
+ *    outputs of the affected prompt or request are then unspecified.  Callers that pass
  *    d_status clear it before the call.
  *  - Prompts are packed ragged: `offsets` is int64 [B+1] with offsets[0] = 0,
  *    offsets[B] = nv; prompt b owns packed vertices (rollouts)
@@ -45,15 +46,16 @@ extern "C" {
 /* Return codes. */
 #define PAIR_OK 0
 #define PAIR_EINVAL (-1)     /* null pointer or malformed size                 */
-#define PAIR_EDTYPE (-2)     /* unknown score dtype                             */
+#define PAIR_EDTYPE (-2)     /* a dtype that the call does not take             */
 #define PAIR_ERANGE (-3)     /* gmax outside [2, 64], D < 1, R < 1, ld < D ...  */
-#define PAIR_EALIGN (-4)     /* scores base or row stride not 16-byte aligned   */
+#define PAIR_EALIGN (-4)     /* scores, caches or rows: a base or stride not
+                                16-byte aligned; gradients: not to an element  */
 #define PAIR_EHIP (-5)       /* a HIP launch or runtime call failed             */
 #define PAIR_EWORKSPACE (-6) /* workspace missing, misaligned or too small      */
 #define PAIR_ESCRATCH (-7)   /* one prompt's audit needs more than the static
                                 scratch of pair_audit_noalloc                  */
 
-/* Score dtypes. */
+/* Element types. */
 #define PAIR_F32 0
 #define PAIR_BF16 1
 #define PAIR_F16 2           /* gradients, caches and queries; scores are fp32 or bf16 */
@@ -62,7 +64,8 @@ extern "C" {
 #define PAIR_ST_BAD_GROUP 1  /* G_b < 2, G_b > gmax or offsets not monotone    */
 #define PAIR_ST_RHO_RANGE 2  /* an OBSERVED edge has rho outside (0, 1]        */
 #define PAIR_ST_P_RANGE 4    /* a continuation probability outside (0, 1]      */
-#define PAIR_ST_NONFINITE 8  /* a non-finite score in an audited score block    */
+#define PAIR_ST_NONFINITE 8  /* a non-finite score in an audited score block, or
+                                a gradient norm that is not finite             */
 #define PAIR_ST_BUDGET 16    /* design: budget below pi_min * sum(c), or an
                                 invalid prefix statistic (p outside [0, 1],
                                 c or m not positive and finite)               */
