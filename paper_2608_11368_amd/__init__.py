@@ -786,21 +786,16 @@ def page_plan(cached, fresh, table, free_pages, free_count, page, max_tokens, ma
     place; `free_pages` int32 lists the pool's pages, the first `free_count`
     (int64 [1], on the GPU) of them free, and the new list and count come back
     as `free_pages` and `free_count`.  `max_tokens` bounds the new tokens."""
-    n, dev, cap = cached.numel(), cached.device, free_pages.numel()
-    # two allocations; the workspace, which must be aligned, comes first
-    scratch = pair_page_plan_workspace_bytes(n) // 4
-    ws, lens, positions, new_free = torch.empty(
-        scratch + n + max_tokens + cap, dtype=torch.int32, device=dev).split(
-            [scratch, n, max_tokens, cap])
-    q_offsets, slots, new_count = torch.empty(
-        n + 1 + max_tokens + 1, dtype=torch.int64, device=dev).split([n + 1, max_tokens, 1])
-    out = {"q_offsets": q_offsets, "lens": lens, "slots": slots, "positions": positions,
-           "table": table, "free_pages": new_free, "free_count": new_count,
-           "status": _status(dev)}
+    n, cap = cached.numel(), free_pages.numel()
+    ws, lens, positions, new_free, q_offsets, slots, new_count = _native().parts(
+        cached.get_device(), torch.uint8, pair_page_plan_workspace_bytes(n), torch.int32, n,
+        torch.int32, max_tokens, torch.int32, cap, torch.int64, n + 1, torch.int64, max_tokens,
+        torch.int64, 1)
+    st = _status(cached.device)
     pair_page_plan(n, cached, fresh, mask, page, table, free_pages, free_count, max_tokens,
-                   out["q_offsets"], out["lens"], out["slots"], out["positions"],
-                   out["free_pages"], out["free_count"], ws.view(torch.uint8), out["status"], stream)
-    return out
+                   q_offsets, lens, slots, positions, new_free, new_count, ws, st, stream)
+    return {"q_offsets": q_offsets, "lens": lens, "slots": slots, "positions": positions,
+            "table": table, "free_pages": new_free, "free_count": new_count, "status": st}
 
 
 @_allocating
@@ -820,14 +815,15 @@ def paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max_len,
     `max_len` bound a request's new tokens and keys; `scale` defaults to
     1/sqrt(dim)."""
     tokens, heads, dim = q.shape
-    dev = q.device
+    parts, index, lse = _native().parts, q.get_device(), None
     if out is None:
-        out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=dev)
-    lse = torch.empty((tokens, heads), dtype=torch.float32, device=dev) if want_lse else None
+        out, = parts(index, q.dtype, (tokens, heads, dim))
+    if want_lse:
+        lse, = parts(index, torch.float32, (tokens, heads))
     need = _attention_workspace(lens.numel(), tokens, heads, k_cache.shape[2], dim, max_q, max_len)
     if workspace is None or workspace.numel() < need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    st = _status(dev)
+        workspace, = parts(index, torch.uint8, need)
+    st = _status(q.device)
     pair_paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max_len,
                          dim ** -0.5 if scale is None else scale, out, lse, workspace, st, stream)
     return {"out": out, "lse": lse, "status": st}
@@ -842,10 +838,8 @@ def clip_grads(grads, max_norm, out=None, stream=None):
     if not grads:
         raise ValueError("grads is empty")
     out = None if out is None else list(out)
-    dev = grads[0].device
-    norm = torch.empty(1, dtype=torch.float32, device=dev)
-    coef = torch.empty(1, dtype=torch.float32, device=dev)
-    st = _status(dev)
-    ws = torch.empty(pair_clip_grads_workspace_bytes(len(grads)), dtype=torch.uint8, device=dev)
+    norm, coef, ws = _native().parts(grads[0].get_device(), torch.float32, 1, torch.float32, 1,
+                                     torch.uint8, pair_clip_grads_workspace_bytes(len(grads)))
+    st = _status(grads[0].device)
     pair_clip_grads(grads, max_norm, norm, coef, ws, out, st, stream)
     return {"norm": norm, "coef": coef, "out": grads if out is None else out, "status": st}

@@ -6,8 +6,10 @@
 
 #include <exception>
 
+#include <ATen/ops/empty.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/DynamicTypes.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 namespace {
@@ -68,8 +70,8 @@ PyObject* grad_table(PyObject*, PyObject* args) {
                      reinterpret_cast<PyObject*>(torch::getTHPDtype(other)));
       else
         result = PyTuple_Pack(3, ptrs, sizes, codes);
-    } catch (const std::exception& e) {
-      if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {
+      torch::translate_exception_to_python(std::current_exception());
     }
   }
   Py_XDECREF(ptrs);
@@ -109,10 +111,77 @@ PyObject* address(PyObject*, PyObject* const* args, Py_ssize_t n) {
                             (long long)t.numel(), least);
     }
     return PyLong_FromUnsignedLongLong(reinterpret_cast<uint64_t>(t.data_ptr()));
-  } catch (const std::exception& e) {
-    if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
+  } catch (...) {
+    torch::translate_exception_to_python(std::current_exception());
     return nullptr;
   }
+}
+
+// parts(device, dtype, shape, dtype, shape, ...): uninitialised tensors, each
+// 256-byte aligned, of one allocation on the current stream (a shape is a tuple,
+// or an int for one dimension).  An allocation takes 1.3 us through the
+// interpreter and a part of one cut there 0.55; here a part takes 0.15.
+PyObject* parts(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  constexpr Py_ssize_t kMost = 16, kDims = 4;
+  if (n < 3 || n % 2 == 0 || n / 2 > kMost || !PyLong_Check(args[0])) {
+    PyErr_SetString(PyExc_TypeError, "parts(device, dtype, shape, ...)");
+    return nullptr;
+  }
+  const Py_ssize_t count = n / 2;
+  at::ScalarType type[kMost];
+  int64_t shape[kMost][kDims], start[kMost], bytes = 0;
+  size_t dims[kMost];
+  for (Py_ssize_t i = 0; i < count; ++i) {
+    PyObject *dtype = args[1 + 2 * i], *size = args[2 + 2 * i];
+    const bool tuple = PyTuple_Check(size);
+    if (!THPDtype_Check(dtype) || (tuple && PyTuple_GET_SIZE(size) > kDims)) {
+      PyErr_SetString(PyExc_TypeError, "parts(device, dtype, shape, ...)");
+      return nullptr;
+    }
+    type[i] = reinterpret_cast<THPDtype*>(dtype)->scalar_type;
+    dims[i] = tuple ? PyTuple_GET_SIZE(size) : 1;
+    int64_t room = (int64_t)c10::elementSize(type[i]);
+    for (size_t d = 0; d < dims[i]; ++d) {
+      const int64_t v = PyLong_AsLongLong(tuple ? PyTuple_GET_ITEM(size, d) : size);
+      if (v == -1 && PyErr_Occurred()) return nullptr;
+      if (v < 0 || __builtin_mul_overflow(room, v, &room) || room > (int64_t)1 << 48) {
+        PyErr_SetString(PyExc_ValueError, "a size is negative or too large");
+        return nullptr;
+      }
+      shape[i][d] = v;
+    }
+    start[i] = bytes;
+    bytes += (room + 255) / 256 * 256;
+  }
+  const long device = PyLong_AsLong(args[0]);
+  if (device < 0) {
+    if (!PyErr_Occurred())
+      PyErr_SetString(PyExc_ValueError, "the arguments must be CUDA (HIP) tensors");
+    return nullptr;
+  }
+  PyObject* result = PyTuple_New(count);
+  if (result == nullptr) return nullptr;
+  try {
+    const at::Tensor all = at::empty(
+        {bytes}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, (c10::DeviceIndex)device));
+    for (Py_ssize_t i = 0; i < count; ++i) {
+      at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(
+          c10::Storage(all.storage()), all.key_set(), c10::scalarTypeToTypeMeta(type[i]));
+      t.unsafeGetTensorImpl()->set_storage_offset(start[i] / (int64_t)c10::elementSize(type[i]));
+      t.unsafeGetTensorImpl()->set_sizes_contiguous(c10::IntArrayRef(shape[i], dims[i]));
+      PyObject* wrapped = THPVariable_Wrap(std::move(t));
+      if (wrapped == nullptr) {
+        Py_DECREF(result);
+        return nullptr;
+      }
+      PyTuple_SET_ITEM(result, i, wrapped);
+    }
+  } catch (...) {
+    Py_DECREF(result);
+    torch::translate_exception_to_python(std::current_exception());
+    return nullptr;
+  }
+  return result;
 }
 
 PyMethodDef kMethods[] = {
@@ -121,6 +190,9 @@ PyMethodDef kMethods[] = {
     {"address", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(address)),
      METH_FASTCALL,
      "address(tensor, name, dtype, least=0, optional=False): a checked tensor's data pointer."},
+    {"parts", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(parts)),
+     METH_FASTCALL,
+     "parts(device, dtype, shape, ...): uninitialised GPU tensors of one allocation."},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, kMethods,

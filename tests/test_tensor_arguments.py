@@ -58,3 +58,48 @@ def test_against_torch():
         address(flat[3:], "x", torch.float32, 998)
     with pytest.raises(TypeError, match="must be torch.int32, got torch.float32"):
         address(flat, "x", torch.int32)
+
+
+def test_parts_refusals():
+    parts = pair._native().parts
+    for call in ((), (0,), (0, torch.int32), (0, torch.int32, 3, 4), ("0", torch.int32, 3),
+                 (0, "int32", 3), (0, torch.int32, (1, 2, 3, 4, 5)), (0, torch.int32, None),
+                 (0,) + (torch.int32, 1) * 17):
+        with pytest.raises(TypeError):
+            parts(*call)
+    for call in ((-1, torch.int32, 3), (0, torch.int32, -1), (0, torch.int32, (1 << 40, 1 << 40))):
+        with pytest.raises(ValueError):
+            parts(*call)
+
+
+@pytest.mark.gpu
+def test_parts():
+    """Parts of one allocation are tensors like others: shapes, types, places
+    apart, written without touching each other, alive on their own."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    want = [(torch.uint8, 7), (torch.int32, (3, 5)), (torch.float32, 0), (torch.int64, 33),
+            (torch.bfloat16, (2, 3, 4)), (torch.float32, (1, 1))]
+    got = pair._native().parts(0, *[x for pair_ in want for x in pair_])
+    spans = []
+    for k, (t, (dtype, shape)) in enumerate(zip(got, want)):
+        assert t.dtype is dtype and t.device == torch.device(DEV) and t.is_contiguous()
+        assert tuple(t.shape) == (shape if isinstance(shape, tuple) else (shape,))
+        assert t.data_ptr() % 256 == 0 and not t.requires_grad and t._base is None
+        if t.numel():                 # an empty tensor's address reads as 0
+            spans.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()))
+        t.fill_(k + 1)
+    assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
+    for k, t in enumerate(got):
+        assert bool((t == k + 1).all())
+    last, first = got[3], got[0]
+    del got, t
+    torch.zeros(1 << 20, device=DEV)
+    assert bool((last == 4).all()) and bool((first == 1).all())
+    leaf = pair._native().parts(0, torch.float32, 4)[0].fill_(2.0).requires_grad_()
+    (leaf * leaf).sum().backward()
+    assert leaf.grad.tolist() == [4.0] * 4
+    with torch.inference_mode():
+        assert pair._native().parts(0, torch.float32, 4)[0].fill_(1.0).sum().item() == 4.0
+    with pytest.raises(torch.OutOfMemoryError):
+        pair._native().parts(0, torch.uint8, 1 << 44)
