@@ -412,9 +412,6 @@ def pair_audit_exact(B, nv, gmax, offsets, scores, rewards, p, pi_w, rule, wmax,
         _dev(d_status, "d_status", torch.int32, 1, True), _stream(stream)), "pair_audit_exact")
 
 
-_DTYPE_CODE = {torch.float32: PAIR_F32, torch.bfloat16: PAIR_BF16, torch.float16: PAIR_F16}
-
-
 def pair_page_plan_workspace_bytes(n) -> int:
     return int(lib().pair_page_plan_workspace_bytes(n))
 
@@ -439,14 +436,7 @@ def pair_page_plan(n, cached, fresh, mask, page, table, free_pages, free_count, 
         at(d_status, "d_status", torch.int32, 1, True), _stream(stream)), "pair_page_plan")
 
 
-def _cache_arg(k_cache, v_cache):
-    """Pointers, element type, layout and shape of a key and a value cache."""
-    if isinstance(k_cache, torch.Tensor) and isinstance(v_cache, torch.Tensor):
-        shape, strides, dtype = k_cache.shape, k_cache.stride(), k_cache.dtype
-        if (v_cache.shape == shape and v_cache.stride() == strides and v_cache.dtype is dtype
-                and len(shape) == 4 and strides[3] == 1 and k_cache.is_cuda and v_cache.is_cuda
-                and (dtype is torch.bfloat16 or dtype is torch.float16)):
-            return k_cache.data_ptr(), v_cache.data_ptr(), dtype, strides, shape
+def _cache_refused(k_cache, v_cache):
     for name, c in (("k_cache", k_cache), ("v_cache", v_cache)):
         if not isinstance(c, torch.Tensor) or not c.is_cuda or c.dim() != 4:
             raise ValueError(f"{name} must be a 4-D CUDA tensor [pages][page][kv_heads][dim]")
@@ -457,33 +447,31 @@ def _cache_arg(k_cache, v_cache):
     raise ValueError("k_cache and v_cache must have the same strides and contiguous rows")
 
 
-def _rows_arg(t, name, dtype, heads, dim):
-    """Pointer, strides and shape of rows [tokens][heads][dim]."""
-    if isinstance(t, torch.Tensor):
-        shape, strides = t.shape, t.stride()
-        if (len(shape) == 3 and t.dtype is dtype and t.is_cuda and shape[2] == dim
-                and strides[2] == 1 and (heads is None or shape[1] == heads)):
-            return t.data_ptr(), strides[0], strides[1], shape
+def _rows_refused(t, name, dtype, heads, dim):
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 3:
         raise ValueError(f"{name} must be a 3-D CUDA tensor [tokens][heads][dim]")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, needs {heads} heads of {dim}")
+    if t.shape[2] != dim or (heads != 0 and t.shape[1] != heads):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, needs {heads or 'its'} heads of {dim}")
     raise ValueError(f"{name} rows must be contiguous")
 
 
 def pair_cache_store(k, v, slots, k_cache, v_cache, d_status=None, stream=None):
-    kc, vc, dtype, st, (pages, page, heads, dim) = _cache_arg(k_cache, v_cache)
-    kp, tok, head, shape = _rows_arg(k, "k", dtype, heads, dim)
-    vp, vtok, vhead, vshape = _rows_arg(v, "v", dtype, heads, dim)
-    if vtok != tok or vhead != head or vshape != shape:
+    native = _native()
+    c = native.cache(k_cache, v_cache) or _cache_refused(k_cache, v_cache)
+    kc, vc, code, page_stride, slot_stride, head_stride, pages, page, heads, dim = c
+    kp, tok, head, tokens, _ = (native.rows(k, code, heads, dim)
+                                or _rows_refused(k, "k", k_cache.dtype, heads, dim))
+    vp, vtok, vhead, vtokens, _ = (native.rows(v, code, heads, dim)
+                                   or _rows_refused(v, "v", k_cache.dtype, heads, dim))
+    if vtok != tok or vhead != head or vtokens != tokens:
         raise ValueError("k and v must have the same shape and strides")
-    at, tokens = _native().address, shape[0]
     _rc(lib().pair_cache_store(
-        tokens, heads, dim, _DTYPE_CODE[dtype], kp, vp, tok, head, kc, vc, st[0], st[1], st[2], page, pages,
-        at(slots, "slots", torch.int64, tokens), at(d_status, "d_status", torch.int32, 1, True),
-        _stream(stream)), "pair_cache_store")
+        tokens, heads, dim, code, kp, vp, tok, head, kc, vc, page_stride, slot_stride, head_stride,
+        page, pages, native.address(slots, "slots", torch.int64, tokens),
+        native.address(d_status, "d_status", torch.int32, 1, True), _stream(stream)),
+        "pair_cache_store")
 
 
 def pair_paged_attention_workspace_bytes(n, tokens, q_heads, kv_heads, dim, max_q, max_len) -> int:
@@ -493,18 +481,22 @@ def pair_paged_attention_workspace_bytes(n, tokens, q_heads, kv_heads, dim, max_
 
 def pair_paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max_len, scale, out,
                          lse, workspace, d_status=None, stream=None):
-    kc, vc, dtype, st, (pages, page, kv_heads, dim) = _cache_arg(k_cache, v_cache)
-    qp, qt, qh, (tokens, heads, _) = _rows_arg(q, "q", dtype, None, dim)
-    op, ot, oh, oshape = _rows_arg(out, "out", dtype, heads, dim)
+    native = _native()
+    c = native.cache(k_cache, v_cache) or _cache_refused(k_cache, v_cache)
+    kc, vc, code, page_stride, slot_stride, head_stride, pages, page, kv_heads, dim = c
+    qp, qt, qh, tokens, heads = (native.rows(q, code, 0, dim)
+                                 or _rows_refused(q, "q", k_cache.dtype, 0, dim))
+    op, ot, oh, orows, _ = (native.rows(out, code, heads, dim)
+                            or _rows_refused(out, "out", k_cache.dtype, heads, dim))
     n = lens.numel()
     if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[0] < n:
         raise ValueError("table must be a 2-D tensor with a row for each request")
-    if oshape[0] < tokens:
-        raise ValueError(f"out holds {oshape[0]} tokens, needs {tokens}")
-    at = _native().address
+    if orows < tokens:
+        raise ValueError(f"out holds {orows} tokens, needs {tokens}")
+    at = native.address
     _rc(lib().pair_paged_attention(
-        n, tokens, heads, kv_heads, dim, _DTYPE_CODE[dtype], qp, qt, qh, kc, vc, st[0], st[1], st[2], page,
-        pages, at(table, "table", torch.int32), table.shape[1],
+        n, tokens, heads, kv_heads, dim, code, qp, qt, qh, kc, vc, page_stride, slot_stride,
+        head_stride, page, pages, at(table, "table", torch.int32), table.shape[1],
         at(q_offsets, "q_offsets", torch.int64, n + 1), at(lens, "lens", torch.int32, n),
         int(max_q), int(max_len), float(scale), op, ot, oh,
         at(lse, "lse", torch.float32, tokens * heads, True),

@@ -117,6 +117,60 @@ PyObject* address(PyObject*, PyObject* const* args, Py_ssize_t n) {
   }
 }
 
+bool half(const at::Tensor& t) {
+  return t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kHalf;
+}
+
+// cache(k_cache, v_cache) -> (addresses, type code, strides of a page, a slot and
+// a head, pages, page, heads, width), or None if they are not a paged cache's
+// halves.
+PyObject* cache(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 2) {
+    PyErr_SetString(PyExc_TypeError, "cache(k_cache, v_cache)");
+    return nullptr;
+  }
+  if (!THPVariable_Check(args[0]) || !THPVariable_Check(args[1])) Py_RETURN_NONE;
+  try {
+    const at::Tensor &k = THPVariable_Unpack(args[0]), &v = THPVariable_Unpack(args[1]);
+    if (!k.is_cuda() || !v.is_cuda() || k.dim() != 4 || !half(k) ||
+        v.scalar_type() != k.scalar_type() || v.sizes() != k.sizes() ||
+        v.strides() != k.strides() || k.stride(3) != 1)
+      Py_RETURN_NONE;
+    return Py_BuildValue("KKiLLLLLLL", (unsigned long long)k.data_ptr(),
+                         (unsigned long long)v.data_ptr(), (int)dtype_code(k.scalar_type()),
+                         (long long)k.stride(0), (long long)k.stride(1), (long long)k.stride(2),
+                         (long long)k.size(0), (long long)k.size(1), (long long)k.size(2),
+                         (long long)k.size(3));
+  } catch (...) {
+    torch::translate_exception_to_python(std::current_exception());
+    return nullptr;
+  }
+}
+
+// rows(tensor, type code, heads or 0, width) -> (address, strides of a row and a
+// head, rows, heads), or None if it is not [rows][heads][width] of that type.
+PyObject* rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 4) {
+    PyErr_SetString(PyExc_TypeError, "rows(tensor, type code, heads, width)");
+    return nullptr;
+  }
+  if (!THPVariable_Check(args[0])) Py_RETURN_NONE;
+  const long code = PyLong_AsLong(args[1]), heads = PyLong_AsLong(args[2]),
+             width = PyLong_AsLong(args[3]);
+  if ((code == -1 || heads == -1 || width == -1) && PyErr_Occurred()) return nullptr;
+  try {
+    const at::Tensor& t = THPVariable_Unpack(args[0]);
+    if (!t.is_cuda() || t.dim() != 3 || dtype_code(t.scalar_type()) != code ||
+        t.size(2) != width || t.stride(2) != 1 || (heads != 0 && t.size(1) != heads))
+      Py_RETURN_NONE;
+    return Py_BuildValue("KLLLL", (unsigned long long)t.data_ptr(), (long long)t.stride(0),
+                         (long long)t.stride(1), (long long)t.size(0), (long long)t.size(1));
+  } catch (...) {
+    torch::translate_exception_to_python(std::current_exception());
+    return nullptr;
+  }
+}
+
 // parts(device, dtype, shape, dtype, shape, ...): uninitialised tensors, each
 // 256-byte aligned, of one allocation on the current stream (a shape is a tuple,
 // or an int for one dimension).  An allocation takes 1.3 us through the
@@ -190,6 +244,10 @@ PyMethodDef kMethods[] = {
     {"address", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(address)),
      METH_FASTCALL,
      "address(tensor, name, dtype, least=0, optional=False): a checked tensor's data pointer."},
+    {"cache", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(cache)),
+     METH_FASTCALL, "cache(k_cache, v_cache): addresses and layout, None if it is no cache."},
+    {"rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(rows)),
+     METH_FASTCALL, "rows(tensor, type code, heads, width): address and layout, or None."},
     {"parts", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(parts)),
      METH_FASTCALL,
      "parts(device, dtype, shape, ...): uninitialised GPU tensors of one allocation."},

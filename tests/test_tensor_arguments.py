@@ -72,6 +72,38 @@ def test_parts_refusals():
             parts(*call)
 
 
+def test_layouts_of_others_are_none():
+    native = pair._native()
+    x = torch.zeros(2, 4, 2, 64, dtype=torch.bfloat16)      # not on a GPU
+    assert native.cache(x, x) is None and native.cache(None, x) is None
+    assert native.rows(x[0], 1, 2, 64) is None and native.rows("x", 1, 2, 64) is None
+    for call in ((), (x,), (x, x, x)):
+        with pytest.raises(TypeError):
+            native.cache(*call)
+    with pytest.raises(TypeError):
+        native.rows(x[0], 1, 2)
+
+
+@pytest.mark.gpu
+def test_layouts_against_torch():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    native = pair._native()
+    both = torch.zeros(3, 5, 16, 2, 2, 64, dtype=torch.float16, device=DEV)
+    k, v = both[1:, :, 2:, 0, :1].transpose(1, 2)[:, :, 0], both[1:, :, 2:, 1, :1].transpose(1, 2)[:, :, 0]
+    assert k.dim() == 4
+    assert native.cache(k, v) == (k.data_ptr(), v.data_ptr(), 2, *k.stride()[:3], *k.shape)
+    assert native.cache(k, v[:1]) is None and native.cache(k, v.bfloat16()) is None
+    assert native.cache(k, v.contiguous()) is None and native.cache(k.float(), v.float()) is None
+    assert native.cache(k[..., ::2], v[..., ::2]) is None and native.cache(k[0], v[0]) is None
+    q = torch.zeros(7, 9, 128, dtype=torch.bfloat16, device=DEV)[1:, ::2, :64]
+    assert native.rows(q, 1, 0, 64) == (q.data_ptr(), 9 * 128, 256, 6, 5)
+    assert native.rows(q, 1, 5, 64) == native.rows(q, 1, 0, 64)
+    for other in ((q, 2, 5, 64), (q, 1, 4, 64), (q, 1, 5, 32), (q[0], 1, 5, 64),
+                  (q[..., ::2], 1, 5, 32)):
+        assert native.rows(*other) is None
+
+
 @pytest.mark.gpu
 def test_parts():
     """Parts of one allocation are tensors like others: shapes, types, places
