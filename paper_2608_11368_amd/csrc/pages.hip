@@ -14,7 +14,7 @@ constexpr int kThreads = 256;
 // given back) settle everything; each output element then finds its request
 // by bisection of the scans' ends.  Bound by launches and by loads that wait for
 // each other, not by bytes: 64 requests 4.4 us; 16,896 requests with half of
-// them released, 1.1M tokens, 4 + 6 + 15 us (of 16 MB: 3 us at the rate of a
+// them released, 1.1M tokens, 4 + 6 + 13 us (of 16 MB: 3 us at the rate of a
 // copy).  Sums saturate at 2^31 - 1, beyond every capacity; saturating addition
 // of counts is associative, so the scans may be split anywhere.
 struct PlanArgs {
@@ -153,7 +153,8 @@ __device__ __forceinline__ uint32_t free_pages_of(const PlanArgs& a) {
   return f < 0 ? 0u : (f > a.capacity ? (uint32_t)a.capacity : (uint32_t)f);
 }
 
-constexpr int kTile = 4 * kThreads;   // outputs of a workgroup
+constexpr int kOwn = 4;               // outputs of a thread: searched and loaded side by side
+constexpr int kTile = kOwn * kThreads;
 constexpr int kNear = 512;            // requests that a tile keeps in LDS
 
 // A scan's ends over the requests [lo, hi] that a tile needs: in LDS where they
@@ -165,10 +166,25 @@ struct Near {
   uint32_t before;   // end of request lo - 1
 };
 
-__device__ __forceinline__ void find(const Near& n, uint32_t x, int* r, uint32_t* start) {
-  const int i = owner(n.ends, x, n.lo - n.base, n.hi - n.base);
-  *r = i + n.base;
-  *start = *r > n.lo ? n.ends[i - 1] : n.before;
+// Requests of several outputs, and where each request's outputs start: the number
+// of ends at or below x, halving all ranges together.
+template <int K>
+__device__ __forceinline__ void find(const Near& n, const uint32_t (&x)[K], int (&r)[K],
+                                     uint32_t (&start)[K]) {
+  int at[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) at[k] = n.lo - n.base;
+  for (int rest = n.hi - n.lo; rest > 0;) {
+    const int half = (rest + 1) >> 1;
+#pragma unroll
+    for (int k = 0; k < K; ++k) at[k] += n.ends[at[k] + half - 1] <= x[k] ? half : 0;
+    rest -= half;
+  }
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    r[k] = at[k] + n.base;
+    start[k] = r[k] > n.lo ? n.ends[at[k] - 1] : n.before;
+  }
 }
 
 // Outputs [tile * kTile, ...) of the tokens, then of the pages (the taken ones
@@ -202,12 +218,31 @@ __device__ __forceinline__ void plan_outputs(const PlanArgs& a, const Ends& e,
     }
     return n;
   };
-  auto pool_entry = [&](const Near& given, uint32_t j) {   // the free list, then the released
-    if (j < free) return a.free_pages[j];
-    int r;
-    uint32_t start;
-    find(given, j - free, &r, &start);
-    return a.table[(int64_t)r * a.ldt + (j - free - start)];
+  // Entry j of the pool: the free list, then the released pages.  Those of the
+  // list are loaded at once; the others take a search first.
+  auto pool_entries = [&](const Near& given, const bool (&wanted)[kOwn],
+                          const int32_t* (&from)[kOwn], const uint32_t (&j)[kOwn],
+                          int32_t (&id)[kOwn]) {
+    bool search = false;
+#pragma unroll
+    for (int s = 0; s < kOwn; ++s) {
+      const bool listed = wanted[s] && from[s] == nullptr && j[s] < free;
+      const bool released = wanted[s] && from[s] == nullptr && j[s] >= free && j[s] < avail;
+      search |= released;
+      if (listed) from[s] = a.free_pages + j[s];
+    }
+#pragma unroll
+    for (int s = 0; s < kOwn; ++s) id[s] = from[s] != nullptr ? *from[s] : -1;
+    if (!search) return;
+    uint32_t x[kOwn], start[kOwn];
+    int r[kOwn];
+#pragma unroll
+    for (int s = 0; s < kOwn; ++s) x[s] = j[s] >= free ? j[s] - free : 0u;
+    find(given, x, r, start);
+#pragma unroll
+    for (int s = 0; s < kOwn; ++s)
+      if (wanted[s] && from[s] == nullptr && j[s] >= free && j[s] < avail)
+        id[s] = a.table[(int64_t)r[s] * a.ldt + (x[s] - start[s])];
   };
   if (tile < token_tiles) {
     const int64_t t0 = tile * kTile;
@@ -224,33 +259,42 @@ __device__ __forceinline__ void plan_outputs(const PlanArgs& a, const Ends& e,
     }
     if (NARROW) __syncthreads();
     const Near anyone = {e.given, 0, last, 0, 0u};
+    uint32_t t[kOwn], start[kOwn], off[kOwn], j[kOwn];
+    int r[kOwn];
+    int32_t pos[kOwn], id[kOwn];
+    bool live[kOwn];
+    const int32_t* from[kOwn];
 #pragma unroll
-    for (int s = 0; s < kTile / kThreads; ++s) {
-      const int64_t t = t0 + s * kThreads + threadIdx.x;
-      if (t >= a.max_tokens) break;
-      int64_t slot = -1;
-      int32_t pos = -1;
-      if ((uint32_t)t < total.tokens) {
-        int r;
-        uint32_t start;
-        find(owners, (uint32_t)t, &r, &start);
-        const uint32_t c = staged ? near[1][r - owners.lo] : (uint32_t)a.cached[r];
-        const uint32_t x = c + (uint32_t)t - start;
+    for (int s = 0; s < kOwn; ++s) t[s] = (uint32_t)t0 + s * kThreads + threadIdx.x;
+    find(owners, t, r, start);
+#pragma unroll
+    for (int s = 0; s < kOwn; ++s) {
+      live[s] = t[s] < total.tokens && t[s] < (uint32_t)a.max_tokens;
+      pos[s] = -1;
+      off[s] = j[s] = 0;
+      from[s] = nullptr;
+      if (live[s]) {
+        const uint32_t c = staged ? near[1][r[s] - owners.lo] : (uint32_t)a.cached[r[s]];
+        const uint32_t x = c + t[s] - start[s];
         const uint32_t held = pages_of(c, a.page);
         const uint32_t pg = div_by(x, a.page);
-        int32_t id;
+        pos[s] = (int32_t)x;
+        off[s] = x - pg * a.page.d;
         if (pg < held) {
-          id = a.table[(int64_t)r * a.ldt + pg];
+          from[s] = a.table + (int64_t)r[s] * a.ldt + pg;
         } else {
-          const uint32_t first = staged ? near[2][r - owners.lo] : (r > 0 ? e.taken[r - 1] : 0u);
-          const uint32_t j = first + (pg - held);
-          id = j < avail ? pool_entry(anyone, j) : -1;
+          const uint32_t first =
+              staged ? near[2][r[s] - owners.lo] : (r[s] > 0 ? e.taken[r[s] - 1] : 0u);
+          j[s] = first + (pg - held);
         }
-        pos = (int32_t)x;
-        if (id >= 0) slot = (int64_t)id * a.page.d + (x - pg * a.page.d);
       }
-      a.slots[t] = slot;
-      if (a.positions != nullptr) a.positions[t] = pos;
+    }
+    pool_entries(anyone, live, from, j, id);
+#pragma unroll
+    for (int s = 0; s < kOwn; ++s) {
+      if (t[s] >= (uint32_t)a.max_tokens) break;
+      a.slots[t[s]] = id[s] >= 0 ? (int64_t)id[s] * a.page.d + off[s] : -1;
+      if (a.positions != nullptr) a.positions[t[s]] = pos[s];
     }
     return;
   }
@@ -264,20 +308,33 @@ __device__ __forceinline__ void plan_outputs(const PlanArgs& a, const Ends& e,
   if (NARROW) __syncthreads();
   const Near takers = stage(0, e.taken), givers = stage(1, e.given), later = stage(2, e.given);
   if (NARROW) __syncthreads();
+  uint32_t j[kOwn], left[kOwn], start[kOwn];
+  int r[kOwn];
+  int32_t id[kOwn];
+  bool inside[kOwn], taken[kOwn];
+  const int32_t* from[kOwn];
 #pragma unroll
-  for (int s = 0; s < kTile / kThreads; ++s) {
-    const int64_t j = j0 + s * kThreads + threadIdx.x;
-    if (j >= a.capacity) break;
-    const uint32_t from = used + (uint32_t)j;
-    a.free_out[j] = from < avail ? pool_entry(later, from) : -1;
-    if ((uint32_t)j < used) {
-      int r;
-      uint32_t start;
-      find(takers, (uint32_t)j, &r, &start);
-      const uint32_t held = pages_of((uint32_t)a.cached[r], a.page);
-      a.table[(int64_t)r * a.ldt + held + ((uint32_t)j - start)] = pool_entry(givers, (uint32_t)j);
-    }
+  for (int s = 0; s < kOwn; ++s) {
+    j[s] = (uint32_t)j0 + s * kThreads + threadIdx.x;
+    inside[s] = j[s] < (uint32_t)a.capacity;
+    taken[s] = inside[s] && j[s] < used;
+    left[s] = used + j[s];
+    from[s] = nullptr;
   }
+  pool_entries(later, inside, from, left, id);
+#pragma unroll
+  for (int s = 0; s < kOwn; ++s)
+    if (inside[s]) a.free_out[j[s]] = id[s];
+  if (first >= used) return;
+  find(takers, j, r, start);
+#pragma unroll
+  for (int s = 0; s < kOwn; ++s) from[s] = nullptr;
+  pool_entries(givers, taken, from, j, id);
+#pragma unroll
+  for (int s = 0; s < kOwn; ++s)
+    if (taken[s])
+      a.table[(int64_t)r[s] * a.ldt + pages_of((uint32_t)a.cached[r[s]], a.page) +
+              (j[s] - start[s])] = id[s];
 }
 
 // Table entries that the pool has no page for become -1, and what does not fit
@@ -347,8 +404,8 @@ __global__ __launch_bounds__(kThreads) void plan_fused_kernel(PlanArgs a, int64_
 // More requests: a first launch writes the scans' ends to the workspace.  Each
 // of its workgroups owns kScan requests and sums the ones before them itself,
 // or, beyond kSelfSummed requests, takes the sums that a launch before it left.
-// (A call of 4,096 requests 23.4 us by itself, 26.2 us with that launch; 16,384:
-// 27.9 and 27.6; 65,536: 41.9 and 30.0; 2^20: 559 and 60.)
+// (A call of 4,096 requests 16.2 us by itself, 18.7 us with that launch; 16,384:
+// 19.8 and 20.7; 32,768: 25.2 and 23.8; 65,536: 33.1 and 22.8; 2^20: 550 and 52.)
 constexpr int kScan = 1024;
 constexpr int64_t kSelfSummed = 1 << 14;
 
