@@ -18,8 +18,9 @@
 // workgroup: they are a few cached kilobytes), and a run has one workgroup for
 // each key head.  Those walk it side by side, so that the heads of a slot, which
 // lie together in memory, are read at about the same time.  A request that is
-// cut leaves partial sums that a second launch joins.  The four waves of a
-// workgroup take the 32-key blocks in turn and are joined through LDS.
+// cut leaves partial sums that a second launch joins.  The waves of a workgroup
+// (four; eight in calls of a few short requests, which are not cut) take the
+// 32-key blocks in turn and are joined through LDS.
 //
 // Bound by the cache's bytes.  Measured: one token for each of 256 requests of
 // 4000 keys on average, 8 heads of width 128, 4.1 GB: 649 us and 8 us for the
@@ -39,6 +40,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBlock = 32;                  // keys of a wave's step
 constexpr int kUnit = kBlock * kWaves;      // keys of a workgroup's step
+constexpr int kWideWaves = 2 * kWaves;      // of a workgroup that has a compute unit for itself
 // Requests whose lengths a workgroup scans; more of them fill the card with
 // one workgroup per request and head.
 constexpr int kMostScanned = 2048;
@@ -171,7 +173,7 @@ __device__ __forceinline__ void add_odd_block(WaveLds<DIM, NT>* lds, const u32x4
   wave_lds_order();
 }
 
-template <bool BF16, int DIM, int NT, bool ALIGNED>
+template <bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
 __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[NT][DIM / 32],
                                          const int (&limit)[NT], int first_limit, int64_t r,
                                          int64_t kvh, int len, int k0, int k1,
@@ -209,7 +211,7 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
     }
   };
   if (k0 < k1) lookup(k0);
-  for (int kb = k0; kb < k1; kb += kUnit) {
+  for (int kb = k0; kb < k1; kb += kBlock * WAVES) {
     Piece<DIM> kr[8], vr[8];
     int64_t at[kIds];
 #pragma unroll
@@ -224,7 +226,7 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       vr[e].load(vbase + at[ALIGNED ? e >> 2 : e] + (ALIGNED ? (e & 3) * slot_bytes : 0));
-    if (kb + kUnit < k1) lookup(kb + kUnit);
+    if (kb + kBlock * WAVES < k1) lookup(kb + kBlock * WAVES);
 
     // keys through LDS: whole rows come from memory, the product wants a row's
     // piece from every lane
@@ -320,7 +322,7 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
 
 // Keys [k0, k1) of one request and head (k0 a multiple of kUnit): the waves'
 // sums, joined, either as results (slot < 0) or as partial sums.
-template <bool BF16, int DIM, int NT, bool ALIGNED>
+template <bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
 __device__ __forceinline__ void attend(const RowArgs& s, int64_t r, int kvh, int k0, int k1,
                                        int64_t slot, WaveLds<DIM, NT>* lds) {
   constexpr int ND = DIM / 16;
@@ -354,7 +356,7 @@ __device__ __forceinline__ void attend(const RowArgs& s, int64_t r, int kvh, int
   // unused rows see nothing, so every block counts as masked for them only if
   // it does for the first token
   const int end = k1 < q.len ? k1 : q.len;
-  add_keys<BF16, DIM, NT, ALIGNED>(s, qf, limit, q.len - q.tokens, r, kvh, q.len,
+  add_keys<BF16, DIM, NT, ALIGNED, WAVES>(s, qf, limit, q.len - q.tokens, r, kvh, q.len,
                                    k0 + kBlock * wave, end, lds + wave, &st);
 
 #pragma unroll
@@ -371,17 +373,17 @@ __device__ __forceinline__ void attend(const RowArgs& s, int64_t r, int kvh, int
 #pragma unroll
       for (int j = 0; j < ND; ++j) lds[wave].sum[x][(4 * g + i) * ND + j] = st.acc[nt][j][i];
     __syncthreads();
-    for (int e = threadIdx.x; e < 16 * DIM / 8; e += kThreads) {
+    for (int e = threadIdx.x; e < 16 * DIM / 8; e += WAVES * kWave) {
       const int y = e / (DIM / 8), d = (e - y * (DIM / 8)) * 8;
       const int i = 16 * nt + y;
       if (i < rows) {
         float m = lds[0].stat[y][0];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, lds[w].stat[y][0]);
+        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, lds[w].stat[y][0]);
         const float base = m == -INFINITY ? 0.0f : m;
         float tot = 0.0f, o[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
           const float mw = lds[w].stat[y][0], lw = lds[w].stat[y][1];
           if (mw == -INFINITY && lw == 0.0f) continue;   // saw no key
           const float f = __builtin_amdgcn_exp2f(mw - base);
@@ -451,13 +453,14 @@ __device__ __forceinline__ void scan_units(const RowArgs& s, int32_t* start, int
     for (int r = threadIdx.x; r <= n; r += kThreads) s.starts[r] = start[r];
 }
 
-template <bool BF16, int DIM, int NT, bool ALIGNED>
-__global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(RowArgs s) {
-  __shared__ WaveLds<DIM, NT> lds[kWaves];
-  __shared__ int32_t start[kMostScanned + 1];
+template <bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave, 2) void attention_rows_kernel(RowArgs s) {
+  constexpr bool kCut = WAVES == kWaves;    // only calls of wide workgroups are never cut
+  __shared__ WaveLds<DIM, NT> lds[WAVES];
+  __shared__ int32_t start[kCut ? kMostScanned + 1 : 1];
   __shared__ int32_t wave_sum_of[kWaves];
   const int64_t heads = s.a.kv_heads;
-  const bool direct = s.runs == 0;          // one workgroup per request and head
+  const bool direct = !kCut || s.runs == 0;   // one workgroup per request and head
   const int64_t run = blockIdx.x / (uint32_t)s.a.kv_heads;   // or the request
   const int h = (int)(blockIdx.x - run * heads);
   const int n = (int)s.a.n;
@@ -495,7 +498,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_rows_kernel(RowArgs s) 
       c1 = count - c0 < end - u ? count : c0 + (int)(end - u);
       whole = c0 == 0 && c1 == count;
     }
-    attend<BF16, DIM, NT, ALIGNED>(s, r, h, c0 * kUnit, c1 * kUnit,
+    attend<BF16, DIM, NT, ALIGNED, WAVES>(s, r, h, c0 * kUnit, c1 * kUnit,
                                    whole ? -1 : part * heads + h, lds);
     part = 2 * run + 1;
     u += c1 - c0;
@@ -590,10 +593,11 @@ Plan plan_rows(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim, int32_
   const int64_t rows = (int64_t)max_q * (q_heads / kv_heads);
   p.rows = (int)(rows < kRowsMost ? rows : kRowsMost);
   p.tiles = p.rows <= 16 ? 1 : 2;
-  // Cut into equal runs (units are counted in 31 bits) unless the longest head is eight steps, which take less
-  // than the second launch would (4 requests of 700 keys: 10.9 us uncut, 16.5 us
-  // cut; of 1000: 14.3 and 16.4; of 2000: 24.7 and 16.7), or the requests are so
-  // many that they fill the card by themselves.
+  // Cut into equal runs (units are counted in 31 bits) unless the longest head is
+  // eight steps, which take less than the second launch would (4 requests of 700
+  // keys: 8.0 us uncut, 9.5 us cut; of 1000: 9.3 and 9.9; of 2000: 21 and 11; 32
+  // requests of 1000: 22 and 27), or the requests are so many that they fill the
+  // card by themselves.
   const int64_t most = n * ((max_len + kUnit - 1) / kUnit);
   int64_t runs = 2 * (int64_t)device_cu_count() / kv_heads;   // two workgroups fit a compute unit
   if (runs > most) runs = most;
@@ -612,14 +616,23 @@ int launch(const RowArgs& s, const Plan& p, hipStream_t stream) {
   const int64_t grid = (p.runs != 0 ? p.runs : s.a.n) * s.a.kv_heads;
   if (s.a.n * s.a.kv_heads > 0x7fffffffLL) return PAIR_ERANGE;
   const bool aligned = s.page.d % 16 == 0;
-#define PAIR_ROWS(NT, AL)                                                                        \
-  hipLaunchKernelGGL((attention_rows_kernel<BF16, DIM, NT, AL>), dim3((unsigned)grid),            \
-                     dim3(kThreads), 0, stream, s)
+  // Uncut workgroups that have a compute unit each: eight waves instead of four
+  // (4 requests of 400 keys, 8 heads of 128: 6.8 us instead of 7.8, of 1000: 9.3
+  // instead of 11.3; 32 requests, a workgroup for every unit: 22.1 both).
+  const bool wide = p.runs == 0 && grid <= device_cu_count();
+#define PAIR_ROWS(NT, AL, W)                                                                     \
+  hipLaunchKernelGGL((attention_rows_kernel<BF16, DIM, NT, AL, W>), dim3((unsigned)grid),         \
+                     dim3(W * kWave), 0, stream, s)
+#define PAIR_ROWS_OF(NT, AL)                                                                     \
+  do {                                                                                           \
+    if (wide) PAIR_ROWS(NT, AL, kWideWaves); else PAIR_ROWS(NT, AL, kWaves);                      \
+  } while (0)
   if (p.tiles == 1) {
-    if (aligned) PAIR_ROWS(1, true); else PAIR_ROWS(1, false);
+    if (aligned) PAIR_ROWS_OF(1, true); else PAIR_ROWS_OF(1, false);
   } else {
-    if (aligned) PAIR_ROWS(2, true); else PAIR_ROWS(2, false);
+    if (aligned) PAIR_ROWS_OF(2, true); else PAIR_ROWS_OF(2, false);
   }
+#undef PAIR_ROWS_OF
 #undef PAIR_ROWS
   if (hipGetLastError() != hipSuccess) return PAIR_EHIP;
   if (p.runs != 0)

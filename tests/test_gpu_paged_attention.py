@@ -298,6 +298,18 @@ def test_many_requests(n, case):
     c.check(c.call(), only=[0, 3, 5, 7, 8, 9, 63, 64, 65, n // 2, n - 2, n - 1])
 
 
+@pytest.mark.parametrize("n,most", [(3, 1024), (3, 1025), (140, 1024), (140, 1025)])
+@pytest.mark.parametrize("page", [16, 20])
+def test_short_requests_around_the_cut(n, most, page):
+    """Lengths at which a call of single tokens changes its split: workgroups of
+    eight waves (few requests) or four, whole or in runs, the longest last."""
+    log(f"paged attention: {n} requests of at most {most} keys, pages of {page}")
+    lens = np.random.default_rng(most).integers(1, 300, n)
+    lens[:3], lens[n - 1] = [33, 257, 0], most
+    c = Cache(lens, np.ones(n, dtype=np.int64), 4, 2, 128, page, "bf16", seed=n)
+    c.check(c.call(), only=[0, 1, 2, n // 2, n - 1])
+
+
 @pytest.mark.parametrize("new", [[1, 1, 0, 1], [70, 1, 0, 40]])
 def test_rows_past_the_last_request(new):
     """More rows of q than the requests have: the others are not touched."""
