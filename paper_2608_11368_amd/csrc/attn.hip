@@ -16,6 +16,19 @@ size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 // bound's tokens, or there is only one, none does.
 bool has_few(int64_t n, int64_t tokens, int32_t max_q) { return n > 1 && tokens < n * max_q; }
 
+// One launch serves both kinds side by side where most requests must be short
+// against the longest (two chunks of 1024 tokens beside 130 single ones over 4000
+// keys, 8 heads of 128: 410 us, two launches 467), or the tiles do not fill the
+// card (one of 90 beside 15 over 3000: 59 and 77; three prompts of 300 to 512 at
+// width 64, none short: 13.6 and 15.4).  It holds the registers of both, for which
+// chunks pay where they are all there is (8 prompts of 301 to 4096 at width 64: 182
+// and 177 us; three chunks over 4000 to 8000 keys at 128: 672 and 627).
+bool together(const AttnCall& a) {
+  const int64_t group = a.q_heads / a.kv_heads;
+  const int64_t tiles = a.tokens * group / 128 + (a.n < a.tokens ? a.n : a.tokens);
+  return a.tokens < a.n * a.max_q / 4 || tiles * a.kv_heads <= 2 * (int64_t)device_cu_count();
+}
+
 }  // namespace
 
 size_t attention_workspace_bytes(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads,
@@ -29,13 +42,17 @@ size_t attention_workspace_bytes(int64_t n, int64_t tokens, int32_t q_heads, int
 int launch_attention(const AttnCall& a, void* workspace, hipStream_t stream) {
   if (most_rows(a.q_heads, a.kv_heads, a.max_q) <= kRowsMost)
     return launch_attention_rows(a, workspace, stream);
-  if (!has_few(a.n, a.tokens, a.max_q)) return launch_attention_tiles(a, 0, workspace, stream);
-  const int rc = launch_attention_rows(a, workspace, stream);
+  if (!has_few(a.n, a.tokens, a.max_q))
+    return launch_attention_tiles(a, 0, nullptr, workspace, stream);
+  void* few = workspace;
+  void* tiles = static_cast<unsigned char*>(workspace) +
+                rounded(attention_rows_workspace(a.n, a.q_heads, a.kv_heads, a.dim, a.max_q,
+                                                 a.max_len));
+  if (together(a))
+    return launch_attention_tiles(a, kRowsMost + 1, few, tiles, stream);
+  const int rc = launch_attention_rows(a, few, stream);
   if (rc != PAIR_OK) return rc;
-  const size_t rows = rounded(
-      attention_rows_workspace(a.n, a.q_heads, a.kv_heads, a.dim, a.max_q, a.max_len));
-  return launch_attention_tiles(a, kRowsMost + 1, static_cast<unsigned char*>(workspace) + rows,
-                                stream);
+  return launch_attention_tiles(a, kRowsMost + 1, nullptr, tiles, stream);
 }
 
 }  // namespace pair

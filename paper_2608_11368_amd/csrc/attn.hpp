@@ -108,7 +108,8 @@ __device__ __forceinline__ int32_t checked_page(const AttnCall& a, int32_t id, i
 }
 
 // The launches of attn_rows.hip (requests of at most kRowsMost rows, a row being
-// a query head of a token) and attn_tiles.hip (the others, or all).
+// a query head of a token) and attn_tiles.hip (those of at least `least_rows`;
+// with a workspace for the others, both).
 constexpr int kRowsMost = 32;
 
 size_t attention_rows_workspace(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim,
@@ -116,7 +117,7 @@ size_t attention_rows_workspace(int64_t n, int32_t q_heads, int32_t kv_heads, in
 int launch_attention_rows(const AttnCall& a, void* workspace, hipStream_t stream);
 size_t attention_tiles_workspace(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads,
                                  int32_t dim, int32_t max_len);
-int launch_attention_tiles(const AttnCall& a, int32_t least_rows, void* workspace,
-                           hipStream_t stream);
+int launch_attention_tiles(const AttnCall& a, int32_t least_rows, void* few_workspace,
+                           void* workspace, hipStream_t stream);
 
 }  // namespace pair

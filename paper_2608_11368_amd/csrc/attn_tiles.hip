@@ -15,7 +15,7 @@
 // LDS rows are stored with their 16-byte pieces permuted by the row number, so
 // that neither the reads of K (32 rows at one place) nor those of V (four rows
 // at two neighbouring places) meet in a bank.
-// The maximum is raised only when a score exceeds it by 2^8 (attn_rows.hip does
+// The maximum is raised only when a score exceeds it by 2^8 (attn_rows.hpp does
 // the same), and steps that every row of a wave sees whole skip the masks.
 //
 // When the tiles are too few for the card, each tile's keys are split and a
@@ -37,7 +37,7 @@
 // which four stay.
 #include <type_traits>
 
-#include "attn.hpp"
+#include "attn_rows.hpp"
 
 namespace pair {
 
@@ -149,7 +149,7 @@ __device__ __forceinline__ bool find_ordered(const TileArgs& s, int64_t at, Requ
       if (rows >= s.least) tiles[i] = (rows + kRows - 1) / kRows;
     }
   }
-  if (bad && blockIdx.x == 0 && threadIdx.x < kWave) raise_status(s.a.d_status, bad);
+  if (bad && at == 0 && threadIdx.x < kWave) raise_status(s.a.d_status, bad);
   const int steps = (s.a.max_len + kKeys - 1) / kKeys;
   const int each = (steps + kClasses - 1) / kClasses;
   // tiles of set i's request of class c or a longer one (class 0: of any length)
@@ -274,8 +274,11 @@ __device__ __forceinline__ void add_odd_step(unsigned char* keys, unsigned char*
   __syncthreads();
 }
 
+// One workgroup's tile, `block` its place in the order.
 template <bool BF16, int DIM, bool ALIGNED>
-__global__ __launch_bounds__(kThreads, DIM == 64 ? 3 : 2) void attention_tiles_kernel(TileArgs s) {
+__device__ __forceinline__ void attend_tile(const TileArgs& s, uint32_t block,
+                                            unsigned char (&kt)[2][kKeys * DIM * 2],
+                                            unsigned char (&vt)[2][kKeys * DIM * 2]) {
   constexpr int NC = DIM / 16;              // k pieces of a score product
   constexpr int ND = DIM / 32;              // dim tiles of the output
   constexpr int kPer = DIM / 8;             // 16-byte pieces of a row
@@ -283,14 +286,12 @@ __global__ __launch_bounds__(kThreads, DIM == 64 ? 3 : 2) void attention_tiles_k
   constexpr int kStep = kThreads / kPer;    // rows between a lane's pieces
   // add_odd_step lays 16 KiB of weights over both key steps
   static_assert(kRows * kKeys * 2 <= 2 * kKeys * DIM * 2, "weights of a step");
-  __shared__ __align__(16) unsigned char kt[2][kKeys * DIM * 2];
-  __shared__ __align__(16) unsigned char vt[2][kKeys * DIM * 2];
 
   // heads fastest: consecutive workgroups go to the XCDs in turn, so that with
   // 8 (4, 2) key heads each XCD's cache holds one (two, four) of them
   const uint32_t heads = (uint32_t)s.a.kv_heads, splits = (uint32_t)s.splits;
-  const uint32_t of_heads = blockIdx.x / heads;   // 32 bits: a long division takes 0.3 us
-  const int kvh = (int)(blockIdx.x - of_heads * heads);
+  const uint32_t of_heads = block / heads;   // 32 bits: a long division takes 0.3 us
+  const int kvh = (int)(block - of_heads * heads);
   const int split = (int)(of_heads % splits);
   int64_t r;
   int tile;
@@ -579,6 +580,62 @@ __global__ __launch_bounds__(kThreads, DIM == 64 ? 3 : 2) void attention_tiles_k
     s.a.lse[row] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718056f;
 }
 
+template <bool BF16, int DIM, bool ALIGNED>
+__global__ __launch_bounds__(kThreads, DIM == 64 ? 3 : 2) void attention_tiles_kernel(TileArgs s) {
+  __shared__ __align__(16) unsigned char kt[2][kKeys * DIM * 2];   // a step's keys, twice
+  __shared__ __align__(16) unsigned char vt[2][kKeys * DIM * 2];
+  attend_tile<BF16, DIM, ALIGNED>(s, blockIdx.x, kt, vt);
+}
+
+// What a call's requests of few rows add to the arguments.
+struct FewArgs {
+  int32_t runs;
+  int32_t* starts;
+  float* part_o;
+  float* part_ml;
+};
+
+// A call that may hold requests of few rows, too: `few` workgroups for those and
+// `tiles` for the others, the first kDealt of each in turn, so that the reading of
+// a long cache and the products run on a compute unit at the same time.
+constexpr uint32_t kDealt = 256;
+
+template <bool BF16, int DIM, bool ALIGNED>
+__global__ __launch_bounds__(kThreads, 2) void attention_mixed_kernel(TileArgs s, FewArgs w,
+                                                                      uint32_t few, uint32_t tiles) {
+  struct FewLds {
+    rows::WaveLds<DIM, 2> wave[rows::kWaves];
+    int32_t start[rows::kMostScanned + 1];
+    int32_t sums[rows::kWaves];
+  };
+  struct StepLds {
+    unsigned char k[2][kKeys * DIM * 2], v[2][kKeys * DIM * 2];
+  };
+  __shared__ __align__(16) union {
+    FewLds few;
+    StepLds step;
+  } lds;
+  const uint32_t b = blockIdx.x;
+  const uint32_t few_first = few < kDealt ? few : kDealt;
+  const uint32_t first = few_first + (tiles < kDealt ? tiles : kDealt);
+  if (b >= few_first && (b < first || b >= first + few - few_first)) {
+    attend_tile<BF16, DIM, ALIGNED>(s, b < first ? b - few_first : b - few, lds.step.k,
+                                    lds.step.v);
+  } else {
+    rows::RowArgs f;
+    f.a = s.a;
+    f.page = s.page;
+    f.group = s.group;
+    f.scale_log2 = s.scale_log2;
+    f.runs = w.runs;
+    f.starts = w.starts;
+    f.part_o = w.part_o;
+    f.part_ml = w.part_ml;
+    rows::serve<BF16, DIM, 2, ALIGNED, rows::kWaves>(
+        f, b < few_first ? b : b - first + few_first, lds.few.wave, lds.few.start, lds.few.sums);
+  }
+}
+
 // Joins a row's parts: one wave a row.
 template <bool BF16, int DIM>
 __global__ __launch_bounds__(kThreads) void join_tiles_kernel(TileArgs s) {
@@ -654,22 +711,37 @@ Plan plan_tiles(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads, in
   return p;
 }
 
+// `w` (or null): the requests of few rows, served by the same launch.
 template <bool BF16, int DIM>
-int launch(const TileArgs& s, const Plan& p, hipStream_t stream) {
+int launch(const TileArgs& s, const Plan& p, const rows::RowArgs* w, const rows::Plan* wp,
+           hipStream_t stream) {
   const int64_t grid = p.tiles * s.a.kv_heads * p.splits;
-  if (grid > 0x7fffffffLL) return PAIR_ERANGE;
+  const int64_t few = w != nullptr ? rows::groups_of(s.a, *wp) : 0;
+  if (grid + few > 0x7fffffffLL || s.a.n * s.a.kv_heads > 0x7fffffffLL) return PAIR_ERANGE;
   if (s.a.n > kInline) {
     hipLaunchKernelGGL(tile_starts_kernel, dim3(1), dim3(1024), 0, stream, s);
     if (hipGetLastError() != hipSuccess) return PAIR_EHIP;
   }
   // 16 slots within 32 bits of offset: any sensible layout
-  if (s.page.d % 16 == 0 && s.a.cache.slot_stride < ((int64_t)1 << 26))
-    hipLaunchKernelGGL((attention_tiles_kernel<BF16, DIM, true>), dim3((unsigned)grid),
-                       dim3(kThreads), 0, stream, s);
-  else
-    hipLaunchKernelGGL((attention_tiles_kernel<BF16, DIM, false>), dim3((unsigned)grid),
-                       dim3(kThreads), 0, stream, s);
+  const bool aligned = s.page.d % 16 == 0 && s.a.cache.slot_stride < ((int64_t)1 << 26);
+#define PAIR_TILES(AL)                                                                           \
+  do {                                                                                           \
+    if (w != nullptr)                                                                            \
+      hipLaunchKernelGGL((attention_mixed_kernel<BF16, DIM, AL>), dim3((unsigned)(grid + few)),   \
+                         dim3(kThreads), 0, stream, s,                                            \
+                         (FewArgs{w->runs, w->starts, w->part_o, w->part_ml}), (uint32_t)few,    \
+                         (uint32_t)grid);                                                        \
+    else                                                                                         \
+      hipLaunchKernelGGL((attention_tiles_kernel<BF16, DIM, AL>), dim3((unsigned)grid),           \
+                         dim3(kThreads), 0, stream, s);                                          \
+  } while (0)
+  if (aligned) PAIR_TILES(true); else PAIR_TILES(false);
+#undef PAIR_TILES
   if (hipGetLastError() != hipSuccess) return PAIR_EHIP;
+  if (w != nullptr) {
+    const int rc = rows::join_rows(*w, *wp, stream);
+    if (rc != PAIR_OK) return rc;
+  }
   if (p.splits > 1) {
     const int64_t rows = s.a.tokens * s.a.q_heads;
     hipLaunchKernelGGL((join_tiles_kernel<BF16, DIM>), dim3((unsigned)((rows + kWaves - 1) / kWaves)),
@@ -685,8 +757,8 @@ size_t attention_tiles_workspace(int64_t n, int64_t tokens, int32_t q_heads, int
   return plan_tiles(n, tokens, q_heads, kv_heads, dim, max_len).total;
 }
 
-int launch_attention_tiles(const AttnCall& a, int32_t least_rows, void* workspace,
-                           hipStream_t stream) {
+int launch_attention_tiles(const AttnCall& a, int32_t least_rows, void* few_workspace,
+                           void* workspace, hipStream_t stream) {
   const Plan p = plan_tiles(a.n, a.tokens, a.q_heads, a.kv_heads, a.dim, a.max_len);
   TileArgs s;
   s.a = a;
@@ -699,8 +771,18 @@ int launch_attention_tiles(const AttnCall& a, int32_t least_rows, void* workspac
   s.starts = reinterpret_cast<int32_t*>(ws);
   s.part_ml = reinterpret_cast<float*>(ws + p.starts);
   s.part_o = reinterpret_cast<float*>(ws + p.starts + p.ml);
-  if (a.dim == 64) return a.bf16 ? launch<true, 64>(s, p, stream) : launch<false, 64>(s, p, stream);
-  return a.bf16 ? launch<true, 128>(s, p, stream) : launch<false, 128>(s, p, stream);
+  rows::RowArgs w;
+  rows::Plan wp;
+  if (few_workspace != nullptr) {
+    wp = rows::plan_of(a.n, a.q_heads, a.kv_heads, a.dim, a.max_q, a.max_len);
+    w = rows::args_of(a, wp, few_workspace);
+  }
+  const rows::RowArgs* few = few_workspace != nullptr ? &w : nullptr;
+  if (a.dim == 64)
+    return a.bf16 ? launch<true, 64>(s, p, few, &wp, stream)
+                  : launch<false, 64>(s, p, few, &wp, stream);
+  return a.bf16 ? launch<true, 128>(s, p, few, &wp, stream)
+                : launch<false, 128>(s, p, few, &wp, stream);
 }
 
 }  // namespace pair

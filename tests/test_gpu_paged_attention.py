@@ -298,6 +298,21 @@ def test_many_requests(n, case):
     c.check(c.call(), only=[0, 3, 5, 7, 8, 9, 63, 64, 65, n // 2, n - 2, n - 1])
 
 
+@pytest.mark.parametrize("page", [16, 20])
+@pytest.mark.parametrize("dim,dtype", [(64, "bf16"), (128, "f16")])
+@pytest.mark.parametrize("new,past,only", [
+    ([320] * 6 + [1, 7], 30, [1, 6, 7]),           # many tiles: two launches
+    ([1, 90, 0, 8, 1, 9, 1, 1], 400, None),        # few tiles: one, side by side
+    ([1] * 40 + [130] + [2] * 20, 1300, [0, 39, 40, 41, 60]),
+])
+def test_chunks_beside_few(new, past, only, dim, dtype, page):
+    log(f"paged attention: new {new[:8]} over {past}, width {dim}, pages of {page}")
+    lens = np.array([past + x + 37 * (i % 5) for i, x in enumerate(new)])
+    c = Cache(lens, new, 32 if len(new) == 8 else 16, 8 if len(new) == 8 else 4, dim, page, dtype,
+              seed=dim + page)
+    c.check(c.call(), only=only)
+
+
 @pytest.mark.parametrize("n,most", [(3, 1024), (3, 1025), (140, 1024), (140, 1025)])
 @pytest.mark.parametrize("page", [16, 20])
 def test_short_requests_around_the_cut(n, most, page):
