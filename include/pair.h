@@ -575,7 +575,8 @@ size_t pair_page_plan_workspace_bytes(int64_t n);
  *   free_count   int64 [1] in (device)
  *   max_tokens   entries of slots and positions (>= the new tokens; < 2^31)
  *   q_offsets    int64 [n+1] out: first new token of each request, packed
- *   lens         int32 [n] out: cached + fresh, 0 for a released request
+ *   lens         int32 [n] out: cached + fresh, 0 for a released request; what
+ *                its pages hold where the pool ran out on a request
  *   slots        int64 [max_tokens] out: slot of each new token, -1 past the last
  *   positions    int32 [max_tokens] out: position of each, -1 past the last (or NULL)
  *   free_out     int32 [capacity] out: the new list, -1 past its end
@@ -584,7 +585,9 @@ size_t pair_page_plan_workspace_bytes(int64_t n);
  *   workspace    device scratch, 256-byte aligned
  * A request whose lengths are negative or whose table row is too narrow is
  * left out (no token, no page, length 0); tokens that the pool has no page for
- * get slot -1 and table entry -1.
+ * get slot -1 and table entry -1, and lens ends before them, so that the request
+ * can be released, or go on later, with the length that it got.  A negative
+ * entry of the pool is handed on as it is and sets PAIR_ST_PAGES.
  * Device status: PAIR_ST_PAGES, PAIR_ST_LENGTH.
  */
 int pair_page_plan(int64_t n, const int32_t* cached, const int32_t* fresh, const uint8_t* mask,

@@ -325,11 +325,21 @@ __device__ __forceinline__ void plan_outputs(const PlanArgs& a, const Ends& e,
 #pragma unroll
   for (int s = 0; s < kOwn; ++s)
     if (inside[s]) a.free_out[j[s]] = id[s];
+  // A negative entry among those of the pool (a list or a released row that holds
+  // one) is no page.
+  bool hole = false;
+#pragma unroll
+  for (int s = 0; s < kOwn; ++s) hole |= inside[s] && left[s] < avail && id[s] < 0;
+  if (hole) raise_status(a.d_status, PAIR_ST_PAGES);
   if (first >= used) return;
   find(takers, j, r, start);
 #pragma unroll
   for (int s = 0; s < kOwn; ++s) from[s] = nullptr;
   pool_entries(givers, taken, from, j, id);
+  hole = false;
+#pragma unroll
+  for (int s = 0; s < kOwn; ++s) hole |= taken[s] && id[s] < 0;
+  if (hole) raise_status(a.d_status, PAIR_ST_PAGES);
 #pragma unroll
   for (int s = 0; s < kOwn; ++s)
     if (taken[s])
@@ -337,8 +347,9 @@ __device__ __forceinline__ void plan_outputs(const PlanArgs& a, const Ends& e,
               (j[s] - start[s])] = id[s];
 }
 
-// Table entries that the pool has no page for become -1, and what does not fit
-// is reported; thread `i` of `step` of one workgroup.
+// Table entries that the pool has no page for become -1, their requests' lengths
+// end with the pages that they got, and what does not fit is reported; by the
+// threads of one workgroup, after the lengths are written.
 __device__ void plan_totals(const PlanArgs& a, const Ends& e, const Counts& total) {
   const uint32_t free = free_pages_of(a);
   const uint32_t avail = sat_add(free, total.given);
@@ -354,7 +365,11 @@ __device__ void plan_totals(const PlanArgs& a, const Ends& e, const Counts& tota
     for (uint32_t j = used + threadIdx.x; j < total.taken; j += blockDim.x) {
       const int r = owner(e.taken, j, 0, last);
       const uint32_t held = pages_of((uint32_t)a.cached[r], a.page);
-      a.table[(int64_t)r * a.ldt + held + j - (r > 0 ? e.taken[r - 1] : 0u)] = -1;
+      const uint32_t start = r > 0 ? e.taken[r - 1] : 0u;
+      a.table[(int64_t)r * a.ldt + held + j - start] = -1;
+      // The request's first entry without a page: the ones before it are full.
+      // A length beyond them would count the -1 as pages when it is released.
+      if (j == used || j == start) a.lens[r] = (int32_t)((held + j - start) * a.page.d);
     }
   }
 }

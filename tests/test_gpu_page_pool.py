@@ -1,0 +1,133 @@
+"""The page pool over several steps: a pool that runs out, the recovery from it,
+and lists that hold what is no page.  Whole numbers, equal to the last bit."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_11368_amd as pair
+from tests.gpu_util import DEV, log
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _device():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    pair.lib()
+    yield
+    torch.cuda.synchronize()
+
+
+def i32(x):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).to(DEV)
+
+
+def count(x):
+    return torch.tensor([x], dtype=torch.int64, device=DEV)
+
+
+def listed(r):
+    return r["free_pages"][:int(r["free_count"].item())].tolist()
+
+
+@pytest.mark.parametrize("n", [4, 70, 2048, 2049, 5000])
+@pytest.mark.parametrize("cached,fresh,short", [(8, 16, 1), (16, 1, 1), (0, 40, 5), (20, 13, 3)])
+def test_what_ran_short_can_be_released(n, cached, fresh, short):
+    """The pool lacks `short` pages: the requests at the end keep the lengths that
+    their pages hold, and when they are released with those, each page returns to
+    the list once and nothing else does."""
+    log(f"page pool: {short} pages short, n={n}, {fresh} after {cached}")
+    page = 16
+    held, need = -(-cached // page), -(-(cached + fresh) // page)
+    ids = np.random.default_rng(n).permutation(n * need).astype(np.int32)
+    table = np.full((n, need), -1, dtype=np.int32)
+    table[:, :held] = ids[:n * held].reshape(n, held)
+    free = np.full(n * need, -1, dtype=np.int32)
+    pool = n * (need - held) - short
+    free[:pool] = ids[n * held:n * held + pool]
+    tab = i32(table)
+    a = pair.page_plan(i32([cached] * n), i32([fresh] * n), tab, i32(free), count(pool), page,
+                       n * fresh)
+    torch.cuda.synchronize()
+    assert int(a["status"].item()) == pair.ST_PAGES and listed(a) == []
+    got = np.full(n, need - held)              # new pages: in request order until the last
+    for r in range(n - 1, -1, -1):
+        lack = min(short, got[r])
+        got[r] -= lack
+        short -= lack
+    want = np.minimum(cached + fresh, (held + got) * page)
+    assert np.array_equal(a["lens"].cpu().numpy(), want)
+    rows = tab.cpu().numpy()
+    has = np.arange(need)[None, :] < (held + got)[:, None]
+    assert np.all(rows[~has] == -1)
+    assert sorted(rows[has].tolist()) == sorted(ids[:n * held + pool].tolist())
+    # the tokens with a slot are those below the length
+    slots = a["slots"].cpu().numpy().reshape(n, fresh)
+    below = cached + np.arange(fresh)[None, :] < want[:, None]
+    assert np.array_equal(slots >= 0, below)
+    # release the ones that ran short, then everyone
+    mask = (got == need - held).astype(np.uint8)
+    b = pair.page_plan(a["lens"], i32([0] * n), tab, a["free_pages"], a["free_count"], page, 1,
+                       mask=torch.from_numpy(mask).to(DEV))
+    torch.cuda.synchronize()
+    assert int(b["status"].item()) == 0
+    assert listed(b) == [p for r in np.flatnonzero(mask == 0) for p in rows[r, :held + got[r]]]
+    c = pair.page_plan(b["lens"], i32([0] * n), tab, b["free_pages"], b["free_count"], page, 1,
+                       mask=torch.zeros(n, dtype=torch.uint8, device=DEV))
+    torch.cuda.synchronize()
+    assert int(c["status"].item()) == 0
+    assert sorted(listed(c)) == sorted(ids[:n * held + pool].tolist())
+
+
+@pytest.mark.parametrize("n", [3, 2100])
+def test_what_ran_short_can_go_on(n):
+    """The last request gets its missing tokens a step later, from released pages."""
+    log(f"page pool: short, then served, n={n}")
+    page = 16
+    table = np.full((n, 3), -1, dtype=np.int32)
+    table[:, 0] = np.arange(n)
+    tab, free = i32(table), np.full(2 * n, -1, dtype=np.int32)
+    free[:n - 1] = np.arange(n, 2 * n - 1)
+    a = pair.page_plan(i32([8] * n), i32([16] * n), tab, i32(free), count(n - 1), page, 16 * n)
+    mask = torch.ones(n, dtype=torch.uint8, device=DEV)
+    mask[0] = 0
+    fresh = np.zeros(n, dtype=np.int32)
+    fresh[-1] = 8
+    b = pair.page_plan(a["lens"], i32(fresh), tab, a["free_pages"], a["free_count"], page, 8,
+                       mask=mask)
+    torch.cuda.synchronize()
+    assert int(a["lens"][-1].item()) == 16 and int(b["status"].item()) == 0
+    assert b["slots"].tolist() == [0 * page + x for x in range(8)]      # request 0's first page
+    assert b["positions"].tolist() == list(range(16, 24))
+    assert int(b["lens"][-1].item()) == 24 and listed(b) == [n]
+
+
+@pytest.mark.parametrize("n", [2, 2100])
+def test_an_entry_that_is_no_page(n):
+    """A negative entry of the list or of a released row sets the status, whether
+    a request gets it or it stays listed; the others keep what is theirs."""
+    log(f"page pool: negative entries, n={n}")
+    page, cap = 16, 2 * n + 4
+    for taken in (True, False):
+        for released in (True, False):
+            table = np.full((n, 2), -1, dtype=np.int32)
+            cached, fresh = np.zeros(n), np.zeros(n)
+            mask = np.ones(n, dtype=np.uint8)
+            free = np.full(cap, -1, dtype=np.int32)
+            if released:
+                cached[0], mask[0] = 20, 0
+                table[0] = [5, -1]
+                pool = [5, -1]
+                left = 0
+            else:
+                free[:3], left = [7, -4, 9], 3
+                pool = [7, -4, 9]
+            fresh[-1] = 32 if taken else 0
+            r = pair.page_plan(i32(cached), i32(fresh), i32(table), i32(free), count(left), page, 32,
+                               mask=torch.from_numpy(mask).to(DEV))
+            torch.cuda.synchronize()
+            assert int(r["status"].item()) == pair.ST_PAGES, (taken, released)
+            assert listed(r) == (pool[2:] if taken else pool)
+            if taken:
+                assert r["slots"].tolist() == [pool[0] * page + x for x in range(16)] + [-1] * 16
