@@ -572,7 +572,8 @@ size_t pair_page_plan_workspace_bytes(int64_t n);
  *   table        int32 [n][ldt] in/out: entries h_r .. h_r + m_r - 1 are written
  *   capacity     entries of free_pages and free_out (the pool's page count)
  *   free_pages   int32 [capacity] in: the first *free_count are free
- *   free_count   int64 [1] in (device)
+ *   free_count   int64 [1] in (device); one outside 0 .. capacity sets
+ *                PAIR_ST_PAGES and counts as the nearer of the two
  *   max_tokens   entries of slots and positions (>= the new tokens; < 2^31)
  *   q_offsets    int64 [n+1] out: first new token of each request, packed
  *   lens         int32 [n] out: cached + fresh, 0 for a released request; what

@@ -357,7 +357,9 @@ __device__ void plan_totals(const PlanArgs& a, const Ends& e, const Counts& tota
   if (threadIdx.x == 0) {
     const uint32_t left = avail - used;
     *a.free_count_out = left < (uint32_t)a.capacity ? left : (uint32_t)a.capacity;
-    if (total.taken > avail || left > (uint32_t)a.capacity) raise_status(a.d_status, PAIR_ST_PAGES);
+    const int64_t counted = *a.free_count;
+    if (total.taken > avail || left > (uint32_t)a.capacity || counted < 0 || counted > a.capacity)
+      raise_status(a.d_status, PAIR_ST_PAGES);
     if (total.tokens > (uint32_t)a.max_tokens) raise_status(a.d_status, PAIR_ST_LENGTH);
   }
   if (total.taken > used) {

@@ -131,3 +131,23 @@ def test_an_entry_that_is_no_page(n):
             assert listed(r) == (pool[2:] if taken else pool)
             if taken:
                 assert r["slots"].tolist() == [pool[0] * page + x for x in range(16)] + [-1] * 16
+
+
+@pytest.mark.parametrize("n", [1, 2100])
+def test_a_count_that_the_list_does_not_hold(n):
+    """A free count below zero or beyond the list sets the status; the plan then
+    takes the list as empty or full."""
+    log(f"page pool: counts outside the list, n={n}")
+    cap = n + 3
+    for given, taken in ((-1, 0), (cap + 1, cap), (2 ** 40, cap)):
+        table = torch.full((n, 2), -1, dtype=torch.int32, device=DEV)
+        r = pair.page_plan(i32([0] * n), i32([1] * n), table, i32(np.arange(cap)), count(given), 16, n)
+        torch.cuda.synchronize()
+        assert int(r["status"].item()) == pair.ST_PAGES, given
+        assert listed(r) == list(range(n, taken))
+        assert r["slots"].tolist() == ([x * 16 for x in range(n)] if taken else [-1] * n)
+    for fine in (n, cap):
+        table = torch.full((n, 2), -1, dtype=torch.int32, device=DEV)
+        r = pair.page_plan(i32([0] * n), i32([1] * n), table, i32(np.arange(cap)), count(fine), 16, n)
+        torch.cuda.synchronize()
+        assert int(r["status"].item()) == 0 and listed(r) == list(range(n, fine))
