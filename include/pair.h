@@ -45,7 +45,8 @@ extern "C" {
 
 /* Return codes. */
 #define PAIR_OK 0
-#define PAIR_EINVAL (-1)     /* null pointer or malformed size                 */
+#define PAIR_EINVAL (-1)     /* null pointer, malformed size, or arrays that
+                                overlap where the call says they may not       */
 #define PAIR_EDTYPE (-2)     /* a dtype that the call does not take             */
 #define PAIR_ERANGE (-3)     /* gmax outside [2, 64], D < 1, R < 1, ld < D ...  */
 #define PAIR_EALIGN (-4)     /* scores, caches or rows: a base or stride not
@@ -581,9 +582,10 @@ size_t pair_page_plan_workspace_bytes(int64_t n);
  *   slots        int64 [max_tokens] out: slot of each new token, -1 past the last
  *   positions    int32 [max_tokens] out: position of each, -1 past the last (or NULL)
  *   free_out     int32 [capacity] out: the new list, -1 past its end
- *                (not overlapping free_pages)
  *   free_count_out int64 [1] out
  *   workspace    device scratch, 256-byte aligned
+ * No output may overlap an input or another output (PAIR_EINVAL): lens is not
+ * cached, free_count_out not free_count; only table is read and written.
  * A request whose lengths are negative or whose table row is too narrow is
  * left out (no token, no page, length 0); tokens that the pool has no page for
  * get slot -1 and table entry -1, and lens ends before them, so that the request

@@ -338,6 +338,18 @@ int pair_clip_grads(int64_t count, const void* const* grads, void* const* outs,
                            workspace, d_status, as_stream(stream));
 }
 
+// A caller's array, as the checks of overlaps see it.
+struct Extent {
+  const void* at;
+  int64_t bytes;
+};
+
+static bool overlap(const Extent& a, const Extent& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+  return a.at != nullptr && b.at != nullptr && a.bytes > 0 && b.bytes > 0 &&
+         x < y + (uint64_t)b.bytes && y < x + (uint64_t)a.bytes;
+}
+
 size_t pair_page_plan_workspace_bytes(int64_t n) {
   return n < 1 || n > kMaxRequests ? 0 : pair::page_plan_workspace_bytes(n);
 }
@@ -359,6 +371,21 @@ int pair_page_plan(int64_t n, const int32_t* cached, const int32_t* fresh, const
   if (max_tokens > 0 && slots == nullptr) return PAIR_EINVAL;
   if (bad_workspace(workspace, ws_bytes, pair::page_plan_workspace_bytes(n)))
     return PAIR_EWORKSPACE;
+  // Every workgroup reads all lengths and the pool while others write.
+  const Extent in[] = {{cached, n * 4}, {fresh, n * 4}, {mask, n}, {free_pages, capacity * 4},
+                       {free_count, 8}};
+  const Extent out[] = {{table, n * ldt * 4},   {q_offsets, (n + 1) * 8},
+                        {lens, n * 4},          {slots, max_tokens * 8},
+                        {positions, max_tokens * 4}, {free_out, capacity * 4},
+                        {free_count_out, 8},    {workspace, (int64_t)pair::page_plan_workspace_bytes(n)},
+                        {d_status, 4}};
+  constexpr int kOuts = sizeof(out) / sizeof(out[0]);
+  for (int i = 0; i < kOuts; ++i) {
+    for (const Extent& e : in)
+      if (overlap(out[i], e)) return PAIR_EINVAL;
+    for (int k = 0; k < i; ++k)
+      if (overlap(out[i], out[k])) return PAIR_EINVAL;
+  }
   return pair::launch_page_plan(n, cached, fresh, mask, page, table, ldt, capacity, free_pages,
                                 free_count, max_tokens, q_offsets, lens, slots, positions,
                                 free_out, free_count_out, workspace, d_status, as_stream(stream));
@@ -479,7 +506,7 @@ int pair_paged_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_
 const char* pair_strerror(int code) {
   switch (code) {
     case PAIR_OK: return "ok";
-    case PAIR_EINVAL: return "invalid argument (null pointer or malformed size)";
+    case PAIR_EINVAL: return "invalid argument (null pointer, malformed size or overlapping arrays)";
     case PAIR_EDTYPE: return "unsupported dtype";
     case PAIR_ERANGE: return "size out of the supported range";
     case PAIR_EALIGN: return "base pointer or row stride misaligned (16 bytes; gradients: an element)";
