@@ -636,7 +636,8 @@ size_t pair_paged_attention_workspace_bytes(int64_t n, int64_t tokens, int32_t q
  * A token that sees no key gets out = 0 and lse = -inf.  What a key or value
  * that a token does not see holds, NaN and infinities among it, has no
  * effect on that token.  Scores, statistics and sums are fp32; exp(s_j - m)
- * is rounded to the type of v for the matrix cores.
+ * is rounded to the type of v for the matrix cores (fp16: those below 2^-21 of
+ * the largest to a multiple of 2^-31 of it).
  *
  *   n, tokens    requests, and rows of q and out
  *   q_heads      a multiple of kv_heads, at most 64 * kv_heads

@@ -48,6 +48,24 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2_t));
 }
 
+// The matrix cores take the softmax's weights in the type of the values, so they
+// are rounded to it (their sum l is of the unrounded ones, in fp32): relative to
+// 64 bits that makes outputs 1.4 times as far off as rounding them alone does.
+// fp16 has no room for small weights below the running maximum's 1: from 2^-14
+// they lose bits and below 2^-25 they would vanish from the output while l still
+// counts them.  The maximum may lag by 2^8 and fp16 ends at 2^16, so all weights
+// are lifted by 2^7, l with them: they keep their bits down to 2^-21 and an
+// error of 2^-32 below.
+template <bool BF16>
+constexpr float kLift = BF16 ? 0.0f : 7.0f;   // log2
+
+// log of the sum of exp(score) from the running maximum and the lifted sum, both
+// of powers of two.
+template <bool BF16>
+__device__ __forceinline__ float log_sum(float m, float l) {
+  return (m - kLift<BF16> + __builtin_amdgcn_logf(l)) * 0.69314718056f;
+}
+
 template <bool BF16>
 __device__ __forceinline__ float half_value(uint32_t bits) {   // of the low 16 bits
   return BF16 ? __uint_as_float(bits << 16)

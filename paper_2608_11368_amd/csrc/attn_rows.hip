@@ -88,7 +88,7 @@ __global__ __launch_bounds__(kThreads) void join_rows_kernel(RowArgs s, int rows
                                h * s.a.out_head + d) = none ? 0u : pack2<BF16>(a * inv, b * inv);
   if (s.a.lse != nullptr && threadIdx.x == 0)
     s.a.lse[(q.q0 + tok) * s.a.q_heads + h] =
-        none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718056f;
+        none ? -INFINITY : log_sum<BF16>(m, l);
 }
 
 template <bool BF16, int DIM>

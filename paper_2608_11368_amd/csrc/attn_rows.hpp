@@ -278,7 +278,7 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
 #pragma unroll
         for (int j = 0; j < ND; ++j) st->acc[nt][j] *= keep;
       }
-      const float base = st->m[nt] == -INFINITY ? 0.0f : st->m[nt];
+      const float base = (st->m[nt] == -INFINITY ? 0.0f : st->m[nt]) - kLift<BF16>;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         p[nt][e] = __builtin_amdgcn_exp2f(p[nt][e] - base);
@@ -414,7 +414,7 @@ __device__ __forceinline__ void attend(const RowArgs& s, int64_t r, int kvh, int
                                       (q.q0 + tok) * s.a.out_token + h * s.a.out_head + d) = w;
           if (s.a.lse != nullptr && d == 0)
             s.a.lse[(q.q0 + tok) * s.a.q_heads + h] =
-                none ? -INFINITY : (m + __builtin_amdgcn_logf(tot)) * 0.69314718056f;
+                none ? -INFINITY : log_sum<BF16>(m, tot);
         }
       }
     }

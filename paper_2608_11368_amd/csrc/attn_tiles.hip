@@ -488,7 +488,7 @@ __device__ __forceinline__ void attend_tile(const TileArgs& s, uint32_t block,
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[d][e] *= keep;
     }
-    const float base = m == -INFINITY ? 0.0f : m;
+    const float base = (m == -INFINITY ? 0.0f : m) - kLift<BF16>;
     u32x4_t pf[4];
     float part = 0.0f;
 #pragma unroll
@@ -577,7 +577,7 @@ __device__ __forceinline__ void attend_tile(const TileArgs& s, uint32_t block,
       *reinterpret_cast<u32x2_t*>(o + 32 * d + 8 * b + 4 * h) = w;
     }
   if (s.a.lse != nullptr && h == 0)
-    s.a.lse[row] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718056f;
+    s.a.lse[row] = none ? -INFINITY : log_sum<BF16>(m, l);
 }
 
 template <bool BF16, int DIM, bool ALIGNED>
@@ -683,7 +683,7 @@ __global__ __launch_bounds__(kThreads) void join_tiles_kernel(TileArgs s) {
     to[lane] = none ? (uint16_t)0 : (uint16_t)pack2<BF16>(o[0] * inv, 0.0f);
   }
   if (s.a.lse != nullptr && lane == 0)
-    s.a.lse[row] = none ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718056f;
+    s.a.lse[row] = none ? -INFINITY : log_sum<BF16>(m, l);
 }
 
 struct Plan {
