@@ -756,12 +756,14 @@ def _status(device):
     if torch.cuda.is_current_stream_capturing():
         return torch.zeros(1, dtype=torch.int32, device=device)
     key = (device, _stream(None))
-    words = _status_words.get(key)
-    if not words:
+    try:
+        return _status_words[key].pop()        # one step: threads may share a stream
+    except (KeyError, IndexError):
         with torch.inference_mode(False):
             words = list(torch.zeros(256, dtype=torch.int32, device=device).split(1))
+        word = words.pop()
         _status_words[key] = words
-    return words.pop()
+        return word
 
 
 @functools.lru_cache(maxsize=256)
