@@ -767,7 +767,8 @@ def _status(device):
 
 
 @functools.lru_cache(maxsize=256)
-def _attention_workspace(*sizes):
+def _attention_workspace(device, *sizes):
+    """`device`: the size follows the current device's compute units."""
     return pair_paged_attention_workspace_bytes(*sizes)
 
 
@@ -814,7 +815,9 @@ def paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max_len,
         out, = parts(index, q.dtype, (tokens, heads, dim))
     if want_lse:
         lse, = parts(index, torch.float32, (tokens, heads))
-    need = _attention_workspace(lens.numel(), tokens, heads, k_cache.shape[2], dim, max_q, max_len)
+    max_q, max_len = int(max_q), int(max_len)
+    need = _attention_workspace(_device_index(), lens.numel(), tokens, heads, k_cache.shape[2], dim,
+                                max_q, max_len)
     if workspace is None or workspace.numel() < need:
         workspace, = parts(index, torch.uint8, need)
     st = _status(q.device)
