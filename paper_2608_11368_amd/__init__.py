@@ -780,7 +780,9 @@ def page_plan(cached, fresh, table, free_pages, free_count, page, max_tokens, ma
     others' pages return to the pool.  `table` int32 [n][entries] is updated in
     place; `free_pages` int32 lists the pool's pages, the first `free_count`
     (int64 [1], on the GPU) of them free, and the new list and count come back
-    as `free_pages` and `free_count`.  `max_tokens` bounds the new tokens."""
+    as `free_pages` and `free_count`.  `max_tokens` bounds the new tokens.  The
+    outputs and the workspace are parts of one allocation and share a storage:
+    any of them keeps, and a saved one stores, all of it (clone what is to last)."""
     n, cap = cached.numel(), free_pages.numel()
     ws, lens, positions, new_free, q_offsets, slots, new_count = _native().parts(
         cached.get_device(), torch.uint8, pair_page_plan_workspace_bytes(n), torch.int32, n,
@@ -830,7 +832,8 @@ def paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max_len,
 def clip_grads(grads, max_norm, out=None, stream=None):
     """The gradients' common 2-norm, and the gradients clipped to `max_norm`:
     in place, or into the tensors of `out`.  A norm that is not finite leaves
-    them as they are and sets ST_NONFINITE."""
+    them as they are and sets ST_NONFINITE.  `norm` and `coef` share a storage with
+    the workspace, 8 KB for every 160 tensors (clone what is to last)."""
     grads = list(grads)
     if not grads:
         raise ValueError("grads is empty")
