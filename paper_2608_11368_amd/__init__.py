@@ -421,7 +421,8 @@ def pair_page_plan(n, cached, fresh, mask, page, table, free_pages, free_count, 
                    d_status=None, stream=None):
     if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[0] < n:
         raise ValueError("table must be a 2-D tensor with a row for each request")
-    at, capacity = _native().address, free_pages.numel()
+    native, capacity = _native(), free_pages.numel()
+    at = native.address
     _rc(lib().pair_page_plan(
         n, at(cached, "cached", torch.int32, n), at(fresh, "fresh", torch.int32, n),
         at(mask, "mask", torch.uint8, n, True), int(page), at(table, "table", torch.int32),
@@ -434,6 +435,7 @@ def pair_page_plan(n, cached, fresh, mask, page, table, free_pages, free_count, 
         at(free_count_out, "free_count_out", torch.int64, 1),
         at(workspace, "workspace", torch.uint8), workspace.numel(),
         at(d_status, "d_status", torch.int32, 1, True), _stream(stream)), "pair_page_plan")
+    native.written(table, q_offsets, lens, slots, positions, free_out, free_count_out)
 
 
 def _cache_refused(k_cache, v_cache):
@@ -472,6 +474,7 @@ def pair_cache_store(k, v, slots, k_cache, v_cache, d_status=None, stream=None):
         page, pages, native.address(slots, "slots", torch.int64, tokens),
         native.address(d_status, "d_status", torch.int32, 1, True), _stream(stream)),
         "pair_cache_store")
+    native.written(k_cache, v_cache)
 
 
 def pair_paged_attention_workspace_bytes(n, tokens, q_heads, kv_heads, dim, max_q, max_len) -> int:
@@ -503,6 +506,7 @@ def pair_paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max
         at(workspace, "workspace", torch.uint8), workspace.numel(),
         at(d_status, "d_status", torch.int32, 1, True), _stream(stream)),
         "pair_paged_attention")
+    native.written(out, lse)
 
 
 def pair_clip_grads_workspace_bytes(count) -> int:
@@ -512,11 +516,14 @@ def pair_clip_grads_workspace_bytes(count) -> int:
 def pair_clip_grads(grads, max_norm, norm, coef, workspace, out=None, d_status=None, stream=None):
     """`out`: None clips in place, else a list of tensors of the gradients'
     sizes, each of its gradient's type or float32."""
-    at, table = _native().address, _native().grad_table
-    ptrs, sizes, codes = table(grads if type(grads) is list else list(grads), "grads")
+    native = _native()
+    at, table = native.address, native.grad_table
+    grads = grads if type(grads) is list else list(grads)
+    ptrs, sizes, codes = table(grads, "grads")
     optrs = ocodes = None
     if out is not None:
-        optrs, osizes, ocodes = table(out if type(out) is list else list(out), "out")
+        out = out if type(out) is list else list(out)
+        optrs, osizes, ocodes = table(out, "out")
         if osizes != sizes:
             raise ValueError("out must hold a tensor of each gradient's size")
     _rc(lib().pair_clip_grads(
@@ -524,6 +531,7 @@ def pair_clip_grads(grads, max_norm, norm, coef, workspace, out=None, d_status=N
         at(norm, "norm", torch.float32, 1), at(coef, "coef", torch.float32, 1),
         at(workspace, "workspace", torch.uint8), workspace.numel(),
         at(d_status, "d_status", torch.int32, 1, True), _stream(stream)), "pair_clip_grads")
+    native.written(norm, coef, grads if out is None else out)
 
 
 # ------------------------------------------------ allocating helpers -------

@@ -238,6 +238,29 @@ PyObject* parts(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return result;
 }
 
+// written(tensor, list of tensors or None, ...): counts a write that torch has not
+// seen, so that autograd notices if it had saved the old values.
+PyObject* written(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  auto count = [](PyObject* x) {
+    if (!THPVariable_Check(x)) return;
+    const at::Tensor& t = THPVariable_Unpack(x);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();   // those have no count
+  };
+  try {
+    for (Py_ssize_t i = 0; i < n; ++i) {
+      if (PyList_Check(args[i])) {
+        for (Py_ssize_t k = 0; k < PyList_GET_SIZE(args[i]); ++k) count(PyList_GET_ITEM(args[i], k));
+      } else {
+        count(args[i]);
+      }
+    }
+  } catch (...) {
+    torch::translate_exception_to_python(std::current_exception());
+    return nullptr;
+  }
+  Py_RETURN_NONE;
+}
+
 PyMethodDef kMethods[] = {
     {"grad_table", grad_table, METH_VARARGS,
      "grad_table(list, name): addresses, sizes and type codes of GPU tensors, as bytes."},
@@ -251,6 +274,8 @@ PyMethodDef kMethods[] = {
     {"parts", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(parts)),
      METH_FASTCALL,
      "parts(device, dtype, shape, ...): uninitialised GPU tensors of one allocation."},
+    {"written", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(written)),
+     METH_FASTCALL, "written(tensor, list or None, ...): counts a write to each tensor."},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, kMethods,
