@@ -806,10 +806,27 @@ def page_plan(cached, fresh, table, free_pages, free_count, page, max_tokens, ma
 @_allocating
 def cache_store(k, v, slots, k_cache, v_cache, stream=None):
     """New keys and values [tokens][kv_heads][dim] into their slots of the
-    caches [pages][page][kv_heads][dim]; negative slots are skipped."""
+    caches [pages][page][kv_heads][dim]; negative slots are skipped.  The caches
+    hold values: no gradient goes through them."""
     st = _status(k_cache.device)
     pair_cache_store(k, v, slots, k_cache, v_cache, st, stream)
     return {"k_cache": k_cache, "v_cache": v_cache, "status": st}
+
+
+class _NoGradient(torch.autograd.Function):
+    """paged_attention on arguments that want a gradient: the results join the
+    graph, so that a backward pass through them fails and is not cut in silence."""
+
+    @staticmethod
+    def forward(ctx, compute, *wanting):
+        r = compute()
+        ctx.mark_non_differentiable(r["status"])
+        return r["out"], r["lse"], r["status"]
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise NotImplementedError("paged_attention has no gradient: call it under torch.no_grad() "
+                                  "or on detached queries and caches")
 
 
 @_allocating
@@ -818,7 +835,14 @@ def paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max_len,
     """Causal attention of the packed new tokens q [tokens][q_heads][dim] over
     their requests' pages, the new tokens' own keys included.  `max_q` and
     `max_len` bound a request's new tokens and keys; `scale` defaults to
-    1/sqrt(dim)."""
+    1/sqrt(dim).  For generation: it has no gradient, and a backward pass through
+    its results raises (a given `out` is written and stays out of the graph)."""
+    if ((q.requires_grad or k_cache.requires_grad or v_cache.requires_grad) and out is None
+            and torch.is_grad_enabled()):
+        out, lse, st = _NoGradient.apply(
+            lambda: paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max_len,
+                                    scale, want_lse, None, workspace, stream), q, k_cache, v_cache)
+        return {"out": out, "lse": lse, "status": st}
     tokens, heads, dim = q.shape
     parts, index, lse = _native().parts, q.get_device(), None
     if out is None:

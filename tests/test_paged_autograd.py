@@ -83,3 +83,35 @@ def test_a_plan_counts_its_table(gpu):
         pair.page_plan(i32(3, 4), i32(0, 0), table.clone(), r["free_pages"], r["free_count"], 16, 7)
         pair.clip_grads([torch.ones(3, device=DEV)], 0.5)
     torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("wants", ["q", "k_cache", "v_cache"])
+def test_attention_is_not_cut_from_the_graph_in_silence(gpu, wants):
+    """A backward pass that comes to the attention's results fails; the results
+    are the same, and under no_grad or on a given output nothing changes."""
+    a = paged()
+    want = pair.paged_attention(**a, want_lse=True)
+    assert not want["out"].requires_grad
+    a[wants] = a[wants].detach().requires_grad_()
+    for lse in (False, True):
+        r = pair.paged_attention(**a, want_lse=lse)
+        assert torch.equal(r["out"], want["out"]) and int(r["status"].item()) == 0
+        assert (r["lse"] is None) if not lse else torch.equal(r["lse"], want["lse"])
+        for x in (r["out"], r["lse"]) if lse else (r["out"],):
+            with pytest.raises(NotImplementedError, match="no gradient"):
+                x.float().sum().backward()
+        assert not r["status"].requires_grad
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    r = pair.paged_attention(**a, stream=side)
+    side.synchronize()
+    assert torch.equal(r["out"], want["out"]) and r["out"].requires_grad
+    with torch.no_grad():
+        assert not pair.paged_attention(**a)["out"].requires_grad
+    with torch.inference_mode():
+        assert not pair.paged_attention(**a)["out"].requires_grad
+    out = torch.empty_like(want["out"])
+    r = pair.paged_attention(**a, out=out)
+    torch.cuda.synchronize()
+    assert r["out"] is out and not out.requires_grad and torch.equal(out, want["out"])
