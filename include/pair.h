@@ -639,7 +639,9 @@ size_t pair_paged_attention_workspace_bytes(int64_t n, int64_t tokens, int32_t q
  * is rounded to the type of v for the matrix cores (fp16: those below 2^-21 of
  * the largest to a multiple of 2^-31 of it).
  *
- *   n, tokens    requests, and rows of q and out
+ *   n, tokens    requests, and rows of q and out; a call is of less than 2^24
+ *                workgroups: (n + tokens * (q_heads / kv_heads) / 128) * kv_heads,
+ *                where requests of one token and longer chunks mix n twice
  *   q_heads      a multiple of kv_heads, at most 64 * kv_heads
  *   dim          head width: 64 or 128
  *   dtype        PAIR_BF16 or PAIR_F16, of q, the caches and out

@@ -31,6 +31,14 @@ bool together(const AttnCall& a) {
 
 }  // namespace
 
+int64_t attention_groups(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads,
+                         int32_t dim, int32_t max_q, int32_t max_len) {
+  const int64_t rows = attention_rows_groups(n, q_heads, kv_heads, dim, max_q, max_len);
+  if (most_rows(q_heads, kv_heads, max_q) <= kRowsMost) return rows;
+  return (has_few(n, tokens, max_q) ? rows : 0) +
+         attention_tiles_groups(n, tokens, q_heads, kv_heads, dim, max_len);
+}
+
 size_t attention_workspace_bytes(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads,
                                  int32_t dim, int32_t max_q, int32_t max_len) {
   const size_t rows = rounded(attention_rows_workspace(n, q_heads, kv_heads, dim, max_q, max_len));

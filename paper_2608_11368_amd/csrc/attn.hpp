@@ -132,9 +132,13 @@ constexpr int kRowsMost = 32;
 
 size_t attention_rows_workspace(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim,
                                 int32_t max_q, int32_t max_len);
+int64_t attention_rows_groups(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim,
+                              int32_t max_q, int32_t max_len);
 int launch_attention_rows(const AttnCall& a, void* workspace, hipStream_t stream);
 size_t attention_tiles_workspace(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads,
                                  int32_t dim, int32_t max_len);
+int64_t attention_tiles_groups(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads,
+                               int32_t dim, int32_t max_len);
 int launch_attention_tiles(const AttnCall& a, int32_t least_rows, void* few_workspace,
                            void* workspace, hipStream_t stream);
 

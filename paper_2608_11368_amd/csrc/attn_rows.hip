@@ -94,7 +94,6 @@ __global__ __launch_bounds__(kThreads) void join_rows_kernel(RowArgs s, int rows
 template <bool BF16, int DIM>
 int launch(const RowArgs& s, const Plan& p, hipStream_t stream) {
   const int64_t grid = groups_of(s.a, p);
-  if (s.a.n * s.a.kv_heads > 0x7fffffffLL) return PAIR_ERANGE;
   const bool aligned = s.page.d % 16 == 0;
   // Uncut workgroups that have a compute unit each: eight waves instead of four
   // (4 requests of 400 keys, 8 heads of 128: 6.8 us instead of 7.8, of 1000: 9.3
@@ -175,6 +174,12 @@ int rows::join_rows(const RowArgs& s, const Plan& p, hipStream_t stream) {
 size_t attention_rows_workspace(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim,
                                 int32_t max_q, int32_t max_len) {
   return plan_of(n, q_heads, kv_heads, dim, max_q, max_len).total;
+}
+
+int64_t attention_rows_groups(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim,
+                              int32_t max_q, int32_t max_len) {
+  const Plan p = plan_of(n, q_heads, kv_heads, dim, max_q, max_len);
+  return (p.runs > n ? p.runs : n) * kv_heads;       // the joins: one for a request and head
 }
 
 int launch_attention_rows(const AttnCall& a, void* workspace, hipStream_t stream) {

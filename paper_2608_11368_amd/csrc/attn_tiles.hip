@@ -717,7 +717,6 @@ int launch(const TileArgs& s, const Plan& p, const rows::RowArgs* w, const rows:
            hipStream_t stream) {
   const int64_t grid = p.tiles * s.a.kv_heads * p.splits;
   const int64_t few = w != nullptr ? rows::groups_of(s.a, *wp) : 0;
-  if (grid + few > 0x7fffffffLL || s.a.n * s.a.kv_heads > 0x7fffffffLL) return PAIR_ERANGE;
   if (s.a.n > kInline) {
     hipLaunchKernelGGL(tile_starts_kernel, dim3(1), dim3(1024), 0, stream, s);
     if (hipGetLastError() != hipSuccess) return PAIR_EHIP;
@@ -755,6 +754,14 @@ int launch(const TileArgs& s, const Plan& p, const rows::RowArgs* w, const rows:
 size_t attention_tiles_workspace(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads,
                                  int32_t dim, int32_t max_len) {
   return plan_tiles(n, tokens, q_heads, kv_heads, dim, max_len).total;
+}
+
+int64_t attention_tiles_groups(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads,
+                               int32_t dim, int32_t max_len) {
+  const Plan p = plan_tiles(n, tokens, q_heads, kv_heads, dim, max_len);
+  const int64_t grid = p.tiles * kv_heads * p.splits;
+  const int64_t joins = p.splits > 1 ? (tokens * q_heads + kWaves - 1) / kWaves : 0;
+  return grid > joins ? grid : joins;
 }
 
 int launch_attention_tiles(const AttnCall& a, int32_t least_rows, void* few_workspace,

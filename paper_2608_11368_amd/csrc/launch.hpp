@@ -129,6 +129,10 @@ struct AttnCall {
   int32_t* d_status;
 };
 
+// Workgroups of a call's largest launch.
+int64_t attention_groups(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads,
+                         int32_t dim, int32_t max_q, int32_t max_len);
+
 size_t attention_workspace_bytes(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads,
                                  int32_t dim, int32_t max_q, int32_t max_len);
 
