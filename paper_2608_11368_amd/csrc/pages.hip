@@ -603,9 +603,11 @@ int launch_cache_store(int64_t tokens, int32_t kv_heads, int32_t dim, const void
   a.slots = slots;
   a.tokens = tokens;
   a.d_status = d_status;
-  // About four pieces a lane, at least one token a workgroup.
+  // About four pieces a lane, at least one token a workgroup, and no more of them
+  // than a launch can have (below 2^32 threads).
   int per_group = (int)(kThreads * kStorePieces / a.per_token.d);
-  if (per_group < 1) per_group = 1;
+  const int least = (int)((tokens + (1 << 23) - 1) >> 23);
+  if (per_group < least) per_group = least;
   const int64_t grid = (tokens + per_group - 1) / per_group;
   hipLaunchKernelGGL(cache_store_kernel, dim3((unsigned)grid), dim3(kThreads), 0, stream, a,
                      per_group);

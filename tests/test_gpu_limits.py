@@ -39,3 +39,21 @@ def test_attention_of_16_million_requests():
     assert bool((r["out"] == few["out"][0]).all())
     with pytest.raises(pair.PairError, match="size out of the supported range"):
         call(n + 1)
+
+
+def test_store_of_16_million_wide_tokens():
+    """Rows of 16 KB, more of them than a launch has workgroups; nearly all are
+    skipped."""
+    n = (1 << 24) + 77
+    log(f"cache store: {n} tokens of 32 heads of 128")
+    row = torch.randn((1, 32, 128), device=DEV).bfloat16()
+    caches = [torch.zeros((2, 16, 32, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    slots = torch.full((n,), -1, dtype=torch.int64, device=DEV)
+    slots[5], slots[n // 2], slots[n - 1] = 3, 30, 17
+    r = pair.cache_store(row.expand(n, 32, 128), row.expand(n, 32, 128), slots, *caches)
+    torch.cuda.synchronize()
+    assert int(r["status"].item()) == 0
+    for c in caches:
+        flat = c.view(32, 32, 128)
+        assert bool((flat[[3, 30, 17]] == row).all())
+        assert int((flat != 0).any(2).any(1).sum()) == 3
