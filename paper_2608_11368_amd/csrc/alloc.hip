@@ -414,6 +414,7 @@ int launch_alloc(int64_t B, int64_t nv, int32_t gmax, const int64_t* offsets, co
                  int32_t design, const float* pi_prev, int32_t max_sweeps, float* pi,
                  double* objective, int32_t* iters, double* residual, int32_t* d_status,
                  hipStream_t stream) {
+  if (too_many_threads(B, kWave)) return PAIR_ERANGE;
   const int32_t cap = max_sweeps > 0 ? max_sweeps : kDefaultCap;
 #define PAIR_ALLOC(EDGES_, SCALED_)                                                               \
   hipLaunchKernelGGL((alloc_kernel<EDGES_, SCALED_>), dim3((unsigned)B), dim3(kWave), 0, stream, B, \

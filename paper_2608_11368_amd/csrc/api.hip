@@ -35,7 +35,6 @@ constexpr int64_t kMaxTensors = (int64_t)1 << 20;
 constexpr int64_t kMaxRequests = (int64_t)1 << 24;
 constexpr int64_t kMaxSlots = 0x7fffffff;
 constexpr int32_t kMaxHeads = 1024;
-constexpr int64_t kMaxGroups = ((int64_t)1 << 24) - 1;   // of 256 threads: HIP counts 2^32 - 1
 
 bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; }
 
@@ -439,7 +438,8 @@ static int check_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t k
   // rows and key positions are counted in 31 bits, with room for a window ahead
   if (tokens > kMaxSlots / q_heads || max_len > kMaxSlots / 2) return PAIR_ERANGE;
   if (max_q < 0 || max_len < 0 || (tokens > 0 && max_q < 1)) return PAIR_ERANGE;
-  if (pair::attention_groups(n, tokens, q_heads, kv_heads, dim, max_q, max_len) > kMaxGroups)
+  if (pair::too_many_threads(
+          pair::attention_groups(n, tokens, q_heads, kv_heads, dim, max_q, max_len), 256))
     return PAIR_ERANGE;
   return PAIR_OK;
 }

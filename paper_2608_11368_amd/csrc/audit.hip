@@ -946,8 +946,14 @@ int run_audit(const AuditLayout& L, const AuditArgs& A) {
   const int64_t stream_grid = A.B * L.slots, eval_grid = A.B * L.nchunk;
   const int64_t table_grid = A.B * (gram_tiles(KS) + 1);
   const int64_t nbias = COS ? 1 : L.nbias, final_grid = A.B * nbias;
-  if (stream_grid > 0x7fffffffLL || eval_grid > 0x7fffffffLL || table_grid > 0x7fffffffLL ||
-      final_grid > 0x7fffffffLL)
+  // Groups of up to 16 have one tile: more prompts than the chip holds of both
+  // kinds of workgroups at once take one workgroup for both (2000 prompts:
+  // 12.9 us in two, 9.5 us in one; 256 prompts: 4.9 us in two).
+  const bool together = KS == 1 && table_grid > 8 * (int64_t)device_cu_count();
+  const bool one_wave = KS == 1 && A.R <= kWave;      // of a chunk's replicates, see below
+  if (too_many_threads(stream_grid, kGramThreads) ||
+      too_many_threads(eval_grid, one_wave ? kWave : kEvalThreads) ||
+      too_many_threads(together ? A.B : table_grid, 256) || too_many_threads(final_grid, kFinalThreads))
     return PAIR_ERANGE;
   // The cosine audit reports what its Gram matrix holds, so it reads every
   // prompt and leaves the products unscaled: an overflow is a non-finite entry.
@@ -958,10 +964,6 @@ int run_audit(const AuditLayout& L, const AuditArgs& A) {
                      reinterpret_cast<uint16_t*>(bits), A.edge_count != nullptr ? 1 : 0,
                      A.d_status);
   if (hipGetLastError() != hipSuccess) return PAIR_EHIP;
-  // Groups of up to 16 have one tile: more prompts than the chip holds of both
-  // kinds of workgroups at once take one workgroup for both (2000 prompts:
-  // 12.9 us in two, 9.5 us in one; 256 prompts: 4.9 us in two).
-  const bool together = KS == 1 && table_grid > 8 * (int64_t)device_cu_count();
   const bool few = L.nsl >= kTableSlices && table_grid <= 2 * (int64_t)device_cu_count();
   hipLaunchKernelGGL((audit_tables_kernel<KS>), dim3((unsigned)(together ? A.B : table_grid)),
                      dim3(few ? kTableThreads : 256), 0,
@@ -977,7 +979,7 @@ int run_audit(const AuditLayout& L, const AuditArgs& A) {
   };
   // A chunk of at most 64 replicates and small tables are one wave's (2000 prompts of 4,
   // R = 32: 13.5 us with four, 8.3 us with one).
-  if (KS == 1 && A.R <= kWave)
+  if (one_wave)
     eval(std::integral_constant<int, KS == 1 ? kWave : kEvalThreads>{});
   else
     eval(std::integral_constant<int, kEvalThreads>{});

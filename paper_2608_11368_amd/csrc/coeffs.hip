@@ -238,6 +238,7 @@ int launch_design_coeffs(int64_t B, int64_t nv, int32_t gmax, const int64_t* off
                          const float* p, const float* rewards, uint64_t seed, int64_t rep,
                          uint8_t* mask, float* pi, float* coeff, int32_t* edge_count,
                          int32_t* completed, int32_t* d_status, hipStream_t stream) {
+  if (too_many_threads(B, 64)) return PAIR_ERANGE;
   hipLaunchKernelGGL(design_coeffs_kernel, dim3((unsigned)B), dim3(64), 0, stream, B, nv, gmax,
                      offsets, p, rewards, seed, rep, mask, pi, coeff, edge_count, completed,
                      d_status);
@@ -248,6 +249,7 @@ int launch_coeffs(int64_t B, int64_t nv, int32_t gmax, const int64_t* offsets,
                   const float* rewards, const uint8_t* mask, const float* pi, int32_t rule,
                   float wmax, float* coeff, int32_t* edge_count, float* ess, float* max_weight,
                   int32_t* d_status, hipStream_t stream) {
+  if (too_many_threads(B, 64)) return PAIR_ERANGE;
   const size_t lds = pi != nullptr ? (size_t)gmax * (gmax + 1) * sizeof(float) : 0;
   hipLaunchKernelGGL(edge_coeffs_kernel, dim3((unsigned)B), dim3(64), lds, stream, B, nv, gmax,
                      offsets, rewards, mask, pi, rule, wmax, coeff, edge_count, ess, max_weight,

@@ -477,6 +477,7 @@ __global__ __launch_bounds__(kDrawReps) void cps_draw_kernel(
 int launch_cps_fit(int64_t B, int64_t nv, int32_t gmax, const int64_t* offsets,
                    const float* pi_target, double* w, int32_t* n_out, float* pi_joint,
                    int32_t* iters, int32_t* d_status, hipStream_t stream) {
+  if (too_many_threads(B, kWave)) return PAIR_ERANGE;
   const int ks = (gmax + 15) / 16;
 #define PAIR_CPS_FIT(KP_)                                                                        \
   hipLaunchKernelGGL(cps_fit_kernel<KP_>, dim3((unsigned)B), dim3(kWave), 0, stream, B, nv, gmax, \
@@ -501,6 +502,7 @@ int launch_cps_draw(int64_t B, int64_t nv, int32_t gmax, const int64_t* offsets,
   const int64_t reps = R < kDrawReps ? (R + kWave - 1) / kWave * kWave : kDrawReps;
   const int64_t nwg = (R + reps - 1) / reps;
   const int64_t grid = B * nwg;
+  if (too_many_threads(grid, reps)) return PAIR_ERANGE;
 #define PAIR_CPS_DRAW(KP_)                                                                     \
   hipLaunchKernelGGL(cps_draw_kernel<KP_>, dim3((unsigned)grid), dim3((unsigned)reps), 0, stream, B, nv, \
                      gmax, offsets, w, n, seed, rep0, R, nwg, mask, edge_count, d_status)

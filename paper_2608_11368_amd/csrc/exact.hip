@@ -328,7 +328,7 @@ int launch_audit_exact(int64_t B, int64_t nv, int32_t gmax, const int64_t* offse
   const ExactLayout L = exact_layout(B, gmax, D);
   const uint16_t* s = static_cast<const uint16_t*>(scores);
   const int64_t grid = B * L.nsl;
-  if (grid > 0x7fffffffLL) return PAIR_ERANGE;
+  if (too_many_threads(grid, kGramThreads) || too_many_threads(B, 1024)) return PAIR_ERANGE;
 #define PAIR_GRAM(KS_, PART_)                                                                    \
   hipLaunchKernelGGL((gram_kernel<KS_, PART_>), dim3((unsigned)grid), dim3(kGramThreads), 0,      \
                      stream, nv, gmax, offsets, D, s, ld, L.nsl, L.slice,                        \

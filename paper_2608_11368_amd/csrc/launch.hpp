@@ -11,6 +11,12 @@ namespace pair {
 // Compute units of the current device (cached per device).
 int device_cu_count();
 
+// Whether a launch is of 2^32 threads or more: HIP counts them in 32 bits and
+// starts the remainder without an error.
+inline bool too_many_threads(int64_t groups, int64_t threads) {
+  return groups > (int64_t)0xffffffff / threads;
+}
+
 int launch_design(int64_t B, int64_t nv, int32_t gmax, const int64_t* offsets, const float* p,
                   uint64_t seed, int64_t rep0, int64_t R, uint8_t* mask, float* pi,
                   int32_t* edge_count, int32_t* completed, int32_t* d_status, hipStream_t stream);

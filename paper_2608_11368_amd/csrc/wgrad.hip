@@ -355,7 +355,7 @@ int launch_wgrad(int64_t B, int64_t nv, const int64_t* offsets, int64_t D, const
   const unsigned char* s = static_cast<const unsigned char*>(scores);
   if (reduce) {
     const int64_t grid = (D + kThreads * kPieceCols - 1) / (kThreads * kPieceCols);
-    if (grid > 0x7fffffffLL) return PAIR_ERANGE;
+    if (too_many_threads(grid, kThreads)) return PAIR_ERANGE;
     // Row groups per workgroup: enough that the grid holds about 8 waves per
     // SIMD of the chip (4 row groups at most, one 1024-thread workgroup).
     const int64_t simds = 4 * (int64_t)device_cu_count();
@@ -377,7 +377,8 @@ int launch_wgrad(int64_t B, int64_t nv, const int64_t* offsets, int64_t D, const
   const int64_t tile = (int64_t)kThreads * kPieceCols * (bf16 ? 4 : 2);
   const int64_t full_tiles = D / tile;                 // tiles wholly inside [0, D)
   const bool tail = full_tiles * tile < D;
-  if (B * full_tiles > 0x7fffffffLL) return PAIR_ERANGE;
+  if (too_many_threads(B * full_tiles, kThreads) || (tail && too_many_threads(B, kThreads)))
+    return PAIR_ERANGE;
   // Prompts streamed at once (see wgrad_kernel): 4 for groups of at most 8
   // rollouts on average, else 2.  Measured on b128 (G = 16), the Qwen3-shaped
   // slice (G = 8) and ragged (mean G 33), against one prompt at a time: +1.5,

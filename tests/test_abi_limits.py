@@ -30,3 +30,37 @@ def test_paged_attention():
                                    (1 << 19, 1 << 24, 16, 8, 40)):
         assert size(n, tokens, hq, hkv, 64, mq, 16) > 0, (n, tokens, hq, hkv, mq)
         assert attention(n, tokens, hq, hkv, mq) == -6        # in range, no workspace
+
+
+def test_paged_attention_past_the_limit():
+    """HIP counts a launch's threads in 32 bits, so a little more than the limit
+    is a launch of a few workgroups and no error."""
+    size = pair.lib().pair_paged_attention_workspace_bytes
+    for n, heads in (((1 << 23) + 77, 2), ((1 << 20) + 5, 16), ((1 << 22) + (1 << 21), 4)):
+        assert attention(n, n, heads, heads, 1) == ERANGE
+        assert size(n, n, heads, heads, 64, 1, 16) == 0
+
+
+def test_calls_of_many_prompts():
+    """64 threads a prompt: 2^26 prompts are one too many; 256: 2^24."""
+    L, ws = pair.lib(), 1 << 62
+
+    def calls(B):
+        nv = 2 * B
+        yield L.pair_edge_coeffs(B, nv, 2, FAKE, FAKE, FAKE, FAKE, FAKE, None, None, None)
+        yield L.pair_design_coeffs(B, nv, 2, FAKE, FAKE, FAKE, 1, 0, None, None, FAKE, None, None,
+                                   None, None)
+        yield L.pair_design_alloc(B, nv, 2, FAKE, FAKE, FAKE, None, FAKE, 0.1, 0, FAKE, None, None,
+                                  None, None)
+        yield L.pair_cps_fit(B, nv, 2, FAKE, FAKE, FAKE, FAKE, None, None, None, None)
+        yield L.pair_cps_draw(B, nv, 2, FAKE, FAKE, FAKE, 1, 0, 1, FAKE, None, None, None)
+        yield L.pair_weighted_grad(B, nv, FAKE, 64, FAKE, 1, 64, FAKE, FAKE, 0, None, None)
+        yield L.pair_audit_exact(B, nv, 2, FAKE, 64, FAKE, 1, 64, FAKE, FAKE, None, 0, 0.0, FAKE,
+                                 FAKE, None, FAKE, ws, None, None)
+        yield L.pair_audit(B, nv, 2, FAKE, 64, FAKE, 1, 64, FAKE, FAKE, None, 1, 0, 1, FAKE, FAKE,
+                           None, None, FAKE, ws, None, None)
+        yield L.pair_audit_direction(B, nv, 2, FAKE, 64, FAKE, 1, 64, FAKE, FAKE, None, 0, 0.0, 1, 0,
+                                     1, FAKE, FAKE, FAKE, ws, None, None)
+
+    for B in (1 << 26, (1 << 26) + 5, (1 << 31) - 1):
+        assert list(calls(B)) == [ERANGE] * 9
