@@ -609,7 +609,8 @@ int pair_page_plan(int64_t n, const int32_t* cached, const int32_t* fresh, const
  *   dtype        PAIR_BF16 or PAIR_F16
  *   k, v         element d of head h of row t at t * token_stride +
  *                h * new_head_stride + d (the same strides for both)
- *   k_cache, v_cache  the caches (see above), n_pages * page < 2^31
+ *   k_cache, v_cache  the caches (see above), n_pages * page < 2^31; their
+ *                slots share no element (PAIR_EINVAL: a stride of 0, say)
  * Device status: PAIR_ST_PAGES (a slot beyond the cache; it is skipped).
  */
 int pair_cache_store(int64_t tokens, int32_t kv_heads, int32_t dim, int32_t dtype, const void* k,
@@ -646,7 +647,9 @@ size_t pair_paged_attention_workspace_bytes(int64_t n, int64_t tokens, int32_t q
  *   dim          head width: 64 or 128
  *   dtype        PAIR_BF16 or PAIR_F16, of q, the caches and out
  *   q, out       element d of head h of token t at t * q_token + h * q_head + d
- *                (strides multiples of 8; out likewise)
+ *                (strides multiples of 8; out likewise).  Rows of out share no
+ *                element (PAIR_EINVAL), and none with q, unless out is q, or the
+ *                caches
  *   table, ldt   int32 [n][ldt]; the first ceil(lens[r] / page) entries of row
  *                r are read
  *   q_offsets    int64 [n+1], q_offsets[0] = 0, q_offsets[n] <= tokens: request

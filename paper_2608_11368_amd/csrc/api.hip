@@ -3,6 +3,7 @@
 // and re-check device-resident offsets themselves.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "../../include/pair.h"
@@ -52,6 +53,37 @@ int check_scores(const void* scores, int32_t dtype, int64_t D, int64_t ld) {
   const int64_t elt = dtype == PAIR_BF16 ? 2 : 4;
   if (!aligned16(scores) || (ld * elt) % 16 != 0) return PAIR_EALIGN;
   return PAIR_OK;
+}
+
+// A caller's array, as the checks of overlaps see it.
+struct Extent {
+  const void* at;
+  int64_t bytes;
+};
+
+bool overlap(const Extent& a, const Extent& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+  return a.at != nullptr && b.at != nullptr && a.bytes > 0 && b.bytes > 0 &&
+         x < y + (uint64_t)b.bytes && y < x + (uint64_t)a.bytes;
+}
+
+// Whether rows of `width` elements at all multiples of the strides, `count` of
+// each, may share elements: every dimension has to reach past the smaller ones
+// together (as those of any permuted or padded array do).
+struct Strided {
+  int64_t count, stride;
+};
+
+template <int N>
+bool rows_overlap(Strided (&dims)[N], int64_t width) {
+  std::sort(dims, dims + N, [](const Strided& a, const Strided& b) { return a.stride < b.stride; });
+  __int128 extent = width;
+  for (const Strided& d : dims) {
+    if (d.count <= 1) continue;
+    if (d.stride < extent) return true;
+    extent += (__int128)(d.count - 1) * d.stride;
+  }
+  return false;
 }
 
 hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }
@@ -338,18 +370,6 @@ int pair_clip_grads(int64_t count, const void* const* grads, void* const* outs,
                            workspace, d_status, as_stream(stream));
 }
 
-// A caller's array, as the checks of overlaps see it.
-struct Extent {
-  const void* at;
-  int64_t bytes;
-};
-
-static bool overlap(const Extent& a, const Extent& b) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
-  return a.at != nullptr && b.at != nullptr && a.bytes > 0 && b.bytes > 0 &&
-         x < y + (uint64_t)b.bytes && y < x + (uint64_t)a.bytes;
-}
-
 size_t pair_page_plan_workspace_bytes(int64_t n) {
   return n < 1 || n > kMaxRequests ? 0 : pair::page_plan_workspace_bytes(n);
 }
@@ -423,6 +443,8 @@ int pair_cache_store(int64_t tokens, int32_t kv_heads, int32_t dim, int32_t dtyp
     return PAIR_ERANGE;
   if (!aligned16(k) || !aligned16(v) || token_stride % 8 != 0 || new_head_stride % 8 != 0)
     return PAIR_EALIGN;
+  Strided places[] = {{n_pages, page_stride}, {page, slot_stride}, {kv_heads, head_stride}};
+  if (rows_overlap(places, dim)) return PAIR_EINVAL;
   const pair::PagedCache cache = {page_stride, slot_stride, head_stride, page, n_pages};
   return pair::launch_cache_store(tokens, kv_heads, dim, k, v, token_stride, new_head_stride,
                                   k_cache, v_cache, cache, slots, d_status, as_stream(stream));
@@ -475,6 +497,8 @@ int pair_paged_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_
   if (!aligned16(q) || !aligned16(out) || q_token % 8 != 0 || q_head % 8 != 0 ||
       out_token % 8 != 0 || out_head % 8 != 0)
     return PAIR_EALIGN;
+  Strided results[] = {{tokens, out_token}, {q_heads, out_head}};
+  if (rows_overlap(results, dim)) return PAIR_EINVAL;
   if (bad_workspace(workspace, ws_bytes, pair::attention_workspace_bytes(
                                              n, tokens, q_heads, kv_heads, dim, max_q, max_len)))
     return PAIR_EWORKSPACE;

@@ -54,3 +54,41 @@ def test_page_plan():
             assert plan(**{out: beside})[0] != EINVAL, (out, other)
     assert plan(cached=at["fresh"])[0] != EINVAL         # inputs may
     assert plan(mask=None, positions=None, d_status=None)[0] != EINVAL
+
+
+BASE = 1 << 20
+
+
+def store(ps, ss, ch, pages=10, page=16, heads=2):
+    return pair.lib().pair_cache_store(
+        10, heads, 64, 1, ptr(BASE), ptr(BASE), heads * 64, 64, ptr(BASE), ptr(BASE), ps, ss, ch,
+        page, pages, ptr(BASE), None, None)
+
+
+def attention(ot, oh, tokens=5, heads=4, qt=256, qh=64):
+    L = pair.lib()
+    need = L.pair_paged_attention_workspace_bytes(2, tokens, heads, 2, 64, 5, 100)
+    return L.pair_paged_attention(
+        2, tokens, heads, 2, 64, 1, ptr(BASE), qt, qh, ptr(BASE), ptr(BASE), 0, 0, 0, 16, 10,
+        ptr(BASE), 7, ptr(BASE), ptr(BASE), 5, 100, 0.1, ptr(BASE), ot, oh, None, ptr(BASE), need,
+        None, None)
+
+
+def test_slots_that_share_elements():
+    for fine in ((2048, 128, 64), (2048, 64, 1024), (64, 1280, 640), (4096, 136, 64), (128, 1 << 40, 64)):
+        assert store(*fine) != EINVAL, fine
+    for bad in ((0, 128, 64), (2048, 0, 64), (2048, 128, 0), (1920, 128, 64), (2048, 64, 64),
+                (2048, 128, 56), (2048, 64, 960), (64, 1280, 632)):
+        assert store(*bad) == EINVAL, bad
+    # of one page, slot or head the stride does not count
+    assert store(0, 128, 64, pages=1) != EINVAL
+    assert store(128, 0, 64, page=1) != EINVAL
+    assert store(1024, 64, 0, heads=1) != EINVAL
+
+
+def test_results_that_share_elements():
+    for fine in ((256, 64), (64, 320), (264, 64), (1 << 40, 64)):
+        assert attention(*fine) != EINVAL, fine
+    for bad in ((0, 64), (256, 0), (192, 64), (64, 256), (256, 56)):
+        assert attention(*bad) == EINVAL, bad
+    assert attention(0, 64, tokens=1) != EINVAL and attention(256, 64, qt=0, qh=0) != EINVAL
