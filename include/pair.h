@@ -680,7 +680,8 @@ size_t pair_clip_grads_workspace_bytes(int64_t count);
  * gradients clipped to it:
  *     norm = sqrt( sum over tensors and elements of g^2 )   (fp64 sums),
  *     coef = max_norm / norm where norm > max_norm, else 1,
- *     out  = coef * g, rounded once to the type of out.
+ *     out  = coef * g: coef rounded to fp32, the product to fp32 and, if that is
+ *            the type of out, to 16 bits.
  * If the norm is not finite, coef = 1 and the gradients stay as they are, so
  * that a step can be skipped by the status word.
  *

@@ -13,16 +13,18 @@ size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // A call of chunks may hold requests of a few rows beside them, which the tile
 // kernel would serve without splitting their keys.  If every request has the
-// bound's tokens, or there is only one, none does.
+// bound's tokens, or there is only one, none does.  The host knows no more: in a
+// call of uneven chunks without short requests the two launches for those find
+// nothing to do, 5 us each (of the 150 us of eight prompts, say).
 bool has_few(int64_t n, int64_t tokens, int32_t max_q) { return n > 1 && tokens < n * max_q; }
 
 // One launch serves both kinds side by side where most requests must be short
 // against the longest (two chunks of 1024 tokens beside 130 single ones over 4000
-// keys, 8 heads of 128: 410 us, two launches 467), or the tiles do not fill the
-// card (one of 90 beside 15 over 3000: 59 and 77; three prompts of 300 to 512 at
-// width 64, none short: 13.6 and 15.4).  It holds the registers of both, for which
-// chunks pay where they are all there is (8 prompts of 301 to 4096 at width 64: 182
-// and 177 us; three chunks over 4000 to 8000 keys at 128: 672 and 627).
+// keys, 8 heads of 128: 409 us, two launches 479), or the tiles do not fill the
+// card (one of 90 beside 15 over 3000: 57 and 76; three prompts of 300 to 512, 4
+// heads of 64, none short: 12.7 and 15).  It holds the registers of both, for which
+// chunks pay where they are all there is (8 prompts of 301 to 4096, 4 heads of 64:
+// 162 and 152 us; three chunks over 4000 to 8000 keys, 8 of 128: 655 both).
 bool together(const AttnCall& a) {
   const int64_t group = a.q_heads / a.kv_heads;
   const int64_t tiles = a.tokens * group / 128 + (a.n < a.tokens ? a.n : a.tokens);

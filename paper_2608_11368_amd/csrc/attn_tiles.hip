@@ -21,12 +21,12 @@
 // When the tiles are too few for the card, each tile's keys are split and a
 // second launch joins the parts.
 //
-// Measured, in 4 * rows * keys * width operations that the masks leave: at width
-// 128 one prompt of 16,384 tokens 1030 TFLOP/s, 8 chunks of 2048 over 8192 keys
-// 1000, three uneven ones over 4000 to 8000 keys 945, 8 prompts of 4096 930, 16
-// chunks of 64 over 4000 keys 700; at width 64 the first two 850 and 850, 8
-// prompts of 301 to 4096 tokens 725.  A product of two 8192^2 matrices by the
-// library runs at 1250.  At width 128 the products and their LDS reads are what
+// Measured, in 4 * rows * keys * width operations that the masks leave, 32 query
+// heads on 8 unless said: at width 128 one prompt of 16,384 tokens 980 TFLOP/s, 8
+// chunks of 2048 after 8192 keys 980, three uneven ones after 4000 to 8000 keys 950,
+// 8 prompts of 4096 (16 on 4) 870, 16 chunks of 64 over 4000 keys 690; at width 64
+// the first two 875 and 860, 8 prompts of 301 to 4096 tokens (16 on 4) 710.  A
+// product of two 8192^2 matrices by the library runs at 1250.  At width 128 the products and their LDS reads are what
 // is left: a wave's 32 rows use each 1 KiB fragment once, and four SIMDs taking
 // one every 32 cycles ask for all of LDS's 128 bytes a cycle; left alone (no
 // weights, no loads) they take 80% of the time, at clocks that the power limit
@@ -49,7 +49,12 @@ constexpr int kRows = 32 * kWaves;          // of a tile
 constexpr int kKeys = 64;                   // of a step
 constexpr float kLazy = 8.0f;
 constexpr int kClasses = 8;                 // of work, in the order of the tiles
-constexpr int kInline = 256;                // requests that a workgroup orders itself
+// Requests that a workgroup orders itself.  Beyond 64 that takes four registers a
+// lane for one, and the launch that counts the tiles first is as fast or faster (16
+// on 4 heads, 30 to 128 tokens after 300: 65 requests 26.6 us ordered and 27.6
+// counted at width 64, 49.5 and 48.4 at 128; 130 47.7 and 45.7, 83 and 76; 256 83 and
+// 75, 158 and 147).
+constexpr int kInline = 256;
 
 // kinds of instructions in a scheduling group
 constexpr int kMfma = 0x8, kDsRead = 0x100;
