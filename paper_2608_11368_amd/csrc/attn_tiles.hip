@@ -26,15 +26,15 @@
 // chunks of 2048 after 8192 keys 980, three uneven ones after 4000 to 8000 keys 950,
 // 8 prompts of 4096 (16 on 4) 870, 16 chunks of 64 over 4000 keys 690; at width 64
 // the first two 875 and 860, 8 prompts of 301 to 4096 tokens (16 on 4) 710.  A
-// product of two 8192^2 matrices by the library runs at 1250.  At width 128 the products and their LDS reads are what
-// is left: a wave's 32 rows use each 1 KiB fragment once, and four SIMDs taking
-// one every 32 cycles ask for all of LDS's 128 bytes a cycle; left alone (no
-// weights, no loads) they take 80% of the time, at clocks that the power limit
-// sets.  At width 64 the exponentials (one per 256 operations instead of 512)
-// take the larger part.  Eight waves in two groups that alternate between
-// products and weights, one workgroup a compute unit, reached 1050 to 1100 on the
-// longest chunks and lost 20 to 40% on 16 x 64 tokens and on single prompts, for
-// which four stay.
+// product of two 8192^2 matrices by the library runs at 1250.  At width 128 the
+// products and their LDS reads are what is left: a wave's 32 rows use each 1 KiB
+// fragment once, and four SIMDs taking one every 32 cycles ask for all of LDS's 128
+// bytes a cycle; left alone (no weights, no loads) they take 80% of the time, at
+// clocks that the power limit sets.  At width 64 the exponentials (one per 256
+// operations instead of 512) take the larger part.  Eight waves in two groups that
+// alternate between products and weights, one workgroup a compute unit, reached 1050
+// to 1100 on the longest chunks and lost 20 to 40% on 16 x 64 tokens and on single
+// prompts, for which four stay.
 #include <type_traits>
 
 #include "attn_rows.hpp"
