@@ -347,7 +347,9 @@ __device__ __forceinline__ void plan_outputs(const PlanArgs& a, const Ends& e,
               (j[s] - start[s])] = id[s];
 }
 
-// Table entries that the pool has no page for become -1, their requests' lengths
+// Pages that requests take beyond the list's length go into the table here (the
+// tiles of pages are as many as the list has: released pages may be more).  Table
+// entries that the pool has no page for become -1, their requests' lengths
 // end with the pages that they got, and what does not fit is reported; by the
 // threads of one workgroup, after the lengths are written.
 __device__ void plan_totals(const PlanArgs& a, const Ends& e, const Counts& total) {
@@ -362,8 +364,16 @@ __device__ void plan_totals(const PlanArgs& a, const Ends& e, const Counts& tota
       raise_status(a.d_status, PAIR_ST_PAGES);
     if (total.tokens > (uint32_t)a.max_tokens) raise_status(a.d_status, PAIR_ST_LENGTH);
   }
+  const int last = (int)a.n - 1;
+  for (uint32_t j = (uint32_t)a.capacity + threadIdx.x; j < used; j += blockDim.x) {
+    const uint32_t x = j - free;              // free is at most the capacity
+    const int from = owner(e.given, x, 0, last), to = owner(e.taken, j, 0, last);
+    const int32_t id = a.table[(int64_t)from * a.ldt + (x - (from > 0 ? e.given[from - 1] : 0u))];
+    a.table[(int64_t)to * a.ldt + pages_of((uint32_t)a.cached[to], a.page) +
+            (j - (to > 0 ? e.taken[to - 1] : 0u))] = id;
+    if (id < 0) raise_status(a.d_status, PAIR_ST_PAGES);
+  }
   if (total.taken > used) {
-    const int last = (int)a.n - 1;
     for (uint32_t j = used + threadIdx.x; j < total.taken; j += blockDim.x) {
       const int r = owner(e.taken, j, 0, last);
       const uint32_t held = pages_of((uint32_t)a.cached[r], a.page);

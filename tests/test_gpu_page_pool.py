@@ -151,3 +151,112 @@ def test_a_count_that_the_list_does_not_hold(n):
         r = pair.page_plan(i32([0] * n), i32([1] * n), table, i32(np.arange(cap)), count(fine), 16, n)
         torch.cuda.synchronize()
         assert int(r["status"].item()) == 0 and listed(r) == list(range(n, fine))
+
+
+def walk(cached, fresh, mask, table, free, page, max_tokens, cap):
+    """The definition, request by request: requests that do not fit are left out,
+    a pool that runs out leaves -1 and shorter lengths, a list that is full drops
+    what is beyond it."""
+    table, width, status = table.copy(), table.shape[1], 0
+    fits = []
+    for c, f, live in zip(cached.tolist(), fresh.tolist(), mask.tolist()):
+        good = c >= 0 and f >= 0 and c + f < 2 ** 31
+        status |= 0 if good else pair.ST_LENGTH
+        if good and -(-(c + f if live else c) // page) > width:
+            good, status = False, status | pair.ST_PAGES
+        fits.append(good)
+    pool = list(free)
+    for r, c in enumerate(cached.tolist()):
+        if fits[r] and not mask[r]:
+            pool += table[r, :-(-c // page)].tolist()
+    if any(p < 0 for p in pool):
+        status |= pair.ST_PAGES
+    taken, q, lens, slots, positions = 0, [0], [], [], []
+    for r, (c, f) in enumerate(zip(cached.tolist(), fresh.tolist())):
+        if not fits[r] or not mask[r]:
+            q.append(q[-1])
+            lens.append(0)
+            continue
+        total, held = c + f, -(-c // page)
+        for k in range(held, -(-total // page)):
+            if taken >= len(pool) and total == c + f:
+                total, status = k * page, status | pair.ST_PAGES
+            table[r, k] = pool[taken] if taken < len(pool) else -1
+            taken += 1
+        for x in range(c, c + f):
+            p = int(table[r, x // page])
+            slots.append(p * page + x % page if p >= 0 else -1)
+            positions.append(x)
+        q.append(q[-1] + f)
+        lens.append(total)
+    left = pool[taken:]
+    if len(left) > cap:
+        status |= pair.ST_PAGES
+    if len(slots) > max_tokens:
+        status |= pair.ST_LENGTH
+    pad = [-1] * (max_tokens - len(slots))
+    return dict(q_offsets=q, lens=lens, slots=(slots + pad)[:max_tokens],
+                positions=(positions + pad)[:max_tokens], table=table,
+                free_pages=(left + [-1] * cap)[:cap], free_count=[min(len(left), cap)], status=[status])
+
+
+@pytest.mark.parametrize("n", [1, 2, 5, 63, 64, 65, 256, 1000, 2047, 2048, 2049, 4000, 16_384, 17_000])
+def test_random_plans_against_a_walk(n):
+    """Pools that are short, exact or ample, lists that are too short for what
+    comes back, requests that do not fit, masks of every density."""
+    log(f"page pool: random plans of {n}")
+    for seed in range(12 if n < 3000 else 4):
+        rng = np.random.default_rng([n, seed])
+        page = int(rng.choice([1, 3, 16, 20, 64]))
+        cached = rng.integers(0, int(rng.choice([2, 30, 200])), n)
+        fresh = rng.integers(0, int(rng.choice([2, 9, 60])), n)
+        mask = (rng.random(n) < rng.choice([0.0, 0.2, 0.6, 1.0, 1.0])).astype(np.uint8)
+        held, need = -(-cached // page), -(-(cached + fresh) // page)
+        width = max(1, int(need.max()) - int(rng.integers(0, 2)), int(held.max()))
+        ids = rng.permutation(int(need.sum()) + 9).astype(np.int32)
+        table = np.full((n, width), -1, dtype=np.int32)
+        at = np.arange(width)[None, :] < held[:, None]
+        table[at] = ids[:int(held.sum())]
+        wanted = int((need - held).sum())
+        some = int(rng.choice([0, wanted // 3, max(0, wanted - 1), wanted, wanted + 9]))
+        free = ids[int(held.sum()):][:some]
+        cap = max(1, len(free) + int(rng.choice([0, 3, int(held.sum())])))
+        if rng.random() < 0.3:
+            cached[rng.integers(0, n)] = -1
+        if rng.random() < 0.3:
+            fresh[rng.integers(0, n)] = 2 ** 31 - 1
+        live = mask != 0
+        room = int(rng.choice([0, 1, 5])) + int(fresh[live & (fresh < 1000)].sum())
+        room = max(0, room - int(rng.choice([0, 0, 3])))
+        full = np.full(cap, -9, dtype=np.int32)
+        full[:len(free)] = free
+        r = pair.page_plan(i32(cached), i32(fresh), i32(table), i32(full), count(len(free)), page, room,
+                           mask=torch.from_numpy(mask).to(DEV))
+        torch.cuda.synchronize()
+        want = walk(cached, fresh, mask, table, free, page, room, cap)
+        for k, w in want.items():
+            got = r[k].cpu().numpy()
+            assert np.array_equal(got, np.asarray(w).reshape(got.shape)), (seed, k)
+
+
+@pytest.mark.parametrize("n", [2, 600, 2500])
+@pytest.mark.parametrize("cap", [0, 1, 5])
+def test_a_short_list_and_many_released_pages(n, cap):
+    """More pages change hands in one step than the list has entries: they go
+    straight from the released requests to the others."""
+    log(f"page pool: a list of {cap}, {n} requests")
+    page, half = 16, n // 2
+    table = np.full((n, 4), -1, dtype=np.int32)
+    table[:half, :3] = np.random.default_rng(n).permutation(3 * half).reshape(half, 3)
+    cached, fresh = np.where(np.arange(n) < half, 40, 0), np.where(np.arange(n) < half, 0, 48)
+    mask = (np.arange(n) >= half).astype(np.uint8)
+    fresh[half * 2:] = 0
+    r = pair.page_plan(i32(cached), i32(fresh), i32(table),
+                       torch.full((cap,), -9, dtype=torch.int32, device=DEV), count(0), page,
+                       48 * half, mask=torch.from_numpy(mask).to(DEV))
+    torch.cuda.synchronize()
+    want = walk(cached, fresh, mask, table, [], page, 48 * half, cap)
+    for k, w in want.items():
+        got = r[k].cpu().numpy()
+        assert np.array_equal(got, np.asarray(w).reshape(got.shape)), k
+    assert want["status"] == [0] and want["free_count"] == [0]
