@@ -571,7 +571,9 @@ size_t pair_page_plan_workspace_bytes(int64_t n);
  *   mask         uint8 [n], 0 = released (or NULL: all continue)
  *   page         tokens per page >= 1
  *   table        int32 [n][ldt] in/out: entries h_r .. h_r + m_r - 1 are written
- *   capacity     entries of free_pages and free_out (the pool's page count)
+ *   capacity     entries of free_pages and free_out (the pool's page count; what
+ *                does not fit the new list is lost and sets PAIR_ST_PAGES, what
+ *                passes from released requests to others need not fit)
  *   free_pages   int32 [capacity] in: the first *free_count are free
  *   free_count   int64 [1] in (device); one outside 0 .. capacity sets
  *                PAIR_ST_PAGES and counts as the nearer of the two
