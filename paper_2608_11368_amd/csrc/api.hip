@@ -460,7 +460,10 @@ static int check_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t k
   // rows and key positions are counted in 31 bits, with room for a window ahead
   if (tokens > kMaxSlots / q_heads || max_len > kMaxSlots / 2) return PAIR_ERANGE;
   if (max_q < 0 || max_len < 0 || (tokens > 0 && max_q < 1)) return PAIR_ERANGE;
-  if (pair::too_many_threads(
+  // Not counted where two workgroups a request and head and one for 64 rows, more
+  // than a call has beside some thousands, are far from a launch's 2^24.
+  if ((2 * n + tokens) * q_heads > (int64_t)1 << 22 &&
+      pair::too_many_threads(
           pair::attention_groups(n, tokens, q_heads, kv_heads, dim, max_q, max_len), 256))
     return PAIR_ERANGE;
   return PAIR_OK;
