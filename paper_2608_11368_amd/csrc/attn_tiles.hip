@@ -49,11 +49,11 @@ constexpr int kRows = 32 * kWaves;          // of a tile
 constexpr int kKeys = 64;                   // of a step
 constexpr float kLazy = 8.0f;
 constexpr int kClasses = 8;                 // of work, in the order of the tiles
-// Requests that a workgroup orders itself.  Beyond 64 that takes four registers a
-// lane for one, and the launch that counts the tiles first is as fast or faster (16
-// on 4 heads, 30 to 128 tokens after 300: 65 requests 26.6 us ordered and 27.6
-// counted at width 64, 49.5 and 48.4 at 128; 130 47.7 and 45.7, 83 and 76; 256 83 and
-// 75, 158 and 147).
+// Requests that a workgroup orders itself.  Beyond 64 of them a lane holds four, and
+// counting the tiles in a launch before is as fast or faster (16 on 4 heads, 30 to
+// 128 tokens after 300, at width 64 and 128: 65 requests 26.6 and 49.5 us ordered,
+// 27.6 and 48.4 counted; 130 requests 47.7 and 83, 45.7 and 76; 256 requests 83 and
+// 158, 75 and 147).
 constexpr int kInline = 256;
 
 // kinds of instructions in a scheduling group
