@@ -61,12 +61,17 @@ extern "C" {
 #define PAIR_BF16 1
 #define PAIR_F16 2           /* gradients, caches and queries; scores are fp32 or bf16 */
 
+/* Formats of a paged cache in 8 and 4 bits. */
+#define PAIR_MXFP8 8         /* E4M3 codes, a byte each                        */
+#define PAIR_MXFP4 4         /* E2M1 codes, two to a byte, the first in its low half */
+
 /* Device status bits (OR-ed into *d_status). */
 #define PAIR_ST_BAD_GROUP 1  /* G_b < 2, G_b > gmax or offsets not monotone    */
 #define PAIR_ST_RHO_RANGE 2  /* an OBSERVED edge has rho outside (0, 1]        */
 #define PAIR_ST_P_RANGE 4    /* a continuation probability outside (0, 1]      */
-#define PAIR_ST_NONFINITE 8  /* a non-finite score in an audited score block, or
-                                a gradient norm that is not finite             */
+#define PAIR_ST_NONFINITE 8  /* a non-finite score in an audited score block, a
+                                gradient norm that is not finite, or a block of
+                                a key or value stored in 8 or 4 bits that is not */
 #define PAIR_ST_BUDGET 16    /* design: budget below pi_min * sum(c), or an
                                 invalid prefix statistic (p outside [0, 1],
                                 c or m not positive and finite)               */
@@ -673,6 +678,99 @@ int pair_paged_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_
                          const int32_t* lens, int32_t max_q, int32_t max_len, float scale,
                          void* out, int64_t out_token, int64_t out_head, float* lse,
                          void* workspace, size_t ws_bytes, int32_t* d_status, void* stream);
+
+/*
+ * A paged cache in 8 or 4 bits: formats MXFP8 (E4M3) and MXFP4 (E2M1) of the OCP
+ * Microscaling specification 1.0.  Blocks of 32 elements of a row (a token's key
+ * or value of one head) share a scale, one byte b that stands for 2^(b - 127)
+ * (255: every element of the block is NaN); an element is its code times it.  A
+ * row takes dim + dim / 32 or dim / 2 + dim / 32 bytes for the 2 * dim of 16 bits.
+ *
+ * Codes and scales are arrays of their own; those of keys and values have the same
+ * layout.  In slot y,
+ *     codes of head h     at (y / page) * page_stride + (y % page) * slot_stride +
+ *                            h * head_stride,    dim or dim / 2 bytes,
+ *     scales of head h    at (y / page) * scale_page + (y % page) * scale_slot +
+ *                            h * scale_head,     dim / 32 bytes.
+ * All strides are in bytes.  Bases and strides of codes are multiples of 16, those of
+ * scales of the largest power of two that divides dim / 32, but at most 4.  (Codes
+ * of a head's slots side by side, [pages][kv_heads][page][..], are read fastest:
+ * a page's scales of a head then share cache lines.)
+ */
+typedef struct pair_mx_cache {
+  void* k;                       /* codes of the keys                          */
+  void* v;                       /* codes of the values                        */
+  void* k_scale;
+  void* v_scale;
+  int64_t page_stride, slot_stride, head_stride;
+  int64_t scale_page, scale_slot, scale_head;
+  int64_t n_pages;               /* n_pages * page < 2^31                      */
+  int32_t page;                  /* slots of a page                            */
+  int32_t kv_heads;
+  int32_t dim;                   /* head width, a multiple of 32, at most 256  */
+  int32_t format;                /* PAIR_MXFP8 or PAIR_MXFP4                   */
+} pair_mx_cache;
+
+/*
+ * pair_cache_store_mx -- the new tokens' keys and values, quantised, into their
+ * slots.
+ *
+ * A block's scale is the smallest power of two, from 2^-100 on, under which its
+ * largest magnitude is at most the largest code (448 or 6); each element is then
+ * rounded to the nearest code, ties to the even one, and is off by at most half a
+ * step between codes.  Numbers near the end of the 16-bit type's range that would
+ * be rounded past it are stored as the largest that stays within (fp16: 61440 in
+ * 8 bits, 49152 in 4).  A block that holds a NaN or an infinity is stored as NaN.
+ *
+ *   tokens       rows of k and v (>= 0); row t goes to slot slots[t], a
+ *                negative slot is skipped; slots of one call are distinct
+ *   dtype        PAIR_BF16 or PAIR_F16, of k and v
+ *   k, v         element d of head h of row t at t * token_stride +
+ *                h * new_head_stride + d (the same strides for both, in elements,
+ *                multiples of 8; bases 16-byte aligned)
+ *   cache        HOST struct, read during the call; its rows share no byte
+ *                (PAIR_EINVAL), nor do its four arrays
+ * Device status: PAIR_ST_PAGES (a slot beyond the cache; it is skipped),
+ * PAIR_ST_NONFINITE (a block was stored as NaN).
+ */
+int pair_cache_store_mx(const pair_mx_cache* cache, int64_t tokens, int32_t dtype, const void* k,
+                        const void* v, int64_t token_stride, int64_t new_head_stride,
+                        const int64_t* slots, int32_t* d_status, void* stream);
+
+/*
+ * pair_cache_load_mx -- cached keys and values, by slot, as 16-bit rows: what the
+ * codes stand for, which rows stored from that type have exactly.  (Rows stored
+ * from bf16 and read as fp16 are rounded, to infinity beyond its range.)
+ *
+ *   tokens       rows of k and v (>= 0); row t is that of slot slots[t], the same
+ *                slot any number of times; zeros where the slot is negative
+ *   dtype        PAIR_BF16 or PAIR_F16, of k and v
+ *   k, v         out: element d of head h of row t at t * token_stride +
+ *                out_head_stride * h + d (strides and bases as above; rows share no
+ *                element: PAIR_EINVAL)
+ * Device status: PAIR_ST_PAGES (a slot beyond the cache; its row is zeros).
+ */
+int pair_cache_load_mx(const pair_mx_cache* cache, int64_t tokens, const int64_t* slots,
+                       int32_t dtype, void* k, void* v, int64_t token_stride,
+                       int64_t out_head_stride, int32_t* d_status, void* stream);
+
+/* pair_paged_attention_mx_workspace_bytes -- device workspace of pair_paged_attention_mx. */
+size_t pair_paged_attention_mx_workspace_bytes(int64_t n, int64_t tokens, int32_t q_heads,
+                                               int32_t kv_heads, int32_t dim, int32_t max_q,
+                                               int32_t max_len);
+
+/*
+ * pair_paged_attention_mx -- pair_paged_attention over a cache in 8 or 4 bits: the
+ * same sums, of the values that codes and scales stand for in the type of q (see
+ * pair_cache_load_mx).  Heads of 64 or 128; every other argument, bound and status
+ * as there.  A page or slot that no token sees may hold any bytes.
+ */
+int pair_paged_attention_mx(const pair_mx_cache* cache, int64_t n, int64_t tokens, int32_t q_heads,
+                            int32_t dtype, const void* q, int64_t q_token, int64_t q_head,
+                            const int32_t* table, int64_t ldt, const int64_t* q_offsets,
+                            const int32_t* lens, int32_t max_q, int32_t max_len, float scale,
+                            void* out, int64_t out_token, int64_t out_head, float* lse,
+                            void* workspace, size_t ws_bytes, int32_t* d_status, void* stream);
 
 /* pair_clip_grads_workspace_bytes -- device workspace for `count` tensors. */
 size_t pair_clip_grads_workspace_bytes(int64_t count);

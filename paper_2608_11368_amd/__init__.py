@@ -33,6 +33,8 @@ LIB_PATH = os.environ.get("PAIR_LIB") or os.path.join(_HERE, "libpair.so")
 PAIR_F32 = 0
 PAIR_BF16 = 1
 PAIR_F16 = 2
+PAIR_MXFP8 = 8
+PAIR_MXFP4 = 4
 ST_BAD_GROUP = 1
 ST_RHO_RANGE = 2
 ST_P_RANGE = 4
@@ -62,6 +64,8 @@ EXPORTED = ("pair_design_coeffs", "pair_design_alloc", "pair_design_alloc_ex", "
             "pair_page_plan_workspace_bytes", "pair_page_plan", "pair_cache_store",
             "pair_paged_attention_workspace_bytes", "pair_paged_attention",
             "pair_clip_grads_workspace_bytes", "pair_clip_grads",
+            "pair_cache_store_mx", "pair_cache_load_mx",
+            "pair_paged_attention_mx_workspace_bytes", "pair_paged_attention_mx",
             "pair_strerror", "pair_version")
 
 
@@ -144,6 +148,16 @@ def lib() -> ctypes.CDLL:
         L.pair_clip_grads_workspace_bytes.restype = size
         L.pair_clip_grads.argtypes = [i64, P, P, P, P, P, f32, P, P, P, size, P, P]
         L.pair_clip_grads.restype = ctypes.c_int
+        # the first: a pair_mx_cache, as bytes or a ctypes structure's address
+        L.pair_cache_store_mx.argtypes = [P, i64, i32, P, P, i64, i64, P, P, P]
+        L.pair_cache_store_mx.restype = ctypes.c_int
+        L.pair_cache_load_mx.argtypes = [P, i64, P, i32, P, P, i64, i64, P, P]
+        L.pair_cache_load_mx.restype = ctypes.c_int
+        L.pair_paged_attention_mx_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32, i32]
+        L.pair_paged_attention_mx_workspace_bytes.restype = size
+        L.pair_paged_attention_mx.argtypes = [P, i64, i64, i32, i32, P, i64, i64, P, i64, P, P, i32,
+                                              i32, f32, P, i64, i64, P, P, size, P, P]
+        L.pair_paged_attention_mx.restype = ctypes.c_int
         L.pair_strerror.argtypes = [ctypes.c_int]
         L.pair_strerror.restype = ctypes.c_char_p
         L.pair_version.argtypes = []
@@ -509,6 +523,108 @@ def pair_paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max
     native.written(out, lse)
 
 
+_MX_CODES = (torch.float8_e4m3fn, torch.float4_e2m1fn_x2)
+_HALF_CODES = {torch.bfloat16: PAIR_BF16, torch.float16: PAIR_F16}
+
+
+def _mx_refused(k_cache, v_cache, k_scale, v_scale):
+    for name, c in (("k_cache", k_cache), ("v_cache", v_cache), ("k_scale", k_scale),
+                    ("v_scale", v_scale)):
+        if not isinstance(c, torch.Tensor) or not c.is_cuda or c.dim() != 4:
+            raise ValueError(f"{name} must be a 4-D CUDA tensor [pages][page][kv_heads][..]")
+    if k_cache.dtype not in _MX_CODES or v_cache.dtype != k_cache.dtype:
+        raise TypeError("the caches must both be float8_e4m3fn or both float4_e2m1fn_x2")
+    if k_scale.dtype != torch.float8_e8m0fnu or v_scale.dtype != torch.float8_e8m0fnu:
+        raise TypeError("the scales must be float8_e8m0fnu")
+    if v_cache.shape != k_cache.shape or v_scale.shape != k_scale.shape:
+        raise ValueError("k_cache and v_cache, and their scales, must have the same shape")
+    dim = k_cache.shape[3] * (1 if k_cache.dtype == _MX_CODES[0] else 2)
+    if k_scale.shape[:3] != k_cache.shape[:3] or k_scale.shape[3] * 32 != dim:
+        raise ValueError(f"rows of {dim} elements need a scale for every 32 of them, got "
+                         f"{tuple(k_scale.shape)} for {tuple(k_cache.shape)}")
+    raise ValueError("keys and values must have the same strides and contiguous rows")
+
+
+def _half_code(t, name):
+    code = _HALF_CODES.get(t.dtype) if isinstance(t, torch.Tensor) else None
+    if code is None:
+        raise TypeError(f"{name} must be a bfloat16 or float16 tensor")
+    return code
+
+
+def _pair_of_rows(native, k, v, code, heads, dim):
+    """Addresses, strides and the count of the rows of two like tensors."""
+    kp, tok, head, tokens, _ = (native.rows(k, code, heads, dim)
+                                or _rows_refused(k, "k", k.dtype, heads, dim))
+    vp, vtok, vhead, vtokens, _ = (native.rows(v, code, heads, dim)
+                                   or _rows_refused(v, "v", k.dtype, heads, dim))
+    if vtok != tok or vhead != head or vtokens != tokens:
+        raise ValueError("k and v must have the same shape and strides")
+    return kp, vp, tok, head, tokens
+
+
+def pair_cache_store_mx(k, v, slots, k_cache, v_cache, k_scale, v_scale, d_status=None,
+                        stream=None):
+    native = _native()
+    cache, heads, dim = (native.mx_cache(k_cache, v_cache, k_scale, v_scale)
+                         or _mx_refused(k_cache, v_cache, k_scale, v_scale))
+    code = _half_code(k, "k")
+    kp, vp, tok, head, tokens = _pair_of_rows(native, k, v, code, heads, dim)
+    _rc(lib().pair_cache_store_mx(
+        cache, tokens, code, kp, vp, tok, head,
+        native.address(slots, "slots", torch.int64, tokens),
+        native.address(d_status, "d_status", torch.int32, 1, True), _stream(stream)),
+        "pair_cache_store_mx")
+    native.written(k_cache, v_cache, k_scale, v_scale)
+
+
+def pair_cache_load_mx(slots, k_cache, v_cache, k_scale, v_scale, k, v, d_status=None,
+                       stream=None):
+    native = _native()
+    cache, heads, dim = (native.mx_cache(k_cache, v_cache, k_scale, v_scale)
+                         or _mx_refused(k_cache, v_cache, k_scale, v_scale))
+    code = _half_code(k, "k")
+    kp, vp, tok, head, tokens = _pair_of_rows(native, k, v, code, heads, dim)
+    _rc(lib().pair_cache_load_mx(
+        cache, tokens, native.address(slots, "slots", torch.int64, tokens), code, kp, vp, tok, head,
+        native.address(d_status, "d_status", torch.int32, 1, True), _stream(stream)),
+        "pair_cache_load_mx")
+    native.written(k, v)
+
+
+def pair_paged_attention_mx_workspace_bytes(n, tokens, q_heads, kv_heads, dim, max_q,
+                                            max_len) -> int:
+    return int(lib().pair_paged_attention_mx_workspace_bytes(n, tokens, q_heads, kv_heads, dim,
+                                                             max_q, max_len))
+
+
+def pair_paged_attention_mx(q, k_cache, v_cache, k_scale, v_scale, table, q_offsets, lens, max_q,
+                            max_len, scale, out, lse, workspace, d_status=None, stream=None):
+    native = _native()
+    cache, _, dim = (native.mx_cache(k_cache, v_cache, k_scale, v_scale)
+                     or _mx_refused(k_cache, v_cache, k_scale, v_scale))
+    code = _half_code(q, "q")
+    qp, qt, qh, tokens, heads = (native.rows(q, code, 0, dim)
+                                 or _rows_refused(q, "q", q.dtype, 0, dim))
+    op, ot, oh, orows, _ = (native.rows(out, code, heads, dim)
+                            or _rows_refused(out, "out", q.dtype, heads, dim))
+    n = lens.numel()
+    if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[0] < n:
+        raise ValueError("table must be a 2-D tensor with a row for each request")
+    if orows < tokens:
+        raise ValueError(f"out holds {orows} tokens, needs {tokens}")
+    at = native.address
+    _rc(lib().pair_paged_attention_mx(
+        cache, n, tokens, heads, code, qp, qt, qh, at(table, "table", torch.int32), table.shape[1],
+        at(q_offsets, "q_offsets", torch.int64, n + 1), at(lens, "lens", torch.int32, n),
+        int(max_q), int(max_len), float(scale), op, ot, oh,
+        at(lse, "lse", torch.float32, tokens * heads, True),
+        at(workspace, "workspace", torch.uint8), workspace.numel(),
+        at(d_status, "d_status", torch.int32, 1, True), _stream(stream)),
+        "pair_paged_attention_mx")
+    native.written(out, lse)
+
+
 def pair_clip_grads_workspace_bytes(count) -> int:
     return int(lib().pair_clip_grads_workspace_bytes(count))
 
@@ -814,7 +930,7 @@ def cache_store(k, v, slots, k_cache, v_cache, stream=None):
 
 
 class _NoGradient(torch.autograd.Function):
-    """paged_attention on arguments that want a gradient: the results join the
+    """A paged attention on arguments that want a gradient: the results join the
     graph, so that a backward pass through them fails and is not cut in silence."""
 
     @staticmethod
@@ -857,6 +973,81 @@ def paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max_len,
     st = _status(q.device)
     pair_paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max_len,
                          dim ** -0.5 if scale is None else scale, out, lse, workspace, st, stream)
+    return {"out": out, "lse": lse, "status": st}
+
+
+def mx_cache(pages, page, kv_heads, dim, dtype=torch.float8_e4m3fn, device="cuda"):
+    """An empty paged cache in 8 or 4 bits: (k_cache, v_cache, k_scale, v_scale), codes
+    [pages][page][kv_heads][dim, or dim / 2 bytes of two] of `dtype` (float8_e4m3fn or
+    float4_e2m1fn_x2) and scales [pages][page][kv_heads][dim / 32], with the slots of
+    a head side by side in memory.  The calls take them in this order, as `*cache`."""
+    if dtype not in _MX_CODES:
+        raise TypeError("dtype must be float8_e4m3fn or float4_e2m1fn_x2")
+    if dim < 32 or dim > 256 or dim % 32:
+        raise ValueError(f"dim must be a multiple of 32 up to 256, got {dim}")
+    width = dim if dtype == _MX_CODES[0] else dim // 2
+
+    def half(width, dtype):
+        return torch.zeros((pages, kv_heads, page, width), dtype=torch.uint8,
+                           device=device).view(dtype).transpose(1, 2)
+
+    return (half(width, dtype), half(width, dtype), half(dim // 32, torch.float8_e8m0fnu),
+            half(dim // 32, torch.float8_e8m0fnu))
+
+
+@_allocating
+def cache_store_mx(k, v, slots, k_cache, v_cache, k_scale, v_scale, stream=None):
+    """New keys and values [tokens][kv_heads][dim], bfloat16 or float16, into their
+    slots of a cache in 8 or 4 bits (see mx_cache): blocks of 32 elements with a power
+    of two as their scale.  Negative slots are skipped; a block that holds a NaN or
+    an infinity is stored as NaN and sets ST_NONFINITE.  No gradient goes through."""
+    st = _status(k_cache.device)
+    pair_cache_store_mx(k, v, slots, k_cache, v_cache, k_scale, v_scale, st, stream)
+    return {"k_cache": k_cache, "v_cache": v_cache, "k_scale": k_scale, "v_scale": v_scale,
+            "status": st}
+
+
+@_allocating
+def cache_load_mx(slots, k_cache, v_cache, k_scale, v_scale, dtype=torch.bfloat16, stream=None):
+    """The keys and values of `slots` (int64; zeros where one is negative) out of a
+    cache in 8 or 4 bits, [tokens][kv_heads][dim] of `dtype`, bfloat16 or float16: the
+    very values that attention over the cache works with.  Both are parts of one
+    allocation and share a storage (clone what is to last)."""
+    tokens, heads = slots.numel(), k_cache.shape[2]
+    shape = (tokens, heads, 32 * k_scale.shape[3])
+    k, v = _native().parts(k_cache.get_device(), dtype, shape, dtype, shape)
+    st = _status(k_cache.device)
+    pair_cache_load_mx(slots, k_cache, v_cache, k_scale, v_scale, k, v, st, stream)
+    return {"k": k, "v": v, "status": st}
+
+
+@_allocating
+def paged_attention_mx(q, k_cache, v_cache, k_scale, v_scale, table, q_offsets, lens, max_q,
+                       max_len, scale=None, want_lse=False, out=None, workspace=None, stream=None):
+    """paged_attention over a cache in 8 or 4 bits, read as it is: q, bfloat16 or
+    float16, is the type that its values are taken in (exactly, if they were stored
+    from it).  All else as for paged_attention."""
+    if q.requires_grad and out is None and torch.is_grad_enabled():
+        out, lse, st = _NoGradient.apply(
+            lambda: paged_attention_mx(q, k_cache, v_cache, k_scale, v_scale, table, q_offsets,
+                                       lens, max_q, max_len, scale, want_lse, None, workspace,
+                                       stream), q)
+        return {"out": out, "lse": lse, "status": st}
+    tokens, heads, dim = q.shape
+    parts, index, lse = _native().parts, q.get_device(), None
+    if out is None:
+        out, = parts(index, q.dtype, (tokens, heads, dim))
+    if want_lse:
+        lse, = parts(index, torch.float32, (tokens, heads))
+    max_q, max_len = int(max_q), int(max_len)
+    need = _attention_workspace(_device_index(), lens.numel(), tokens, heads, k_cache.shape[2], dim,
+                                max_q, max_len)
+    if workspace is None or workspace.numel() < need:
+        workspace, = parts(index, torch.uint8, need)
+    st = _status(q.device)
+    pair_paged_attention_mx(q, k_cache, v_cache, k_scale, v_scale, table, q_offsets, lens, max_q,
+                            max_len, dim ** -0.5 if scale is None else scale, out, lse, workspace,
+                            st, stream)
     return {"out": out, "lse": lse, "status": st}
 
 

@@ -18,7 +18,8 @@ LIB = os.path.join(HERE, "libpair.so")
 TENSORS = os.path.join(HERE, "_tensors.so")
 SOURCES = ["api.hip", "design.hip", "coeffs.hip", "wgrad.hip", "audit.hip", "exact.hip", "alloc.hip",
            "cps.hip", "noalloc.hip", "clip.hip", "pages.hip", "attn.hip", "attn_rows.hip",
-           "attn_tiles.hip"]
+           "attn_tiles.hip", "mx_cache.hip", "mx_rows8.hip", "mx_rows4.hip", "mx_tiles8.hip",
+           "mx_tiles4.hip"]
 ARCH = "gfx950"
 
 # Packed fp32 VALU ops are kept off in all device code.

@@ -476,19 +476,14 @@ size_t pair_paged_attention_workspace_bytes(int64_t n, int64_t tokens, int32_t q
   return pair::attention_workspace_bytes(n, tokens, q_heads, kv_heads, dim, max_q, max_len);
 }
 
-int pair_paged_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads, int32_t dim,
-                         int32_t dtype, const void* q, int64_t q_token, int64_t q_head,
-                         const void* k_cache, const void* v_cache, int64_t page_stride,
-                         int64_t slot_stride, int64_t head_stride, int32_t page, int64_t n_pages,
-                         const int32_t* table, int64_t ldt, const int64_t* q_offsets,
-                         const int32_t* lens, int32_t max_q, int32_t max_len, float scale,
-                         void* out, int64_t out_token, int64_t out_head, float* lse,
-                         void* workspace, size_t ws_bytes, int32_t* d_status, void* stream) {
-  if (dtype != PAIR_BF16 && dtype != PAIR_F16) return PAIR_EDTYPE;
-  int st = check_attention(n, tokens, q_heads, kv_heads, dim, max_q, max_len);
-  if (st) return st;
-  st = check_cache(k_cache, v_cache, page_stride, slot_stride, head_stride, page, n_pages);
-  if (st) return st;
+// What the attention's calls share: `c` has the cache, already checked, and dim,
+// kv_heads and bits.
+static int attention(pair::AttnCall c, int64_t n, int64_t tokens, int32_t q_heads, int32_t dtype,
+                     const void* q, int64_t q_token, int64_t q_head, const int32_t* table,
+                     int64_t ldt, const int64_t* q_offsets, const int32_t* lens, int32_t max_q,
+                     int32_t max_len, float scale, void* out, int64_t out_token, int64_t out_head,
+                     float* lse, void* workspace, size_t ws_bytes, int32_t* d_status,
+                     void* stream) {
   if (table == nullptr || q_offsets == nullptr || lens == nullptr) return PAIR_EINVAL;
   if (ldt < 1 || ldt > kMaxSlots / n) return PAIR_ERANGE;
   if (!(scale > 0.0f && scale <= 3.4e38f)) return PAIR_ERANGE;
@@ -501,23 +496,18 @@ int pair_paged_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_
       out_token % 8 != 0 || out_head % 8 != 0)
     return PAIR_EALIGN;
   Strided results[] = {{tokens, out_token}, {q_heads, out_head}};
-  if (rows_overlap(results, dim)) return PAIR_EINVAL;
-  if (bad_workspace(workspace, ws_bytes, pair::attention_workspace_bytes(
-                                             n, tokens, q_heads, kv_heads, dim, max_q, max_len)))
+  if (rows_overlap(results, c.dim)) return PAIR_EINVAL;
+  if (bad_workspace(workspace, ws_bytes,
+                    pair::attention_workspace_bytes(n, tokens, q_heads, c.kv_heads, c.dim, max_q,
+                                                    max_len)))
     return PAIR_EWORKSPACE;
-  pair::AttnCall c;
   c.n = n;
   c.tokens = tokens;
   c.q_heads = q_heads;
-  c.kv_heads = kv_heads;
-  c.dim = dim;
   c.bf16 = dtype == PAIR_BF16;
   c.q = q;
   c.q_token = q_token;
   c.q_head = q_head;
-  c.k_cache = k_cache;
-  c.v_cache = v_cache;
-  c.cache = {page_stride, slot_stride, head_stride, page, n_pages};
   c.table = table;
   c.ldt = ldt;
   c.q_offsets = q_offsets;
@@ -533,13 +523,153 @@ int pair_paged_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_
   return pair::launch_attention(c, workspace, as_stream(stream));
 }
 
+int pair_paged_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads, int32_t dim,
+                         int32_t dtype, const void* q, int64_t q_token, int64_t q_head,
+                         const void* k_cache, const void* v_cache, int64_t page_stride,
+                         int64_t slot_stride, int64_t head_stride, int32_t page, int64_t n_pages,
+                         const int32_t* table, int64_t ldt, const int64_t* q_offsets,
+                         const int32_t* lens, int32_t max_q, int32_t max_len, float scale,
+                         void* out, int64_t out_token, int64_t out_head, float* lse,
+                         void* workspace, size_t ws_bytes, int32_t* d_status, void* stream) {
+  if (dtype != PAIR_BF16 && dtype != PAIR_F16) return PAIR_EDTYPE;
+  int st = check_attention(n, tokens, q_heads, kv_heads, dim, max_q, max_len);
+  if (st) return st;
+  st = check_cache(k_cache, v_cache, page_stride, slot_stride, head_stride, page, n_pages);
+  if (st) return st;
+  pair::AttnCall c = {};
+  c.kv_heads = kv_heads;
+  c.dim = dim;
+  c.bits = 16;
+  c.k_cache = k_cache;
+  c.v_cache = v_cache;
+  c.cache = {page_stride, slot_stride, head_stride, page, n_pages};
+  return attention(c, n, tokens, q_heads, dtype, q, q_token, q_head, table, ldt, q_offsets, lens,
+                   max_q, max_len, scale, out, out_token, out_head, lse, workspace, ws_bytes,
+                   d_status, stream);
+}
+
+// A cache in 8 or 4 bits; `out` is what the launches take.
+static int check_mx(const pair_mx_cache* c, pair::MxCache* out) {
+  if (c == nullptr || c->k == nullptr || c->v == nullptr || c->k_scale == nullptr ||
+      c->v_scale == nullptr)
+    return PAIR_EINVAL;
+  if (c->format != PAIR_MXFP8 && c->format != PAIR_MXFP4) return PAIR_EDTYPE;
+  if (c->kv_heads < 1 || c->kv_heads > kMaxHeads || c->dim < 32 || c->dim > 256 || c->dim % 32 != 0)
+    return PAIR_ERANGE;
+  if (c->page < 1 || c->n_pages < 1 || c->n_pages > kMaxSlots / c->page) return PAIR_ERANGE;
+  const int64_t codes[] = {c->page_stride, c->slot_stride, c->head_stride};
+  const int64_t scales[] = {c->scale_page, c->scale_slot, c->scale_head};
+  const int blocks = c->dim / 32;
+  const int unit = (blocks & -blocks) < 4 ? blocks & -blocks : 4;
+  for (int64_t s : codes)
+    if (s < 0 || s > kMaxCount) return PAIR_ERANGE;
+  for (int64_t s : scales)
+    if (s < 0 || s > kMaxCount) return PAIR_ERANGE;
+  for (int64_t s : codes)
+    if (s % 16 != 0) return PAIR_EALIGN;
+  for (int64_t s : scales)
+    if (s % unit != 0) return PAIR_EALIGN;
+  if (!aligned16(c->k) || !aligned16(c->v) ||
+      reinterpret_cast<uintptr_t>(c->k_scale) % unit != 0 ||
+      reinterpret_cast<uintptr_t>(c->v_scale) % unit != 0)
+    return PAIR_EALIGN;
+  *out = {c->k,           c->v,           c->k_scale,    c->v_scale,  c->page_stride,
+          c->slot_stride, c->head_stride, c->scale_page, c->scale_slot, c->scale_head,
+          c->n_pages,     c->page,        c->kv_heads,   c->dim,      c->format == PAIR_MXFP8 ? 8 : 4};
+  return PAIR_OK;
+}
+
+// The 16-bit rows that a call of an mx cache moves.
+static int check_rows(int64_t tokens, const void* k, const void* v, int64_t token_stride,
+                      int64_t head_stride, const int64_t* slots) {
+  if (k == nullptr || v == nullptr || slots == nullptr) return PAIR_EINVAL;
+  if (token_stride < 0 || head_stride < 0 || token_stride > kMaxCount || head_stride > kMaxCount)
+    return PAIR_ERANGE;
+  if (!aligned16(k) || !aligned16(v) || token_stride % 8 != 0 || head_stride % 8 != 0)
+    return PAIR_EALIGN;
+  return PAIR_OK;
+}
+
+int pair_cache_store_mx(const pair_mx_cache* cache, int64_t tokens, int32_t dtype, const void* k,
+                        const void* v, int64_t token_stride, int64_t new_head_stride,
+                        const int64_t* slots, int32_t* d_status, void* stream) {
+  if (dtype != PAIR_BF16 && dtype != PAIR_F16) return PAIR_EDTYPE;
+  pair::MxCache c;
+  int st = check_mx(cache, &c);
+  if (st) return st;
+  if (tokens < 0 || tokens > kMaxSlots) return PAIR_ERANGE;
+  if (tokens == 0) return PAIR_OK;
+  st = check_rows(tokens, k, v, token_stride, new_head_stride, slots);
+  if (st) return st;
+  Strided codes[] = {{c.n_pages, c.page_stride}, {c.page, c.slot_stride}, {c.kv_heads, c.head_stride}};
+  Strided scales[] = {{c.n_pages, c.scale_page}, {c.page, c.scale_slot}, {c.kv_heads, c.scale_head}};
+  if (rows_overlap(codes, c.dim * c.bits / 8) || rows_overlap(scales, c.dim / 32)) return PAIR_EINVAL;
+  const void* arrays[] = {c.k, c.v, c.k_scale, c.v_scale};
+  for (int i = 0; i < 4; ++i)
+    for (int j = 0; j < i; ++j)
+      if (arrays[i] == arrays[j]) return PAIR_EINVAL;
+  return pair::launch_mx_move(true, c, tokens, dtype == PAIR_BF16, const_cast<void*>(k),
+                              const_cast<void*>(v), token_stride, new_head_stride, slots, d_status,
+                              as_stream(stream));
+}
+
+int pair_cache_load_mx(const pair_mx_cache* cache, int64_t tokens, const int64_t* slots,
+                       int32_t dtype, void* k, void* v, int64_t token_stride,
+                       int64_t out_head_stride, int32_t* d_status, void* stream) {
+  if (dtype != PAIR_BF16 && dtype != PAIR_F16) return PAIR_EDTYPE;
+  pair::MxCache c;
+  int st = check_mx(cache, &c);
+  if (st) return st;
+  if (tokens < 0 || tokens > kMaxSlots) return PAIR_ERANGE;
+  if (tokens == 0) return PAIR_OK;
+  st = check_rows(tokens, k, v, token_stride, out_head_stride, slots);
+  if (st) return st;
+  Strided rows[] = {{tokens, token_stride}, {c.kv_heads, out_head_stride}};
+  if (rows_overlap(rows, c.dim) || k == v) return PAIR_EINVAL;
+  return pair::launch_mx_move(false, c, tokens, dtype == PAIR_BF16, k, v, token_stride,
+                              out_head_stride, slots, d_status, as_stream(stream));
+}
+
+size_t pair_paged_attention_mx_workspace_bytes(int64_t n, int64_t tokens, int32_t q_heads,
+                                               int32_t kv_heads, int32_t dim, int32_t max_q,
+                                               int32_t max_len) {
+  return pair_paged_attention_workspace_bytes(n, tokens, q_heads, kv_heads, dim, max_q, max_len);
+}
+
+int pair_paged_attention_mx(const pair_mx_cache* cache, int64_t n, int64_t tokens, int32_t q_heads,
+                            int32_t dtype, const void* q, int64_t q_token, int64_t q_head,
+                            const int32_t* table, int64_t ldt, const int64_t* q_offsets,
+                            const int32_t* lens, int32_t max_q, int32_t max_len, float scale,
+                            void* out, int64_t out_token, int64_t out_head, float* lse,
+                            void* workspace, size_t ws_bytes, int32_t* d_status, void* stream) {
+  if (dtype != PAIR_BF16 && dtype != PAIR_F16) return PAIR_EDTYPE;
+  pair::MxCache m;
+  int st = check_mx(cache, &m);
+  if (st) return st;
+  st = check_attention(n, tokens, q_heads, m.kv_heads, m.dim, max_q, max_len);
+  if (st) return st;
+  pair::AttnCall c = {};
+  c.kv_heads = m.kv_heads;
+  c.dim = m.dim;
+  c.bits = m.bits;
+  c.k_cache = m.k;
+  c.v_cache = m.v;
+  c.cache = {m.page_stride, m.slot_stride, m.head_stride, m.page, m.n_pages};
+  c.scales = {static_cast<const unsigned char*>(m.k_scale),
+              static_cast<const unsigned char*>(m.v_scale), m.scale_page, m.scale_slot,
+              m.scale_head};
+  return attention(c, n, tokens, q_heads, dtype, q, q_token, q_head, table, ldt, q_offsets, lens,
+                   max_q, max_len, scale, out, out_token, out_head, lse, workspace, ws_bytes,
+                   d_status, stream);
+}
+
 const char* pair_strerror(int code) {
   switch (code) {
     case PAIR_OK: return "ok";
     case PAIR_EINVAL: return "invalid argument (null pointer, malformed size or overlapping arrays)";
     case PAIR_EDTYPE: return "unsupported dtype";
     case PAIR_ERANGE: return "size out of the supported range";
-    case PAIR_EALIGN: return "base pointer or row stride misaligned (16 bytes; gradients: an element)";
+    case PAIR_EALIGN: return "base pointer or row stride misaligned (16 bytes; gradients: an element; scales: their blocks)";
     case PAIR_EHIP: return "HIP launch or runtime error";
     case PAIR_EWORKSPACE: return "workspace missing, misaligned or too small";
     case PAIR_ESCRATCH:
@@ -548,6 +678,6 @@ const char* pair_strerror(int code) {
   }
 }
 
-int pair_version(void) { return 400; }   // 0.4.0: paged cache and gradient clipping added
+int pair_version(void) { return 500; }   // 0.5.0: paged cache in 8 and 4 bits added
 
 }  // extern "C"

@@ -4,7 +4,7 @@
 
 #include <math.h>
 
-#include "paged.hpp"
+#include "mx.hpp"
 
 namespace pair {
 
@@ -125,8 +125,8 @@ __device__ __forceinline__ int32_t checked_page(const AttnCall& a, int32_t id, i
   return ok ? id : 0;
 }
 
-// The launches of attn_rows.hip (requests of at most kRowsMost rows, a row being
-// a query head of a token) and attn_tiles.hip (those of at least `least_rows`;
+// The launches of attn_rows.hpp (requests of at most kRowsMost rows, a row being
+// a query head of a token) and attn_tiles.hpp (those of at least `least_rows`;
 // with a workspace for the others, both).  32 rows of 8 heads of 128, by the first
 // and by the second: 2 requests of 131,000 keys 187 and 207 us, 256 of 1000 200 and
 // 215, 32 of 4000 112 and 104.  Of 40 and 64 rows, for which only tiles are built:

@@ -8,14 +8,6 @@ using namespace rows;
 
 namespace {
 
-template <bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
-__global__ __launch_bounds__(WAVES * kWave, 2) void attention_rows_kernel(RowArgs s) {
-  __shared__ WaveLds<DIM, NT> lds[WAVES];
-  __shared__ int32_t start[WAVES == kWaves ? kMostScanned + 1 : 1];
-  __shared__ int32_t sums[kWaves];
-  serve<BF16, DIM, NT, ALIGNED, WAVES>(s, blockIdx.x, lds, start, sums);
-}
-
 // Joins the partial sums of the requests that were cut: one workgroup per
 // request, head and row.  The parts' maxima first, a lane each, then their sums
 // with several parts' loads in flight.
@@ -91,32 +83,6 @@ __global__ __launch_bounds__(kThreads) void join_rows_kernel(RowArgs s, int rows
         none ? -INFINITY : log_sum<BF16>(m, l);
 }
 
-template <bool BF16, int DIM>
-int launch(const RowArgs& s, const Plan& p, hipStream_t stream) {
-  const int64_t grid = groups_of(s.a, p);
-  const bool aligned = s.page.d % 16 == 0;
-  // Uncut workgroups that have a compute unit each: eight waves instead of four
-  // (4 requests of 400 keys, 8 heads of 128: 6.8 us instead of 7.8, of 1000: 9.3
-  // instead of 11.3; 32 requests, a workgroup for every unit: 22.1 both).
-  const bool wide = p.runs == 0 && grid <= device_cu_count();
-#define PAIR_ROWS(NT, AL, W)                                                                     \
-  hipLaunchKernelGGL((attention_rows_kernel<BF16, DIM, NT, AL, W>), dim3((unsigned)grid),         \
-                     dim3(W * kWave), 0, stream, s)
-#define PAIR_ROWS_OF(NT, AL)                                                                     \
-  do {                                                                                           \
-    if (wide) PAIR_ROWS(NT, AL, kWideWaves); else PAIR_ROWS(NT, AL, kWaves);                      \
-  } while (0)
-  if (p.tiles == 1) {
-    if (aligned) PAIR_ROWS_OF(1, true); else PAIR_ROWS_OF(1, false);
-  } else {
-    if (aligned) PAIR_ROWS_OF(2, true); else PAIR_ROWS_OF(2, false);
-  }
-#undef PAIR_ROWS_OF
-#undef PAIR_ROWS
-  if (hipGetLastError() != hipSuccess) return PAIR_EHIP;
-  return join_rows(s, p, stream);
-}
-
 }  // namespace
 
 Plan rows::plan_of(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim, int32_t max_q,
@@ -185,8 +151,9 @@ int64_t attention_rows_groups(int64_t n, int32_t q_heads, int32_t kv_heads, int3
 int launch_attention_rows(const AttnCall& a, void* workspace, hipStream_t stream) {
   const Plan p = plan_of(a.n, a.q_heads, a.kv_heads, a.dim, a.max_q, a.max_len);
   const RowArgs s = args_of(a, p, workspace);
-  if (a.dim == 64) return a.bf16 ? launch<true, 64>(s, p, stream) : launch<false, 64>(s, p, stream);
-  return a.bf16 ? launch<true, 128>(s, p, stream) : launch<false, 128>(s, p, stream);
+  if (a.bits == 8) return launch_mx8(s, p, stream);
+  if (a.bits == 4) return launch_mx4(s, p, stream);
+  return launch_of<16>(s, p, stream);
 }
 
 }  // namespace pair

@@ -126,7 +126,7 @@ __device__ __forceinline__ int key_place(int row, int b) {
 
 // LDS of one wave: a block's keys, the values and weights of an odd one, or the
 // wave's sums.
-template <int DIM, int NT>
+template <int BITS, int DIM, int NT>
 struct WaveLds {
   union {
     float sum[16][DIM + 4];
@@ -135,13 +135,14 @@ struct WaveLds {
   };
   uint32_t weight[NT][16][kBlock / 2];
   float stat[16][2];
+  uint32_t scale[2][BITS == 16 ? 1 : kBlock];   // of a block's keys and values: a row's bytes
 };
 
 // A block whose values are not all finite and not all seen by every row: each
 // row adds the values that it sees, one key at a time, and the values are
 // cleared so that the matrix product adds nothing.
-template <bool BF16, int DIM, int NT>
-__device__ __forceinline__ void add_odd_block(WaveLds<DIM, NT>* lds, const u32x4_t (&pf)[NT],
+template <int BITS, bool BF16, int DIM, int NT>
+__device__ __forceinline__ void add_odd_block(WaveLds<BITS, DIM, NT>* lds, const u32x4_t (&pf)[NT],
                                               int kb, const int (&limit)[NT],
                                               Piece<DIM> (*vr)[8], State<DIM, NT>* st) {
   constexpr int ND = DIM / 16;
@@ -177,21 +178,23 @@ __device__ __forceinline__ void add_odd_block(WaveLds<DIM, NT>* lds, const u32x4
   wave_lds_order();
 }
 
-template <bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
+template <int BITS, bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
 __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[NT][DIM / 32],
                                          const int (&limit)[NT], int first_limit, int64_t r,
                                          int64_t kvh, int len, int k0, int k1,
-                                         WaveLds<DIM, NT>* lds, State<DIM, NT>* st) {
+                                         WaveLds<BITS, DIM, NT>* lds, State<DIM, NT>* st) {
   constexpr int NC = DIM / 32;       // 32-dim pieces of a key row
   constexpr int ND = DIM / 16;       // dims of a lane's piece of a value row
   const int lane = threadIdx.x & (kWave - 1);
   const int x = lane & 15, g = lane >> 4;
-  const int64_t head = kvh * s.a.cache.head_stride * 2;
+  constexpr int kUnitBytes = BITS == 16 ? 2 : 1;      // of the cache's strides
+  const int64_t head = kvh * s.a.cache.head_stride * kUnitBytes;
   const unsigned char* kbase = static_cast<const unsigned char*>(s.a.k_cache) + head;
   const unsigned char* vbase = static_cast<const unsigned char*>(s.a.v_cache) + head;
-  const int64_t slot_bytes = s.a.cache.slot_stride * 2, page_bytes = s.a.cache.page_stride * 2;
+  const int64_t slot_bytes = s.a.cache.slot_stride * kUnitBytes;
+  const int64_t page_bytes = s.a.cache.page_stride * kUnitBytes;
   const int32_t* row = s.a.table + r * s.a.ldt;
-  const int64_t lane_off = x * (DIM / 8) + (ALIGNED ? 4 * g * slot_bytes : 0);
+  const int64_t lane_off = x * (DIM / 16 * BITS / 8) + (ALIGNED ? 4 * g * slot_bytes : 0);
 
   // A lane reads piece x of eight rows, the same of keys and values.  Pages are
   // looked up a step before: one per tile of 16 keys where pages are multiples
@@ -217,6 +220,7 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
   if (k0 < k1) lookup(k0);
   for (int kb = k0; kb < k1; kb += kBlock * WAVES) {
     Piece<DIM> kr[8], vr[8];
+    Codes<BITS, DIM / 16> kc[8], vc[8];
     int64_t at[kIds];
 #pragma unroll
     for (int n = 0; n < kIds; ++n) {
@@ -224,17 +228,54 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
       at[n] = checked_page(s.a, id[n], &bad_page) * page_bytes +
               (int64_t)(key - div_by(key, s.page) * s.page.d) * slot_bytes + lane_off;
     }
+    uint32_t scales = 0;
+    if constexpr (BITS != 16) {          // lane: those of one key, or of its value
+      const int y = lane & (kBlock - 1);
+      const uint32_t key = (uint32_t)(kb + y < len ? kb + y : len - 1);
+      const uint32_t pg = div_by(key, s.page);
+      const int32_t page = ALIGNED ? (y < 16 ? id[0] : id[kIds - 1]) : row[pg];
+      const unsigned char* from = (lane < kBlock ? s.a.scales.k : s.a.scales.v) +
+                                  checked_page(s.a, page, &bad_page) * s.a.scales.page +
+                                  (int64_t)(key - pg * s.page.d) * s.a.scales.slot +
+                                  kvh * s.a.scales.head;
+      scales = DIM == 128 ? *reinterpret_cast<const uint32_t*>(from)
+                          : *reinterpret_cast<const uint16_t*>(from);
+    }
+    if constexpr (BITS == 16) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      kr[e].load(kbase + at[ALIGNED ? e >> 2 : e] + (ALIGNED ? (e & 3) * slot_bytes : 0));
+      for (int e = 0; e < 8; ++e)
+        kr[e].load(kbase + at[ALIGNED ? e >> 2 : e] + (ALIGNED ? (e & 3) * slot_bytes : 0));
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      vr[e].load(vbase + at[ALIGNED ? e >> 2 : e] + (ALIGNED ? (e & 3) * slot_bytes : 0));
+      for (int e = 0; e < 8; ++e)
+        vr[e].load(vbase + at[ALIGNED ? e >> 2 : e] + (ALIGNED ? (e & 3) * slot_bytes : 0));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        kc[e].load_once(kbase + at[ALIGNED ? e >> 2 : e] + (ALIGNED ? (e & 3) * slot_bytes : 0));
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        vc[e].load_once(vbase + at[ALIGNED ? e >> 2 : e] + (ALIGNED ? (e & 3) * slot_bytes : 0));
+    }
     if (kb + kBlock * WAVES < k1) lookup(kb + kBlock * WAVES);
 
     // keys through LDS: whole rows come from memory, the product wants a row's
     // piece from every lane
     wave_lds_order();
+    if constexpr (BITS != 16) {
+      lds->scale[lane / kBlock][lane & (kBlock - 1)] = scales;
+      wave_lds_order();
+      const int b = 8 * (x * (DIM / 16) / kMxBlock);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const u32x4_t kb4 = *reinterpret_cast<const u32x4_t*>(&lds->scale[0][16 * t + 4 * g]);
+        const u32x4_t vb4 = *reinterpret_cast<const u32x4_t*>(&lds->scale[1][16 * t + 4 * g]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          kc[4 * t + i].template values<BF16>(mx_scale((kb4[i] >> b) & 255u), kr[4 * t + i].w);
+          vc[4 * t + i].template values<BF16>(mx_scale((vb4[i] >> b) & 255u), vr[4 * t + i].w);
+        }
+      }
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int y = 16 * (e >> 2) + 4 * g + (e & 3);
@@ -307,7 +348,7 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
           bad |= not_finite<BF16>(vr[e].w[w]) ? 1u : 0u;
         }
       }
-      if (__any(bad != 0u)) add_odd_block<BF16, DIM, NT>(lds, pf, kb, limit, &vr, st);
+      if (__any(bad != 0u)) add_odd_block<BITS, BF16, DIM, NT>(lds, pf, kb, limit, &vr, st);
     }
 
 #pragma unroll
@@ -326,9 +367,9 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
 
 // Keys [k0, k1) of one request and head (k0 a multiple of kUnit): the waves'
 // sums, joined, either as results (slot < 0) or as partial sums.
-template <bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
+template <int BITS, bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
 __device__ __forceinline__ void attend(const RowArgs& s, int64_t r, int kvh, int k0, int k1,
-                                       int64_t slot, WaveLds<DIM, NT>* lds) {
+                                       int64_t slot, WaveLds<BITS, DIM, NT>* lds) {
   constexpr int ND = DIM / 16;
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
   const int x = lane & 15, g = lane >> 4;
@@ -360,8 +401,8 @@ __device__ __forceinline__ void attend(const RowArgs& s, int64_t r, int kvh, int
   // unused rows see nothing, so every block counts as masked for them only if
   // it does for the first token
   const int end = k1 < q.len ? k1 : q.len;
-  add_keys<BF16, DIM, NT, ALIGNED, WAVES>(s, qf, limit, q.len - q.tokens, r, kvh, q.len,
-                                   k0 + kBlock * wave, end, lds + wave, &st);
+  add_keys<BITS, BF16, DIM, NT, ALIGNED, WAVES>(s, qf, limit, q.len - q.tokens, r, kvh, q.len,
+                                                k0 + kBlock * wave, end, lds + wave, &st);
 
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -460,9 +501,9 @@ __device__ __forceinline__ void scan_units(const RowArgs& s, uint32_t block, int
 
 // One workgroup's share of a call, `block` its number.  Only workgroups of kWaves
 // waves serve cut calls, and need `start` (kMostScanned + 1) and `sums` (kWaves).
-template <bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
+template <int BITS, bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
 __device__ __forceinline__ void serve(const RowArgs& s, uint32_t block,
-                                      WaveLds<DIM, NT>* lds, int32_t* start, int32_t* sums) {
+                                      WaveLds<BITS, DIM, NT>* lds, int32_t* start, int32_t* sums) {
   const int64_t heads = s.a.kv_heads;
   const bool direct = WAVES != kWaves || s.runs == 0;   // one workgroup per request and head
   const int64_t run = block / (uint32_t)s.a.kv_heads;   // or the request
@@ -502,8 +543,8 @@ __device__ __forceinline__ void serve(const RowArgs& s, uint32_t block,
       c1 = count - c0 < end - u ? count : c0 + (int)(end - u);
       whole = c0 == 0 && c1 == count;
     }
-    attend<BF16, DIM, NT, ALIGNED, WAVES>(s, r, h, c0 * kUnit, c1 * kUnit,
-                                   whole ? -1 : part * heads + h, lds);
+    attend<BITS, BF16, DIM, NT, ALIGNED, WAVES>(s, r, h, c0 * kUnit, c1 * kUnit,
+                                                whole ? -1 : part * heads + h, lds);
     part = 2 * run + 1;
     u += c1 - c0;
   }
@@ -528,6 +569,51 @@ inline int64_t groups_of(const AttnCall& a, const Plan& p) {
 
 // The launch that joins cut requests, if any may be.
 int join_rows(const RowArgs& s, const Plan& p, hipStream_t stream);
+
+template <int BITS, bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave, 2) void attention_rows_kernel(RowArgs s) {
+  __shared__ WaveLds<BITS, DIM, NT> lds[WAVES];
+  __shared__ int32_t start[WAVES == kWaves ? kMostScanned + 1 : 1];
+  __shared__ int32_t sums[kWaves];
+  serve<BITS, BF16, DIM, NT, ALIGNED, WAVES>(s, blockIdx.x, lds, start, sums);
+}
+
+template <int BITS, bool BF16, int DIM>
+int launch(const RowArgs& s, const Plan& p, hipStream_t stream) {
+  const int64_t grid = groups_of(s.a, p);
+  const bool aligned = s.page.d % 16 == 0;
+  // Uncut workgroups that have a compute unit each: eight waves instead of four
+  // (4 requests of 400 keys, 8 heads of 128: 6.8 us instead of 7.8, of 1000: 9.3
+  // instead of 11.3; 32 requests, a workgroup for every unit: 22.1 both).
+  const bool wide = p.runs == 0 && grid <= device_cu_count();
+#define PAIR_ROWS(NT, AL, W)                                                                     \
+  hipLaunchKernelGGL((attention_rows_kernel<BITS, BF16, DIM, NT, AL, W>),                         \
+                     dim3((unsigned)grid), dim3(W * kWave), 0, stream, s)
+#define PAIR_ROWS_OF(NT, AL)                                                                     \
+  do {                                                                                           \
+    if (wide) PAIR_ROWS(NT, AL, kWideWaves); else PAIR_ROWS(NT, AL, kWaves);                      \
+  } while (0)
+  if (p.tiles == 1) {
+    if (aligned) PAIR_ROWS_OF(1, true); else PAIR_ROWS_OF(1, false);
+  } else {
+    if (aligned) PAIR_ROWS_OF(2, true); else PAIR_ROWS_OF(2, false);
+  }
+#undef PAIR_ROWS_OF
+#undef PAIR_ROWS
+  if (hipGetLastError() != hipSuccess) return PAIR_EHIP;
+  return join_rows(s, p, stream);
+}
+
+template <int BITS>
+int launch_of(const RowArgs& s, const Plan& p, hipStream_t stream) {
+  if (s.a.dim == 64)
+    return s.a.bf16 ? launch<BITS, true, 64>(s, p, stream) : launch<BITS, false, 64>(s, p, stream);
+  return s.a.bf16 ? launch<BITS, true, 128>(s, p, stream) : launch<BITS, false, 128>(s, p, stream);
+}
+
+// launch_of for caches of 8 and 4 bits (a file each).
+int launch_mx8(const RowArgs& s, const Plan& p, hipStream_t stream);
+int launch_mx4(const RowArgs& s, const Plan& p, hipStream_t stream);
 
 }  // namespace rows
 

@@ -102,7 +102,7 @@ int launch_page_plan(int64_t n, const int32_t* cached, const int32_t* fresh, con
                      int32_t* free_out, int64_t* free_count_out, void* workspace,
                      int32_t* d_status, hipStream_t stream);
 
-// A paged cache of 16-bit elements: strides in elements.
+// A paged cache: strides in elements, of 16 bits, or (in 8 and 4 bits) in bytes.
 struct PagedCache {
   int64_t page_stride, slot_stride, head_stride;
   int32_t page;
@@ -114,15 +114,41 @@ int launch_cache_store(int64_t tokens, int32_t kv_heads, int32_t dim, const void
                        void* v_cache, const PagedCache& cache, const int64_t* slots,
                        int32_t* d_status, hipStream_t stream);
 
+// The scales of a cache in 8 or 4 bits: strides in bytes.
+struct PagedScales {
+  const unsigned char* k;
+  const unsigned char* v;
+  int64_t page, slot, head;
+};
+
+// A paged cache in 8 or 4 bits, strides in bytes.
+struct MxCache {
+  void* k;
+  void* v;
+  void* k_scale;
+  void* v_scale;
+  int64_t page_stride, slot_stride, head_stride;
+  int64_t scale_page, scale_slot, scale_head;
+  int64_t n_pages;
+  int32_t page, kv_heads, dim, bits;
+};
+
+// New rows into the cache (`store`), or cached ones out of it.
+int launch_mx_move(bool store, const MxCache& cache, int64_t tokens, bool bf16, void* k, void* v,
+                   int64_t token_stride, int64_t row_head_stride, const int64_t* slots,
+                   int32_t* d_status, hipStream_t stream);
+
 struct AttnCall {
   int64_t n, tokens;
   int32_t q_heads, kv_heads, dim;
+  int32_t bits;           // of an element of the cache: 16, 8, 4
   bool bf16;
   const void* q;
   int64_t q_token, q_head;
   const void* k_cache;
   const void* v_cache;
   PagedCache cache;
+  PagedScales scales;     // where bits < 16
   const int32_t* table;
   int64_t ldt;
   const int64_t* q_offsets;

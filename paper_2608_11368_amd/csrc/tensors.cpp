@@ -2,15 +2,19 @@
 // tensors: read through the interpreter, a property takes 30 to 60 ns, the checks
 // of an argument 0.5 us and a gradient's entry 0.2 us, which is longer than small
 // calls, and the clipping of hundreds of gradients, take on the GPU.
+#define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
 #include <exception>
+#include <string.h>
 
 #include <ATen/ops/empty.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/DynamicTypes.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include "../../include/pair.h"
 
 namespace {
 
@@ -147,6 +151,56 @@ PyObject* cache(PyObject*, PyObject* const* args, Py_ssize_t n) {
   }
 }
 
+// mx_cache(k_cache, v_cache, k_scale, v_scale) -> (pair_mx_cache as bytes, heads,
+// width), or None if they are not a cache in 8 or 4 bits.
+PyObject* mx_cache(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 4) {
+    PyErr_SetString(PyExc_TypeError, "mx_cache(k_cache, v_cache, k_scale, v_scale)");
+    return nullptr;
+  }
+  for (Py_ssize_t i = 0; i < 4; ++i)
+    if (!THPVariable_Check(args[i])) Py_RETURN_NONE;
+  try {
+    const at::Tensor &k = THPVariable_Unpack(args[0]), &v = THPVariable_Unpack(args[1]),
+                     &ks = THPVariable_Unpack(args[2]), &vs = THPVariable_Unpack(args[3]);
+    const bool wide = k.scalar_type() == at::kFloat8_e4m3fn;
+    if (!k.is_cuda() || !v.is_cuda() || !ks.is_cuda() || !vs.is_cuda() || k.dim() != 4 ||
+        (!wide && k.scalar_type() != at::kFloat4_e2m1fn_x2) ||
+        v.scalar_type() != k.scalar_type() || ks.scalar_type() != at::kFloat8_e8m0fnu ||
+        vs.scalar_type() != at::kFloat8_e8m0fnu || v.sizes() != k.sizes() ||
+        v.strides() != k.strides() || ks.dim() != 4 || vs.sizes() != ks.sizes() ||
+        vs.strides() != ks.strides() || k.stride(3) != 1 ||
+        (ks.stride(3) != 1 && ks.size(3) > 1))
+      Py_RETURN_NONE;
+    const int64_t dim = wide ? k.size(3) : 2 * k.size(3);
+    if (ks.size(0) != k.size(0) || ks.size(1) != k.size(1) || ks.size(2) != k.size(2) ||
+        ks.size(3) * 32 != dim || k.size(1) > INT32_MAX || k.size(2) > INT32_MAX || dim > INT32_MAX)
+      Py_RETURN_NONE;
+    pair_mx_cache c;
+    memset(&c, 0, sizeof(c));
+    c.k = k.data_ptr();
+    c.v = v.data_ptr();
+    c.k_scale = ks.data_ptr();
+    c.v_scale = vs.data_ptr();
+    c.page_stride = k.stride(0);
+    c.slot_stride = k.stride(1);
+    c.head_stride = k.stride(2);
+    c.scale_page = ks.stride(0);
+    c.scale_slot = ks.stride(1);
+    c.scale_head = ks.stride(2);
+    c.n_pages = k.size(0);
+    c.page = (int32_t)k.size(1);
+    c.kv_heads = (int32_t)k.size(2);
+    c.dim = (int32_t)dim;
+    c.format = wide ? PAIR_MXFP8 : PAIR_MXFP4;
+    return Py_BuildValue("y#ii", reinterpret_cast<const char*>(&c), (Py_ssize_t)sizeof(c),
+                         (int)c.kv_heads, (int)c.dim);
+  } catch (...) {
+    torch::translate_exception_to_python(std::current_exception());
+    return nullptr;
+  }
+}
+
 // rows(tensor, type code, heads or 0, width) -> (address, strides of a row and a
 // head, rows, heads), or None if it is not [rows][heads][width] of that type.
 PyObject* rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -269,6 +323,9 @@ PyMethodDef kMethods[] = {
      "address(tensor, name, dtype, least=0, optional=False): a checked tensor's data pointer."},
     {"cache", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(cache)),
      METH_FASTCALL, "cache(k_cache, v_cache): addresses and layout, None if it is no cache."},
+    {"mx_cache", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(mx_cache)),
+     METH_FASTCALL,
+     "mx_cache(k_cache, v_cache, k_scale, v_scale): (pair_mx_cache, heads, width), or None."},
     {"rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(rows)),
      METH_FASTCALL, "rows(tensor, type code, heads, width): address and layout, or None."},
     {"parts", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(parts)),
