@@ -756,8 +756,8 @@ int pair_cache_load_mx(const pair_mx_cache* cache, int64_t tokens, const int64_t
 
 /* pair_paged_attention_mx_workspace_bytes -- device workspace of pair_paged_attention_mx. */
 size_t pair_paged_attention_mx_workspace_bytes(int64_t n, int64_t tokens, int32_t q_heads,
-                                               int32_t kv_heads, int32_t dim, int32_t max_q,
-                                               int32_t max_len);
+                                               int32_t kv_heads, int32_t dim, int32_t format,
+                                               int32_t max_q, int32_t max_len);
 
 /*
  * pair_paged_attention_mx -- pair_paged_attention over a cache in 8 or 4 bits: the

@@ -153,7 +153,8 @@ def lib() -> ctypes.CDLL:
         L.pair_cache_store_mx.restype = ctypes.c_int
         L.pair_cache_load_mx.argtypes = [P, i64, P, i32, P, P, i64, i64, P, P]
         L.pair_cache_load_mx.restype = ctypes.c_int
-        L.pair_paged_attention_mx_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32, i32]
+        L.pair_paged_attention_mx_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32, i32,
+                                                              i32]
         L.pair_paged_attention_mx_workspace_bytes.restype = size
         L.pair_paged_attention_mx.argtypes = [P, i64, i64, i32, i32, P, i64, i64, P, i64, P, P, i32,
                                               i32, f32, P, i64, i64, P, P, size, P, P]
@@ -592,10 +593,10 @@ def pair_cache_load_mx(slots, k_cache, v_cache, k_scale, v_scale, k, v, d_status
     native.written(k, v)
 
 
-def pair_paged_attention_mx_workspace_bytes(n, tokens, q_heads, kv_heads, dim, max_q,
+def pair_paged_attention_mx_workspace_bytes(n, tokens, q_heads, kv_heads, dim, format, max_q,
                                             max_len) -> int:
     return int(lib().pair_paged_attention_mx_workspace_bytes(n, tokens, q_heads, kv_heads, dim,
-                                                             max_q, max_len))
+                                                             format, max_q, max_len))
 
 
 def pair_paged_attention_mx(q, k_cache, v_cache, k_scale, v_scale, table, q_offsets, lens, max_q,
@@ -896,6 +897,11 @@ def _attention_workspace(device, *sizes):
     return pair_paged_attention_workspace_bytes(*sizes)
 
 
+@functools.lru_cache(maxsize=256)
+def _attention_mx_workspace(device, *sizes):
+    return pair_paged_attention_mx_workspace_bytes(*sizes)
+
+
 @_allocating
 def page_plan(cached, fresh, table, free_pages, free_count, page, max_tokens, mask=None,
               stream=None):
@@ -1040,8 +1046,9 @@ def paged_attention_mx(q, k_cache, v_cache, k_scale, v_scale, table, q_offsets, 
     if want_lse:
         lse, = parts(index, torch.float32, (tokens, heads))
     max_q, max_len = int(max_q), int(max_len)
-    need = _attention_workspace(_device_index(), lens.numel(), tokens, heads, k_cache.shape[2], dim,
-                                max_q, max_len)
+    need = _attention_mx_workspace(_device_index(), lens.numel(), tokens, heads, k_cache.shape[2],
+                                   dim, PAIR_MXFP8 if k_cache.dtype == _MX_CODES[0] else PAIR_MXFP4,
+                                   max_q, max_len)
     if workspace is None or workspace.numel() < need:
         workspace, = parts(index, torch.uint8, need)
     st = _status(q.device)

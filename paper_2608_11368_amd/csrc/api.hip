@@ -451,7 +451,7 @@ int pair_cache_store(int64_t tokens, int32_t kv_heads, int32_t dim, int32_t dtyp
 }
 
 static int check_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads,
-                           int32_t dim, int32_t max_q, int32_t max_len) {
+                           int32_t dim, int32_t bits, int32_t max_q, int32_t max_len) {
   if (n < 1 || n > kMaxRequests || tokens < 0 || tokens > kMaxSlots) return PAIR_ERANGE;
   if (kv_heads < 1 || kv_heads > kMaxHeads || q_heads < kv_heads || q_heads % kv_heads != 0 ||
       q_heads / kv_heads > 64)
@@ -464,7 +464,7 @@ static int check_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t k
   // than a call has beside some thousands, are far from a launch's 2^24.
   if ((2 * n + tokens) * q_heads > (int64_t)1 << 22 &&
       pair::too_many_threads(
-          pair::attention_groups(n, tokens, q_heads, kv_heads, dim, max_q, max_len), 256))
+          pair::attention_groups(n, tokens, q_heads, kv_heads, dim, bits, max_q, max_len), 256))
     return PAIR_ERANGE;
   return PAIR_OK;
 }
@@ -472,8 +472,8 @@ static int check_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t k
 size_t pair_paged_attention_workspace_bytes(int64_t n, int64_t tokens, int32_t q_heads,
                                             int32_t kv_heads, int32_t dim, int32_t max_q,
                                             int32_t max_len) {
-  if (check_attention(n, tokens, q_heads, kv_heads, dim, max_q, max_len)) return 0;
-  return pair::attention_workspace_bytes(n, tokens, q_heads, kv_heads, dim, max_q, max_len);
+  if (check_attention(n, tokens, q_heads, kv_heads, dim, 16, max_q, max_len)) return 0;
+  return pair::attention_workspace_bytes(n, tokens, q_heads, kv_heads, dim, 16, max_q, max_len);
 }
 
 // What the attention's calls share: `c` has the cache, already checked, and dim,
@@ -498,8 +498,8 @@ static int attention(pair::AttnCall c, int64_t n, int64_t tokens, int32_t q_head
   Strided results[] = {{tokens, out_token}, {q_heads, out_head}};
   if (rows_overlap(results, c.dim)) return PAIR_EINVAL;
   if (bad_workspace(workspace, ws_bytes,
-                    pair::attention_workspace_bytes(n, tokens, q_heads, c.kv_heads, c.dim, max_q,
-                                                    max_len)))
+                    pair::attention_workspace_bytes(n, tokens, q_heads, c.kv_heads, c.dim, c.bits,
+                                                    max_q, max_len)))
     return PAIR_EWORKSPACE;
   c.n = n;
   c.tokens = tokens;
@@ -532,7 +532,7 @@ int pair_paged_attention(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_
                          void* out, int64_t out_token, int64_t out_head, float* lse,
                          void* workspace, size_t ws_bytes, int32_t* d_status, void* stream) {
   if (dtype != PAIR_BF16 && dtype != PAIR_F16) return PAIR_EDTYPE;
-  int st = check_attention(n, tokens, q_heads, kv_heads, dim, max_q, max_len);
+  int st = check_attention(n, tokens, q_heads, kv_heads, dim, 16, max_q, max_len);
   if (st) return st;
   st = check_cache(k_cache, v_cache, page_stride, slot_stride, head_stride, page, n_pages);
   if (st) return st;
@@ -631,9 +631,12 @@ int pair_cache_load_mx(const pair_mx_cache* cache, int64_t tokens, const int64_t
 }
 
 size_t pair_paged_attention_mx_workspace_bytes(int64_t n, int64_t tokens, int32_t q_heads,
-                                               int32_t kv_heads, int32_t dim, int32_t max_q,
-                                               int32_t max_len) {
-  return pair_paged_attention_workspace_bytes(n, tokens, q_heads, kv_heads, dim, max_q, max_len);
+                                               int32_t kv_heads, int32_t dim, int32_t format,
+                                               int32_t max_q, int32_t max_len) {
+  if (format != PAIR_MXFP8 && format != PAIR_MXFP4) return 0;
+  const int32_t bits = format == PAIR_MXFP8 ? 8 : 4;
+  if (check_attention(n, tokens, q_heads, kv_heads, dim, bits, max_q, max_len)) return 0;
+  return pair::attention_workspace_bytes(n, tokens, q_heads, kv_heads, dim, bits, max_q, max_len);
 }
 
 int pair_paged_attention_mx(const pair_mx_cache* cache, int64_t n, int64_t tokens, int32_t q_heads,
@@ -646,7 +649,7 @@ int pair_paged_attention_mx(const pair_mx_cache* cache, int64_t n, int64_t token
   pair::MxCache m;
   int st = check_mx(cache, &m);
   if (st) return st;
-  st = check_attention(n, tokens, q_heads, m.kv_heads, m.dim, max_q, max_len);
+  st = check_attention(n, tokens, q_heads, m.kv_heads, m.dim, m.bits, max_q, max_len);
   if (st) return st;
   pair::AttnCall c = {};
   c.kv_heads = m.kv_heads;

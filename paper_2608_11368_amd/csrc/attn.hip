@@ -34,16 +34,17 @@ bool together(const AttnCall& a) {
 }  // namespace
 
 int64_t attention_groups(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads,
-                         int32_t dim, int32_t max_q, int32_t max_len) {
-  const int64_t rows = attention_rows_groups(n, q_heads, kv_heads, dim, max_q, max_len);
+                         int32_t dim, int32_t bits, int32_t max_q, int32_t max_len) {
+  const int64_t rows = attention_rows_groups(n, q_heads, kv_heads, dim, bits, max_q, max_len);
   if (most_rows(q_heads, kv_heads, max_q) <= kRowsMost) return rows;
   return (has_few(n, tokens, max_q) ? rows : 0) +
          attention_tiles_groups(n, tokens, q_heads, kv_heads, dim, max_len);
 }
 
 size_t attention_workspace_bytes(int64_t n, int64_t tokens, int32_t q_heads, int32_t kv_heads,
-                                 int32_t dim, int32_t max_q, int32_t max_len) {
-  const size_t rows = rounded(attention_rows_workspace(n, q_heads, kv_heads, dim, max_q, max_len));
+                                 int32_t dim, int32_t bits, int32_t max_q, int32_t max_len) {
+  const size_t rows =
+      rounded(attention_rows_workspace(n, q_heads, kv_heads, dim, bits, max_q, max_len));
   if (most_rows(q_heads, kv_heads, max_q) <= kRowsMost) return rows;
   return (has_few(n, tokens, max_q) ? rows : 0) +
          rounded(attention_tiles_workspace(n, tokens, q_heads, kv_heads, dim, max_len));
@@ -56,7 +57,7 @@ int launch_attention(const AttnCall& a, void* workspace, hipStream_t stream) {
     return launch_attention_tiles(a, 0, nullptr, workspace, stream);
   void* few = workspace;
   void* tiles = static_cast<unsigned char*>(workspace) +
-                rounded(attention_rows_workspace(a.n, a.q_heads, a.kv_heads, a.dim, a.max_q,
+                rounded(attention_rows_workspace(a.n, a.q_heads, a.kv_heads, a.dim, a.bits, a.max_q,
                                                  a.max_len));
   if (together(a))
     return launch_attention_tiles(a, kRowsMost + 1, few, tiles, stream);

@@ -85,8 +85,8 @@ __global__ __launch_bounds__(kThreads) void join_rows_kernel(RowArgs s, int rows
 
 }  // namespace
 
-Plan rows::plan_of(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim, int32_t max_q,
-                   int32_t max_len) {
+Plan rows::plan_of(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim, int32_t bits,
+                   int32_t max_q, int32_t max_len) {
   Plan p;
   const int64_t rows = (int64_t)max_q * (q_heads / kv_heads);
   p.rows = (int)(rows < kRowsMost ? rows : kRowsMost);
@@ -97,7 +97,8 @@ Plan rows::plan_of(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim, in
   // requests of 1000: 22 and 27), or the requests are so many that they fill the
   // card by themselves.
   const int64_t most = n * ((max_len + kUnit - 1) / kUnit);
-  int64_t runs = 2 * (int64_t)device_cu_count() / kv_heads;   // two workgroups fit a compute unit
+  const int per_cu = p.tiles == 1 ? groups_per_cu(bits, dim) : 2;
+  int64_t runs = per_cu * (int64_t)device_cu_count() / kv_heads;
   if (runs > most) runs = most;
   if (runs > kMostRuns) runs = kMostRuns;
   if (runs < 1) runs = 1;
@@ -138,18 +139,18 @@ int rows::join_rows(const RowArgs& s, const Plan& p, hipStream_t stream) {
 }
 
 size_t attention_rows_workspace(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim,
-                                int32_t max_q, int32_t max_len) {
-  return plan_of(n, q_heads, kv_heads, dim, max_q, max_len).total;
+                                int32_t bits, int32_t max_q, int32_t max_len) {
+  return plan_of(n, q_heads, kv_heads, dim, bits, max_q, max_len).total;
 }
 
 int64_t attention_rows_groups(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim,
-                              int32_t max_q, int32_t max_len) {
-  const Plan p = plan_of(n, q_heads, kv_heads, dim, max_q, max_len);
+                              int32_t bits, int32_t max_q, int32_t max_len) {
+  const Plan p = plan_of(n, q_heads, kv_heads, dim, bits, max_q, max_len);
   return (p.runs > n ? p.runs : n) * kv_heads;       // the joins: one for a request and head
 }
 
 int launch_attention_rows(const AttnCall& a, void* workspace, hipStream_t stream) {
-  const Plan p = plan_of(a.n, a.q_heads, a.kv_heads, a.dim, a.max_q, a.max_len);
+  const Plan p = plan_of(a.n, a.q_heads, a.kv_heads, a.dim, a.bits, a.max_q, a.max_len);
   const RowArgs s = args_of(a, p, workspace);
   if (a.bits == 8) return launch_mx8(s, p, stream);
   if (a.bits == 4) return launch_mx4(s, p, stream);

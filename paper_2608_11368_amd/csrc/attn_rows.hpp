@@ -50,6 +50,7 @@ constexpr int kWideWaves = 2 * kWaves;      // of a workgroup that has a compute
 constexpr int kMostScanned = 2048;
 constexpr int kMostRuns = 1024;
 constexpr float kLazy = 8.0f;
+constexpr uint32_t kXcds = 8;
 
 struct RowArgs {
   AttnCall a;
@@ -124,18 +125,31 @@ __device__ __forceinline__ int key_place(int row, int b) {
   return row * (DIM * 2) + ((((b >> 4) ^ row) & (DIM / 8 - 1)) << 4) + (b & 15);
 }
 
-// LDS of one wave: a block's keys, the values and weights of an odd one, or the
-// wave's sums.
+// LDS of one wave: a block's keys (in 8 and 4 bits its keys' and values' codes), the
+// values and weights of an odd one, or the wave's sums.
 template <int BITS, int DIM, int NT>
 struct WaveLds {
+  static constexpr int kRowBytes = DIM * BITS / 8;
   union {
     float sum[16][DIM + 4];
     unsigned char key[kBlock * DIM * 2];
+    unsigned char codes[2 * kBlock * kRowBytes];
     uint16_t value[kBlock][DIM];
   };
   uint32_t weight[NT][16][kBlock / 2];
   float stat[16][2];
-  uint32_t scale[2][BITS == 16 ? 1 : kBlock];   // of a block's keys and values: a row's bytes
+  uint32_t scale[BITS == 16 ? 1 : 2 * kBlock];   // of a block's keys and values: each row's bytes
+
+  // Piece `c` of 16 bytes of key `y`: permuted by the row so that eight rows'
+  // pieces at one place lie in different banks.
+  static __device__ __forceinline__ int key_at(int y, int c) {
+    const int turn = kRowBytes == 128 ? y & 7 : kRowBytes == 64 ? (y >> 2) & 3 : 0;
+    return y * kRowBytes + ((c ^ turn) << 4);
+  }
+  // Value `y`: rows 4 g + i of a tile, of which an instruction reads one i, side by side.
+  static __device__ __forceinline__ int value_at(int y) {
+    return (kBlock + (y & 16) + (y & 3) * 4 + ((y >> 2) & 3)) * kRowBytes;
+  }
 };
 
 // A block whose values are not all finite and not all seen by every row: each
@@ -178,23 +192,131 @@ __device__ __forceinline__ void add_odd_block(WaveLds<BITS, DIM, NT>* lds, const
   wave_lds_order();
 }
 
-template <int BITS, bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
+// A block's scores of this lane's rows (keys 16 t + 4 g + i) and its values, piece
+// x of eight rows: their share of the sums.
+template <int BITS, bool BF16, int DIM, int NT>
+__device__ __forceinline__ void weigh_block(const RowArgs& s, const f32x4_t (&sc)[NT][2],
+                                            const int (&limit)[NT], int first_limit, int len,
+                                            int kb, Piece<DIM> (&vr)[8],
+                                            WaveLds<BITS, DIM, NT>* lds, State<DIM, NT>* st) {
+  constexpr int ND = DIM / 16;       // dims of a lane's piece of a value row
+  const int g = (threadIdx.x & (kWave - 1)) >> 4;
+  float p[NT][8];
+  const bool masked = kb + kBlock - 1 > first_limit;   // some row does not see some key
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[nt][e] = sc[nt][e >> 2][e & 3] * s.scale_log2;
+    if (masked) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (kb + 16 * (e >> 2) + 4 * g + (e & 3) > limit[nt]) p[nt][e] = -INFINITY;
+    }
+    float top = p[nt][0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) top = fmaxf(top, p[nt][e]);
+    if (__any(top > st->m[nt] + kLazy)) {
+      top = fmaxf(top, __shfl_xor(top, 16, kWave));
+      top = fmaxf(top, __shfl_xor(top, 32, kWave));
+      const float mn = fmaxf(st->m[nt], top);
+      const float keep = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st->m[nt] - mn);
+      st->m[nt] = mn;
+      st->l[nt] *= keep;
+#pragma unroll
+      for (int j = 0; j < ND; ++j) st->acc[nt][j] *= keep;
+    }
+    const float base = (st->m[nt] == -INFINITY ? 0.0f : st->m[nt]) - kLift<BF16>;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      p[nt][e] = __builtin_amdgcn_exp2f(p[nt][e] - base);
+      st->l[nt] += p[nt][e];
+    }
+  }
+
+  u32x4_t pf[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) pf[nt][w] = pack2<BF16>(p[nt][2 * w], p[nt][2 * w + 1]);
+  // Values that some row must not see: past the end they are no values at
+  // all, and within the chunk a weight of zero does not hide a NaN or an
+  // infinity from the matrix product.
+  if (masked) {
+    uint32_t bad = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int key = kb + 16 * (e >> 2) + 4 * g + (e & 3);
+#pragma unroll
+      for (int w = 0; w < ND / 2; ++w) {
+        if (key >= len) vr[e].w[w] = 0u;
+        bad |= not_finite<BF16>(vr[e].w[w]) ? 1u : 0u;
+      }
+    }
+    if (__any(bad != 0u)) add_odd_block<BITS, BF16, DIM, NT>(lds, pf, kb, limit, &vr, st);
+  }
+
+#pragma unroll
+  for (int j = 0; j < ND; ++j) {
+    u32x4_t vt;                                   // dim j of this lane's eight keys
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      vt[w] = __builtin_amdgcn_perm(vr[2 * w + 1].w[j >> 1], vr[2 * w].w[j >> 1],
+                                    (j & 1) ? 0x07060302u : 0x05040100u);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) st->acc[nt][j] = mma16<BF16>(vt, pf[nt], st->acc[nt][j]);
+  }
+}
+
+// A block's keys and values, piece x of eight rows: its scores, and its share of
+// the sums.
+template <bool BF16, int DIM, int NT>
+__device__ __forceinline__ void add_block(const RowArgs& s, const u32x4_t (&qf)[NT][DIM / 32],
+                                          const int (&limit)[NT], int first_limit, int len, int kb,
+                                          const Piece<DIM> (&kr)[8], Piece<DIM> (&vr)[8],
+                                          WaveLds<16, DIM, NT>* lds, State<DIM, NT>* st) {
+  constexpr int NC = DIM / 32;       // 32-dim pieces of a key row
+  const int lane = threadIdx.x & (kWave - 1);
+  const int x = lane & 15, g = lane >> 4;
+
+  // keys through LDS: whole rows come from memory, the product wants a row's
+  // piece from every lane
+  wave_lds_order();
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int y = 16 * (e >> 2) + 4 * g + (e & 3);
+    kr[e].store(lds->key + key_place<DIM>(y, x * (DIM / 8)));
+  }
+  wave_lds_order();
+  f32x4_t sc[NT][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) sc[nt][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const u32x4_t kf = *reinterpret_cast<const u32x4_t*>(
+          lds->key + key_place<DIM>(16 * t + x, 64 * c + 16 * g));
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) sc[nt][t] = mma16<BF16>(kf, qf[nt][c], sc[nt][t]);
+    }
+  weigh_block<16, BF16, DIM, NT>(s, sc, limit, first_limit, len, kb, vr, lds, st);
+}
+
+template <bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
 __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[NT][DIM / 32],
                                          const int (&limit)[NT], int first_limit, int64_t r,
                                          int64_t kvh, int len, int k0, int k1,
-                                         WaveLds<BITS, DIM, NT>* lds, State<DIM, NT>* st) {
-  constexpr int NC = DIM / 32;       // 32-dim pieces of a key row
-  constexpr int ND = DIM / 16;       // dims of a lane's piece of a value row
+                                         WaveLds<16, DIM, NT>* lds, State<DIM, NT>* st) {
   const int lane = threadIdx.x & (kWave - 1);
   const int x = lane & 15, g = lane >> 4;
-  constexpr int kUnitBytes = BITS == 16 ? 2 : 1;      // of the cache's strides
-  const int64_t head = kvh * s.a.cache.head_stride * kUnitBytes;
+  const int64_t head = kvh * s.a.cache.head_stride * 2;
   const unsigned char* kbase = static_cast<const unsigned char*>(s.a.k_cache) + head;
   const unsigned char* vbase = static_cast<const unsigned char*>(s.a.v_cache) + head;
-  const int64_t slot_bytes = s.a.cache.slot_stride * kUnitBytes;
-  const int64_t page_bytes = s.a.cache.page_stride * kUnitBytes;
+  const int64_t slot_bytes = s.a.cache.slot_stride * 2, page_bytes = s.a.cache.page_stride * 2;
   const int32_t* row = s.a.table + r * s.a.ldt;
-  const int64_t lane_off = x * (DIM / 16 * BITS / 8) + (ALIGNED ? 4 * g * slot_bytes : 0);
+  const int64_t lane_off = x * (DIM / 8) + (ALIGNED ? 4 * g * slot_bytes : 0);
 
   // A lane reads piece x of eight rows, the same of keys and values.  Pages are
   // looked up a step before: one per tile of 16 keys where pages are multiples
@@ -220,7 +342,6 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
   if (k0 < k1) lookup(k0);
   for (int kb = k0; kb < k1; kb += kBlock * WAVES) {
     Piece<DIM> kr[8], vr[8];
-    Codes<BITS, DIM / 16> kc[8], vc[8];
     int64_t at[kIds];
 #pragma unroll
     for (int n = 0; n < kIds; ++n) {
@@ -228,139 +349,183 @@ __device__ __forceinline__ void add_keys(const RowArgs& s, const u32x4_t (&qf)[N
       at[n] = checked_page(s.a, id[n], &bad_page) * page_bytes +
               (int64_t)(key - div_by(key, s.page) * s.page.d) * slot_bytes + lane_off;
     }
-    uint32_t scales = 0;
-    if constexpr (BITS != 16) {          // lane: those of one key, or of its value
-      const int y = lane & (kBlock - 1);
-      const uint32_t key = (uint32_t)(kb + y < len ? kb + y : len - 1);
-      const uint32_t pg = div_by(key, s.page);
-      const int32_t page = ALIGNED ? (y < 16 ? id[0] : id[kIds - 1]) : row[pg];
-      const unsigned char* from = (lane < kBlock ? s.a.scales.k : s.a.scales.v) +
-                                  checked_page(s.a, page, &bad_page) * s.a.scales.page +
-                                  (int64_t)(key - pg * s.page.d) * s.a.scales.slot +
-                                  kvh * s.a.scales.head;
-      scales = DIM == 128 ? *reinterpret_cast<const uint32_t*>(from)
-                          : *reinterpret_cast<const uint16_t*>(from);
-    }
-    if constexpr (BITS == 16) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        kr[e].load(kbase + at[ALIGNED ? e >> 2 : e] + (ALIGNED ? (e & 3) * slot_bytes : 0));
+    for (int e = 0; e < 8; ++e)
+      kr[e].load(kbase + at[ALIGNED ? e >> 2 : e] + (ALIGNED ? (e & 3) * slot_bytes : 0));
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        vr[e].load(vbase + at[ALIGNED ? e >> 2 : e] + (ALIGNED ? (e & 3) * slot_bytes : 0));
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        kc[e].load_once(kbase + at[ALIGNED ? e >> 2 : e] + (ALIGNED ? (e & 3) * slot_bytes : 0));
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        vc[e].load_once(vbase + at[ALIGNED ? e >> 2 : e] + (ALIGNED ? (e & 3) * slot_bytes : 0));
-    }
+    for (int e = 0; e < 8; ++e)
+      vr[e].load(vbase + at[ALIGNED ? e >> 2 : e] + (ALIGNED ? (e & 3) * slot_bytes : 0));
     if (kb + kBlock * WAVES < k1) lookup(kb + kBlock * WAVES);
+    add_block<BF16, DIM, NT>(s, qf, limit, first_limit, len, kb, kr, vr, lds, st);
+  }
+  if (bad_page) raise_status(s.a.d_status, bad_page);
+}
 
-    // keys through LDS: whole rows come from memory, the product wants a row's
-    // piece from every lane
-    wave_lds_order();
-    if constexpr (BITS != 16) {
-      lds->scale[lane / kBlock][lane & (kBlock - 1)] = scales;
-      wave_lds_order();
-      const int b = 8 * (x * (DIM / 16) / kMxBlock);
+// The same as add_keys over a cache in 8 or 4 bits.  A wave's loads are contiguous,
+// 16 bytes a lane; codes pass through the wave's LDS and are converted when they are
+// read from it.  The products' k index takes a key's elements in the order in which
+// a lane has those of one block (with the queries alike), so that it needs one scale.
+// The next block is on its way while one is used: a block has a half or a quarter of
+// the bytes, too few in flight otherwise (4 bits: 226 us without, 203 with one ahead,
+// 203 with two; 256 requests of 4000 keys, 8 heads of 128).
+//
+// The matrix instructions that take codes and scales as they are were measured and
+// not taken: their sums are not those of 32 bits (off by up to 2^-12 of the largest
+// product, 2^-19 of the sum of magnitudes in the mean square).
+template <int BITS, bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
+__device__ __forceinline__ void add_codes(const RowArgs& s,
+                                          const u32x4_t (&qf)[NT][DIM / 32],
+                                          const int (&limit)[NT], int first_limit, int64_t r,
+                                          int64_t kvh, int len, int k0, int k1,
+                                          WaveLds<BITS, DIM, NT>* lds, State<DIM, NT>* st) {
+  using Lds = WaveLds<BITS, DIM, NT>;
+  constexpr int W = DIM * BITS / 8;                        // bytes of a row
+  constexpr int kLoads = kBlock * W / 1024;                // of keys, and of values
+  constexpr int kRowLanes = W / 16;
+  constexpr int kStep = kBlock * WAVES;
+  // Not beside two tiles of rows, which leave no registers for it (five drafted tokens
+  // of 2 requests of 131,000 keys, 32 query heads on 8, in 8 bits: 128 us with
+  // registers spilled, 97 without).
+  constexpr bool kAhead = NT == 1;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int x = lane & 15, g = lane >> 4;
+  const int64_t head = kvh * s.a.cache.head_stride;
+  const unsigned char* kbase = static_cast<const unsigned char*>(s.a.k_cache) + head;
+  const unsigned char* vbase = static_cast<const unsigned char*>(s.a.v_cache) + head;
+  const unsigned char* sbase =                             // those of a key, or of its value
+      (lane < kBlock ? s.a.scales.k : s.a.scales.v) + kvh * s.a.scales.head;
+  const int64_t slot_bytes = s.a.cache.slot_stride, page_bytes = s.a.cache.page_stride;
+  const int32_t* row = s.a.table + r * s.a.ldt;
+  const int my_row = lane / kRowLanes, my_piece = lane % kRowLanes;   // of a load
+  const int s_row = lane & (kBlock - 1);
+  const int v_turn = (8 * (x * (DIM / 16) / kMxBlock) + 9) & 31;
+
+  // Pages of a block's tiles, or (pages not of a multiple of 16) of this lane's
+  // rows, the last for its scales; looked up a step before.
+  constexpr int kIds = ALIGNED ? 2 : kLoads + 1;
+  int32_t id[kIds];
+  int32_t bad_page = 0;
+  auto key_of = [&](int kb, int n) {
+    if (ALIGNED) {                       // a tile past the end repeats the last
+      const int key = kb + 16 * n;
+      return uniform(key < len ? key : (len - 1) & ~15);
+    }
+    const int key = kb + (n < kLoads ? n * (kWave / kRowLanes) + my_row : s_row);
+    return key < len ? key : len - 1;
+  };
+  auto lookup = [&](int kb) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const u32x4_t kb4 = *reinterpret_cast<const u32x4_t*>(&lds->scale[0][16 * t + 4 * g]);
-        const u32x4_t vb4 = *reinterpret_cast<const u32x4_t*>(&lds->scale[1][16 * t + 4 * g]);
+    for (int n = 0; n < kIds; ++n) {
+      const uint32_t pg = div_by((uint32_t)key_of(kb, n), s.page);
+      id[n] = ALIGNED ? table_entry(row, pg) : row[pg];
+    }
+  };
+  struct Ahead {
+    u32x4_t k[kLoads], v[kLoads];
+    uint32_t scales;
+  };
+  Ahead ahead;
+  // ALIGNED: a tile's place is scalar, a lane's place in it the same for every tile.
+  const int64_t lane_at = (ALIGNED ? (my_row & 15) * slot_bytes : 0) + my_piece * 16;
+  const unsigned char* s_at = sbase + (ALIGNED ? (s_row & 15) * s.a.scales.slot : 0);
+  auto fetch = [&](int kb) {
+    int64_t place[kIds], scale_place[kIds];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          kc[4 * t + i].template values<BF16>(mx_scale((kb4[i] >> b) & 255u), kr[4 * t + i].w);
-          vc[4 * t + i].template values<BF16>(mx_scale((vb4[i] >> b) & 255u), vr[4 * t + i].w);
-        }
-      }
+    for (int n = 0; n < kIds; ++n) {
+      const uint32_t key = (uint32_t)key_of(kb, n);
+      const int64_t pg = checked_page(s.a, id[n], &bad_page);
+      const int64_t y = key - div_by(key, s.page) * s.page.d;          // slot in the page
+      place[n] = pg * page_bytes + y * slot_bytes;
+      scale_place[n] = pg * s.a.scales.page + y * s.a.scales.slot;
+    }
+    const unsigned char* scales =
+        s_at + (ALIGNED && (s_row & 16) == 0 ? scale_place[0] : scale_place[kIds - 1]);
+    ahead.scales = DIM == 128 ? *reinterpret_cast<const uint32_t*>(scales)
+                               : *reinterpret_cast<const uint16_t*>(scales);
+    int64_t at[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      int64_t from = place[ALIGNED ? j * (kWave / kRowLanes) / 16 : j];
+      if (ALIGNED && kLoads == 1 && my_row >= 16) from = place[kIds - 1];
+      if (ALIGNED && kLoads > 2 && j % 2 == 1) from += 8 * slot_bytes;  // half a tile a load
+      at[j] = from + lane_at;
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int y = 16 * (e >> 2) + 4 * g + (e & 3);
-      kr[e].store(lds->key + key_place<DIM>(y, x * (DIM / 8)));
-    }
+    for (int j = 0; j < kLoads; ++j)
+      ahead.k[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(kbase + at[j]));
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+      ahead.v[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(vbase + at[j]));
+  };
+  auto use = [&](int kb) {
     wave_lds_order();
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int y = j * (kWave / kRowLanes) + my_row;
+      *reinterpret_cast<u32x4_t*>(lds->codes + Lds::key_at(y, my_piece)) = ahead.k[j];
+      *reinterpret_cast<u32x4_t*>(lds->codes + Lds::value_at(y) + my_piece * 16) = ahead.v[j];
+    }
+    lds->scale[lane] = ahead.scales;
+    wave_lds_order();
+    const int next = kb + kStep;
+    if (kAhead && next < k1) {
+      fetch(next);
+      if (next + kStep < k1) lookup(next + kStep);
+    }
     f32x4_t sc[NT][2];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int t = 0; t < 2; ++t) {
+      const int y = 16 * t + x;
+      Codes<BITS, DIM / 4> c;            // elements DIM / 4 * g .. of key x of the tile
+      if constexpr (Lds::kRowBytes == 32) {
+        c.load(lds->codes + Lds::key_at(y, g >> 1) + (g & 1) * 8);
+      } else {
+        constexpr int kOwn = W / 64;     // pieces
 #pragma unroll
-      for (int t = 0; t < 2; ++t) sc[nt][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < kOwn; ++j) {
+          const u32x4_t v = *reinterpret_cast<const u32x4_t*>(
+              lds->codes + Lds::key_at(y, kOwn * g + j));
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const u32x4_t kf = *reinterpret_cast<const u32x4_t*>(
-            lds->key + key_place<DIM>(16 * t + x, 64 * c + 16 * g));
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) sc[nt][t] = mma16<BF16>(kf, qf[nt][c], sc[nt][t]);
-      }
-
-    float p[NT][8];
-    const bool masked = kb + kBlock - 1 > first_limit;   // some row does not see some key
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[nt][e] = sc[nt][e >> 2][e & 3] * s.scale_log2;
-      if (masked) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (kb + 16 * (e >> 2) + 4 * g + (e & 3) > limit[nt]) p[nt][e] = -INFINITY;
-      }
-      float top = p[nt][0];
-#pragma unroll
-      for (int e = 1; e < 8; ++e) top = fmaxf(top, p[nt][e]);
-      if (__any(top > st->m[nt] + kLazy)) {
-        top = fmaxf(top, __shfl_xor(top, 16, kWave));
-        top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        const float mn = fmaxf(st->m[nt], top);
-        const float keep = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(st->m[nt] - mn);
-        st->m[nt] = mn;
-        st->l[nt] *= keep;
-#pragma unroll
-        for (int j = 0; j < ND; ++j) st->acc[nt][j] *= keep;
-      }
-      const float base = (st->m[nt] == -INFINITY ? 0.0f : st->m[nt]) - kLift<BF16>;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[nt][e] = __builtin_amdgcn_exp2f(p[nt][e] - base);
-        st->l[nt] += p[nt][e];
-      }
-    }
-
-    u32x4_t pf[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) pf[nt][w] = pack2<BF16>(p[nt][2 * w], p[nt][2 * w + 1]);
-    // Values that some row must not see: past the end they are no values at
-    // all, and within the chunk a weight of zero does not hide a NaN or an
-    // infinity from the matrix product.
-    if (masked) {
-      uint32_t bad = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int key = kb + 16 * (e >> 2) + 4 * g + (e & 3);
-#pragma unroll
-        for (int w = 0; w < ND / 2; ++w) {
-          if (key >= len) vr[e].w[w] = 0u;
-          bad |= not_finite<BF16>(vr[e].w[w]) ? 1u : 0u;
+          for (int w = 0; w < 4; ++w) c.w[4 * j + w] = v[w];
         }
       }
-      if (__any(bad != 0u)) add_odd_block<BITS, BF16, DIM, NT>(lds, pf, kb, limit, &vr, st);
+      uint32_t kf[DIM / 8];
+      c.template values<BF16>(mx_scale(reinterpret_cast<const unsigned char*>(
+                                  &lds->scale[y])[g * (DIM / 4) / kMxBlock]), kf);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        sc[nt][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < DIM / 32; ++j)
+          sc[nt][t] = mma16<BF16>(u32x4_t{kf[4 * j], kf[4 * j + 1], kf[4 * j + 2], kf[4 * j + 3]},
+                                  qf[nt][j], sc[nt][t]);
+      }
     }
-
+    Piece<DIM> vr[8];
 #pragma unroll
-    for (int j = 0; j < ND; ++j) {
-      u32x4_t vt;                                   // dim j of this lane's eight keys
+    for (int t = 0; t < 2; ++t) {
+      const u32x4_t four = *reinterpret_cast<const u32x4_t*>(&lds->scale[kBlock + 16 * t + 4 * g]);
 #pragma unroll
-      for (int w = 0; w < 4; ++w)
-        vt[w] = __builtin_amdgcn_perm(vr[2 * w + 1].w[j >> 1], vr[2 * w].w[j >> 1],
-                                      (j & 1) ? 0x07060302u : 0x05040100u);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) st->acc[nt][j] = mma16<BF16>(vt, pf[nt], st->acc[nt][j]);
+      for (int i = 0; i < 4; ++i) {      // the block's byte where a float's exponent is
+        Codes<BITS, DIM / 16> c;
+        c.load(lds->codes + Lds::value_at(16 * t + 4 * g + i) + x * (W / 16));
+        c.template values<BF16>(
+            __uint_as_float(__builtin_amdgcn_alignbit(four[i], four[i], v_turn)), vr[4 * t + i].w);
+      }
     }
+    weigh_block<BITS, BF16, DIM, NT>(s, sc, limit, first_limit, len, kb, vr, lds, st);
+  };
+  if (k0 < k1) lookup(k0);
+  if (kAhead && k0 < k1) {
+    fetch(k0);
+    if (k0 + kStep < k1) lookup(k0 + kStep);
+  }
+  for (int kb = k0; kb < k1; kb += kStep) {
+    if (!kAhead) {
+      fetch(kb);
+      if (kb + kStep < k1) lookup(kb + kStep);
+    }
+    use(kb);
   }
   if (bad_page) raise_status(s.a.d_status, bad_page);
 }
@@ -392,17 +557,24 @@ __device__ __forceinline__ void attend(const RowArgs& s, int64_t r, int kvh, int
 #pragma unroll
     for (int c = 0; c < DIM / 32; ++c) qf[nt][c] = u32x4_t{0u, 0u, 0u, 0u};
     if (i < rows) {
+      // elements 32 c + 8 g .., as the products take a key's; add_codes' order
+      constexpr int kLane = BITS == 16 ? 8 : DIM / 4, kNext = BITS == 16 ? 32 : 8;
       const uint16_t* p = static_cast<const uint16_t*>(s.a.q) + (q.q0 + tok) * s.a.q_token +
-                          (kvh * (int)s.group.d + i - tok * (int)s.group.d) * s.a.q_head + g * 8;
+                          (kvh * (int)s.group.d + i - tok * (int)s.group.d) * s.a.q_head + g * kLane;
 #pragma unroll
-      for (int c = 0; c < DIM / 32; ++c) qf[nt][c] = *reinterpret_cast<const u32x4_t*>(p + c * 32);
+      for (int c = 0; c < DIM / 32; ++c)
+        qf[nt][c] = *reinterpret_cast<const u32x4_t*>(p + c * kNext);
     }
   }
   // unused rows see nothing, so every block counts as masked for them only if
   // it does for the first token
   const int end = k1 < q.len ? k1 : q.len;
-  add_keys<BITS, BF16, DIM, NT, ALIGNED, WAVES>(s, qf, limit, q.len - q.tokens, r, kvh, q.len,
-                                                k0 + kBlock * wave, end, lds + wave, &st);
+  if constexpr (BITS == 16)
+    add_keys<BF16, DIM, NT, ALIGNED, WAVES>(s, qf, limit, q.len - q.tokens, r, kvh, q.len,
+                                            k0 + kBlock * wave, end, lds + wave, &st);
+  else
+    add_codes<BITS, BF16, DIM, NT, ALIGNED, WAVES>(s, qf, limit, q.len - q.tokens, r, kvh, q.len,
+                                                   k0 + kBlock * wave, end, lds + wave, &st);
 
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -506,8 +678,20 @@ __device__ __forceinline__ void serve(const RowArgs& s, uint32_t block,
                                       WaveLds<BITS, DIM, NT>* lds, int32_t* start, int32_t* sums) {
   const int64_t heads = s.a.kv_heads;
   const bool direct = WAVES != kWaves || s.runs == 0;   // one workgroup per request and head
-  const int64_t run = block / (uint32_t)s.a.kv_heads;   // or the request
-  const int h = (int)(block - run * heads);
+  int64_t run = block / (uint32_t)s.a.kv_heads;         // or the request
+  int h = (int)(block - run * heads);
+  if (BITS != 16) {
+    // Workgroups go to the XCDs in turn: a run's heads to one of them, because rows
+    // and scales of several heads may lie in a cache line of 128 bytes (codes of a
+    // head side by side: 340 us, this 330 in 8 bits, 199 and 193 in 4; heads side by
+    // side in 4 bits 387 and 277).
+    const uint32_t of_runs = s.runs != 0 ? (uint32_t)s.runs : (uint32_t)s.a.n;
+    if (block < of_runs / kXcds * kXcds * (uint32_t)heads) {
+      const uint32_t i = block / kXcds, turn = i / (uint32_t)heads;
+      run = turn * kXcds + block % kXcds;
+      h = (int)(i - turn * (uint32_t)heads);
+    }
+  }
   const int n = (int)s.a.n;
   int64_t u = 0, end = 0;
   if (direct) {
@@ -558,8 +742,14 @@ struct Plan {
   size_t starts, ml, total;   // workspace: bytes of the parts
 };
 
-Plan plan_of(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim, int32_t max_q,
-             int32_t max_len);
+Plan plan_of(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim, int32_t bits,
+             int32_t max_q, int32_t max_len);
+
+// Workgroups of one tile of rows that fit a compute unit.  Rows of 32 bytes (64
+// elements in 4 bits) leave room for three, which read a cache of 256 requests of
+// 4000 keys, 8 heads, in 133 us, two in 161; rows of 64 bytes gain nothing (8 bits
+// of 64 186 us both, 4 of 128 198 and 199), wider ones have no room.
+constexpr int groups_per_cu(int bits, int dim) { return bits * dim == 256 ? 3 : 2; }
 RowArgs args_of(const AttnCall& a, const Plan& p, void* workspace);
 
 // Workgroups of a call: one for each run and head, or request and head.
@@ -571,7 +761,9 @@ inline int64_t groups_of(const AttnCall& a, const Plan& p) {
 int join_rows(const RowArgs& s, const Plan& p, hipStream_t stream);
 
 template <int BITS, bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
-__global__ __launch_bounds__(WAVES * kWave, 2) void attention_rows_kernel(RowArgs s) {
+__global__ __launch_bounds__(WAVES * kWave,
+                             NT == 1 && WAVES == kWaves ? groups_per_cu(BITS, DIM) : 2)
+void attention_rows_kernel(RowArgs s) {
   __shared__ WaveLds<BITS, DIM, NT> lds[WAVES];
   __shared__ int32_t start[WAVES == kWaves ? kMostScanned + 1 : 1];
   __shared__ int32_t sums[kWaves];

@@ -156,7 +156,7 @@ int launch_attention_tiles(const AttnCall& a, int32_t least_rows, void* few_work
   rows::RowArgs w;
   rows::Plan wp;
   if (few_workspace != nullptr) {
-    wp = rows::plan_of(a.n, a.q_heads, a.kv_heads, a.dim, a.max_q, a.max_len);
+    wp = rows::plan_of(a.n, a.q_heads, a.kv_heads, a.dim, a.bits, a.max_q, a.max_len);
     w = rows::args_of(a, wp, few_workspace);
   }
   const rows::RowArgs* few = few_workspace != nullptr ? &w : nullptr;

@@ -44,23 +44,6 @@ struct Codes {
   static constexpr int kWords = kBytes >= 4 ? kBytes / 4 : 1;
   uint32_t w[kWords];
 
-  // Read once: non-temporal.
-  __device__ __forceinline__ void load_once(const unsigned char* p) {
-    if constexpr (kBytes == 16) {
-      const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = v[i];
-    } else if constexpr (kBytes == 8) {
-      const u32x2_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(p));
-      w[0] = v[0];
-      w[1] = v[1];
-    } else if constexpr (kBytes == 4) {
-      w[0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
-    } else {
-      w[0] = __builtin_nontemporal_load(reinterpret_cast<const uint16_t*>(p));
-    }
-  }
-
   __device__ __forceinline__ void load(const unsigned char* p) {
     if constexpr (kBytes == 16) {
       const u32x4_t v = *reinterpret_cast<const u32x4_t*>(p);

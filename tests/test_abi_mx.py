@@ -89,9 +89,9 @@ def test_rows_that_share_memory():
 
 def test_attention():
     size = pair.lib().pair_paged_attention_mx_workspace_bytes
-    assert size(4, 4, 16, 2, 128, 1, 1000) > 0
-    for i, bad in ((0, 0), (1, -1), (2, 13), (3, 0), (4, 96), (5, 0), (6, -1)):
-        args = [4, 4, 16, 2, 128, 1, 1000]
+    assert size(4, 4, 16, 2, 128, 8, 1, 1000) > 0
+    for i, bad in ((0, 0), (1, -1), (2, 13), (3, 0), (4, 96), (5, 16), (6, 0), (7, -1)):
+        args = [4, 4, 16, 2, 128, 4, 1, 1000]
         args[i] = bad
         assert size(*args) == 0, (i, bad)
     for name in ("q", "table", "off", "lens", "out"):
@@ -105,7 +105,7 @@ def test_attention():
         assert attention(cache(), **kw) == EALIGN, kw
     for kw in (dict(oh=64), dict(ot=0)):
         assert attention(cache(), **kw) == EINVAL, kw
-    need = size(4, 4, 16, 2, 128, 1, 1000)
+    need = size(4, 4, 16, 2, 128, 8, 1, 1000)
     assert attention(cache(), ws=NULL) == EWORKSPACE and attention(cache(), wsb=need - 1) == EWORKSPACE
     assert attention(cache(), tokens=0, q=NULL, out=NULL, wsb=0) == 0      # nothing to do
     for n, tokens, heads, mq in ((1 << 24, 1 << 24, 1, 1), (1 << 14, 1 << 14, 1024, 1)):
