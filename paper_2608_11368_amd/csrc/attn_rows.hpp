@@ -133,12 +133,14 @@ struct WaveLds {
   union {
     float sum[16][DIM + 4];
     unsigned char key[kBlock * DIM * 2];
-    unsigned char codes[2 * kBlock * kRowBytes];
+    unsigned char codes[BITS == 16 ? 16 : 2 * kBlock * kRowBytes];
     uint16_t value[kBlock][DIM];
   };
   uint32_t weight[NT][16][kBlock / 2];
-  float stat[16][2];
-  uint32_t scale[BITS == 16 ? 1 : 2 * kBlock];   // of a block's keys and values: each row's bytes
+  union {
+    float stat[16][2];
+    uint32_t scale[BITS == 16 ? 1 : 2 * kBlock];   // of a block's keys and values: each row's bytes
+  };
 
   // Piece `c` of 16 bytes of key `y`: permuted by the row so that eight rows'
   // pieces at one place lie in different banks.

@@ -258,22 +258,38 @@ __device__ __forceinline__ int64_t lane_value64(int64_t v, int lane) {
   return (int64_t)(((uint64_t)hi << 32) | lo);
 }
 
-// A lane's eight elements of a row on their way from memory: as values, or as
-// codes and their block's scale.
+// A lane's eight elements of a row on their way from memory: codes and their block's
+// scale, or the values themselves.
 template <int BITS>
 struct Piece8 {
   Codes<BITS, 8> codes;
   uint32_t scale;
   __device__ __forceinline__ void load(const unsigned char* p, const unsigned char* at) {
     codes.load(p);
-    if (BITS != 16) scale = *at;
+    scale = *at;
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < Codes<BITS, 8>::kWords; ++i) codes.w[i] = 0u;
+    scale = 127u;
   }
   template <bool BF16>
   __device__ __forceinline__ u32x4_t values() const {
     uint32_t v[4];
-    codes.template values<BF16>(BITS != 16 ? mx_scale(scale) : 0.0f, v);
+    codes.template values<BF16>(mx_scale(scale), v);
     return u32x4_t{v[0], v[1], v[2], v[3]};
   }
+};
+
+template <>
+struct Piece8<16> {
+  u32x4_t v;
+  __device__ __forceinline__ void load(const unsigned char* p, const unsigned char*) {
+    v = *reinterpret_cast<const u32x4_t*>(p);
+  }
+  __device__ __forceinline__ void clear() { v = u32x4_t{0u, 0u, 0u, 0u}; }
+  template <bool>
+  __device__ __forceinline__ u32x4_t values() const { return v; }
 };
 
 // One workgroup's tile, `block` its place in the order.
@@ -432,16 +448,14 @@ __device__ __forceinline__ void attend_tile(const TileArgs& s, uint32_t block,
     // see whole holds a value that is not finite.
     const bool edge = kb + kKeys - 1 > tile_limit;
     bool odd = false;
-    u32x4_t vw[kStage];
-#pragma unroll
-    for (int p = 0; p < kStage; ++p) vw[p] = vs[p].template values<BF16>();
     if (edge) {
       uint32_t bad = 0;
 #pragma unroll
       for (int p = 0; p < kStage; ++p) {
-        if (kb + p * kStep + my_row >= q.len) vw[p] = u32x4_t{0u, 0u, 0u, 0u};   // no value at all
+        if (kb + p * kStep + my_row >= q.len) vs[p].clear();   // no value at all
+        const u32x4_t v = vs[p].template values<BF16>();
 #pragma unroll
-        for (int w = 0; w < 4; ++w) bad |= not_finite<BF16>(vw[p][w]) ? 1u : 0u;
+        for (int w = 0; w < 4; ++w) bad |= not_finite<BF16>(v[w]) ? 1u : 0u;
       }
       odd = __syncthreads_or((int)bad) != 0;
     }
@@ -449,7 +463,8 @@ __device__ __forceinline__ void attend_tile(const TileArgs& s, uint32_t block,
     for (int p = 0; p < kStage; ++p) {
       *reinterpret_cast<u32x4_t*>(kt[buf] + p * kStep * DIM * 2 + k_in) =
           ks[p].template values<BF16>();
-      *reinterpret_cast<u32x4_t*>(vt[buf] + p * kStep * DIM * 2 + v_in) = vw[p];
+      *reinterpret_cast<u32x4_t*>(vt[buf] + p * kStep * DIM * 2 + v_in) =
+          vs[p].template values<BF16>();
     }
     __syncthreads();
     if (kb + kKeys < k1) fetch(kb + kKeys);

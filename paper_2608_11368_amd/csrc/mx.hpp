@@ -36,8 +36,7 @@ __device__ __forceinline__ uint32_t mx_pair(uint32_t codes, float scale) {
                             __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, I & 3));
 }
 
-// N elements of a row as they lie in a cache of BITS bits an element (16: the values
-// themselves).
+// N elements of a row as they lie in a cache of BITS bits an element.
 template <int BITS, int N>
 struct Codes {
   static constexpr int kBytes = N * BITS / 8;
@@ -66,10 +65,6 @@ struct Codes {
     constexpr int kPairs = 16 / BITS;               // of a dword
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) {
-      if (BITS == 16) {
-        to[i] = w[i];
-        continue;
-      }
       const uint32_t c = w[i / kPairs];
       const int at = i % kPairs;
       to[i] = at == 0   ? mx_pair<BF16, BITS, 0>(c, scale)
