@@ -258,11 +258,11 @@ __device__ __forceinline__ int64_t lane_value64(int64_t v, int lane) {
   return (int64_t)(((uint64_t)hi << 32) | lo);
 }
 
-// A lane's eight elements of a row on their way from memory: codes and their block's
-// scale, or the values themselves.
-template <int BITS>
-struct Piece8 {
-  Codes<BITS, 8> codes;
+// A lane's elements of a row on their way from memory, N of them, of one block:
+// codes and their scale, or the values themselves.
+template <int BITS, int N>
+struct Piece {
+  Codes<BITS, N> codes;
   uint32_t scale;
   __device__ __forceinline__ void load(const unsigned char* p, const unsigned char* at) {
     codes.load(p);
@@ -270,26 +270,26 @@ struct Piece8 {
   }
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int i = 0; i < Codes<BITS, 8>::kWords; ++i) codes.w[i] = 0u;
+    for (int i = 0; i < Codes<BITS, N>::kWords; ++i) codes.w[i] = 0u;
     scale = 127u;
   }
   template <bool BF16>
-  __device__ __forceinline__ u32x4_t values() const {
-    uint32_t v[4];
+  __device__ __forceinline__ u32x4_t values(int i) const {   // elements 8 i ..
+    uint32_t v[N / 2];
     codes.template values<BF16>(mx_scale(scale), v);
-    return u32x4_t{v[0], v[1], v[2], v[3]};
+    return u32x4_t{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
   }
 };
 
 template <>
-struct Piece8<16> {
+struct Piece<16, 8> {
   u32x4_t v;
   __device__ __forceinline__ void load(const unsigned char* p, const unsigned char*) {
     v = *reinterpret_cast<const u32x4_t*>(p);
   }
   __device__ __forceinline__ void clear() { v = u32x4_t{0u, 0u, 0u, 0u}; }
   template <bool>
-  __device__ __forceinline__ u32x4_t values() const { return v; }
+  __device__ __forceinline__ u32x4_t values(int) const { return v; }
 };
 
 // One workgroup's tile, `block` its place in the order.
@@ -299,7 +299,11 @@ __device__ __forceinline__ void attend_tile(const TileArgs& s, uint32_t block,
                                             unsigned char (&vt)[2][kKeys * DIM * 2]) {
   constexpr int NC = DIM / 16;              // k pieces of a score product
   constexpr int ND = DIM / 32;              // dim tiles of the output
-  constexpr int kPer = DIM / 8;             // 16-byte pieces of a row
+  // A lane's piece of a row: 16 bytes in memory (8 of 4 bits at width 64), kPut
+  // times 16 in LDS.
+  constexpr int kOwn = BITS == 16 ? 8 : BITS == 4 && DIM == 128 ? 32 : 16;   // elements
+  constexpr int kPut = kOwn / 8;
+  constexpr int kPer = DIM / kOwn;          // pieces of a row
   constexpr int kStage = kKeys * kPer / kThreads;   // pieces of a lane per step
   constexpr int kStep = kThreads / kPer;    // rows between a lane's pieces
   // add_odd_step lays 16 KiB of weights over both key steps
@@ -388,13 +392,13 @@ __device__ __forceinline__ void attend_tile(const TileArgs& s, uint32_t block,
   // a scalar base.  The next window's pages are loaded a window ahead.  Else
   // each lane looks its rows up a step ahead.
   constexpr int kWindow = 16 * kWave;
-  Piece8<BITS> ks[kStage], vs[kStage];
+  Piece<BITS, kOwn> ks[kStage], vs[kStage];
   int32_t id[ALIGNED ? 1 : kStage];
   int64_t group_at = 0, group_scales = 0;
   int window = k0;
   const uint32_t lane_off =
-      my_piece * BITS + (ALIGNED ? (uint32_t)((my_row & 15) * slot_bytes) : 0u);
-  const int64_t scale_off = kvh * s.a.scales.head + my_piece / 4 +
+      my_piece * (kOwn * BITS / 8) + (ALIGNED ? (uint32_t)((my_row & 15) * slot_bytes) : 0u);
+  const int64_t scale_off = kvh * s.a.scales.head + my_piece * kOwn / kMxBlock +
                             (ALIGNED ? (my_row & 15) * s.a.scales.slot : 0);
   auto row_key = [&](int kb, int p) {       // one past the end repeats the last
     const int key = ALIGNED ? kb + 16 * lane : kb + p * kStep + my_row;
@@ -430,9 +434,12 @@ __device__ __forceinline__ void attend_tile(const TileArgs& s, uint32_t block,
   };
 
   // Offsets in LDS; a step's buffer and the rows' higher parts are constants.
-  int k_in, v_in, k_out[NC], v_out[ND];
-  k_in = key_piece<DIM>(my_row, my_piece);
-  v_in = value_piece<DIM>(my_row, my_piece);
+  int k_in[kPut], v_in[kPut], k_out[NC], v_out[ND];
+#pragma unroll
+  for (int i = 0; i < kPut; ++i) {
+    k_in[i] = key_piece<DIM>(my_row, my_piece * kPut + i);
+    v_in[i] = value_piece<DIM>(my_row, my_piece * kPut + i);
+  }
 #pragma unroll
   for (int c = 0; c < NC; ++c) k_out[c] = key_piece<DIM>(x, 2 * c + h);
 #pragma unroll
@@ -453,18 +460,25 @@ __device__ __forceinline__ void attend_tile(const TileArgs& s, uint32_t block,
 #pragma unroll
       for (int p = 0; p < kStage; ++p) {
         if (kb + p * kStep + my_row >= q.len) vs[p].clear();   // no value at all
-        const u32x4_t v = vs[p].template values<BF16>();
 #pragma unroll
-        for (int w = 0; w < 4; ++w) bad |= not_finite<BF16>(v[w]) ? 1u : 0u;
+        for (int i = 0; i < kPut; ++i) {
+          const u32x4_t v = vs[p].template values<BF16>(i);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) bad |= not_finite<BF16>(v[w]) ? 1u : 0u;
+        }
       }
       odd = __syncthreads_or((int)bad) != 0;
     }
 #pragma unroll
     for (int p = 0; p < kStage; ++p) {
-      *reinterpret_cast<u32x4_t*>(kt[buf] + p * kStep * DIM * 2 + k_in) =
-          ks[p].template values<BF16>();
-      *reinterpret_cast<u32x4_t*>(vt[buf] + p * kStep * DIM * 2 + v_in) =
-          vs[p].template values<BF16>();
+#pragma unroll
+      for (int i = 0; i < kPut; ++i)
+        *reinterpret_cast<u32x4_t*>(kt[buf] + p * kStep * DIM * 2 + k_in[i]) =
+            ks[p].template values<BF16>(i);
+#pragma unroll
+      for (int i = 0; i < kPut; ++i)
+        *reinterpret_cast<u32x4_t*>(vt[buf] + p * kStep * DIM * 2 + v_in[i]) =
+            vs[p].template values<BF16>(i);
     }
     __syncthreads();
     if (kb + kKeys < k1) fetch(kb + kKeys);
