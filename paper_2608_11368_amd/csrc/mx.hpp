@@ -59,6 +59,14 @@ struct Codes {
     }
   }
 
+  __device__ __forceinline__ void store(unsigned char* p) const {
+    static_assert(kBytes == 16 || kBytes == 8, "wide stores");
+    if constexpr (kBytes == 16)
+      *reinterpret_cast<u32x4_t*>(p) = u32x4_t{w[0], w[1], w[2], w[3]};
+    else
+      *reinterpret_cast<u32x2_t*>(p) = u32x2_t{w[0], w[1]};
+  }
+
   // The elements' values, two to a dword: all of one block.
   template <bool BF16>
   __device__ __forceinline__ void values(float scale, uint32_t (&to)[N / 2]) const {

@@ -7,13 +7,19 @@ namespace pair {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPieces = 4;        // in flight per lane
+// Pieces of a lane at a time.  HBM-bound (a copy of 2 GiB runs at 4.9 TB/s of reads and
+// writes): 32,467 fp16 tokens of 8 heads of 128 into 8 bits, 202 MB, 42 us and 4.8
+// TB/s with one, 44 with two, 48 with four; 60,000 of 4 heads of 128 out of 8 bits
+// 32.5, 32.0 and 41 us.  Pieces of 8 elements stored in 48 us.
+constexpr int kStored = 1, kLoaded = 2;
 
 typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
 
-// A piece is eight elements of a row: piece i of a call is piece i % per_token of
-// token i / per_token, the keys' pieces before the values'.  Four neighbouring
-// lanes have a block.
+// A piece is 16 elements of a row: piece i of a call is piece i % per_token of token
+// i / per_token, the keys' pieces before the values'.  Two neighbouring lanes have a
+// block.
+constexpr int kPiece = 16;
+
 struct MoveArgs {
   unsigned char* rows[2];             // 16-bit rows: keys, values
   unsigned char* codes[2];
@@ -48,15 +54,15 @@ __device__ __forceinline__ Place place_of(const MoveArgs& a, int64_t t0, uint32_
   const uint32_t d = c - h * a.per_head.d;
   Place p;
   p.row = (value ? a.rows[1] : a.rows[0]) + (t0 + tok) * a.token_bytes + h * a.head_row_bytes +
-          d * 16u;
+          d * (uint32_t)(2 * kPiece);
   if (slot >= a.slots_total) raise_status(a.d_status, PAIR_ST_PAGES);
   p.stored = slot >= 0 && slot < a.slots_total;
   const uint32_t y = p.stored ? (uint32_t)slot : 0u;
   const uint32_t pg = div_by(y, a.page), at = y - pg * a.page.d;
   p.code = (value ? a.codes[1] : a.codes[0]) + pg * a.page_bytes + at * a.slot_bytes +
-           h * a.head_bytes + d * (uint32_t)BITS;
+           h * a.head_bytes + d * (uint32_t)(kPiece * BITS / 8);
   p.scale = (value ? a.scales[1] : a.scales[0]) + pg * a.scale_page + at * a.scale_slot +
-            h * a.scale_head + (d >> 2);
+            h * a.scale_head + d / (uint32_t)(kMxBlock / kPiece);
   return p;
 }
 
@@ -81,18 +87,38 @@ __device__ __forceinline__ uint32_t scale_byte(float most) {
   return (uint32_t)(e < 27 ? 27 : e);
 }
 
-// Eight elements, a quarter of a block.  Magnitudes are compared as the integers
-// that their bits are; the four lanes of a block exchange their largest.  A block
-// that holds a NaN or an infinity becomes NaN.
+// Two values with their signs as codes: bytes 2 (I % 2) .. of `old` (8 bits), byte I
+// of it (4 bits).
+template <bool BF16, int BITS, int I>
+__device__ __forceinline__ uint32_t mx_code(uint32_t old, uint32_t two, float scale) {
+  if (BITS == 8) {
+    const mx_s16x2_t o = __builtin_bit_cast(mx_s16x2_t, old);
+    if (BF16)
+      return __builtin_bit_cast(uint32_t,
+                                __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(
+                                    o, __builtin_bit_cast(mx_bf16x2_t, two), scale, (I & 1) != 0));
+    return __builtin_bit_cast(uint32_t,
+                              __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(
+                                  o, __builtin_bit_cast(mx_f16x2_t, two), scale, (I & 1) != 0));
+  }
+  if (BF16)
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, __builtin_bit_cast(mx_bf16x2_t, two),
+                                                     scale, I & 3);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(old, __builtin_bit_cast(mx_f16x2_t, two), scale,
+                                                  I & 3);
+}
+
+// 16 elements, half a block.  Magnitudes are compared as the integers that their
+// bits are; the two lanes of a block exchange their largest.  A block that holds a
+// NaN or an infinity becomes NaN.
 template <bool BF16, int BITS>
-__device__ __forceinline__ Codes<BITS, 8> quantise(u32x4_t v, uint32_t* byte) {
+__device__ __forceinline__ Codes<BITS, kPiece> quantise(const u32x4_t (&v)[2], uint32_t* byte) {
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) top = max16x2(top, v[i] & 0x7fff7fffu);
+  for (int i = 0; i < 8; ++i) top = max16x2(top, v[i >> 2][i & 3] & 0x7fff7fffu);
   uint32_t most = (top & 0xffffu) > (top >> 16) ? top & 0xffffu : top >> 16;
-  uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0xB1, 0xf, 0xf, false);
-  most = most > other ? most : other;
-  other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0x4E, 0xf, 0xf, false);
+  const uint32_t other =
+      (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0xB1, 0xf, 0xf, false);
   most = most > other ? most : other;
   const bool odd = most >= (BF16 ? 0x7f80u : 0x7c00u);
   // The last numbers of the 16-bit type would be rounded past its range: the
@@ -103,42 +129,23 @@ __device__ __forceinline__ Codes<BITS, 8> quantise(u32x4_t v, uint32_t* byte) {
                        : (float)__builtin_bit_cast(_Float16, (uint16_t)most);
   *byte = odd ? 255u : scale_byte<BITS>(m);
   const float scale = mx_scale(*byte);
-  Codes<BITS, 8> c;
-  mx_s16x2_t s8[2] = {{0, 0}, {0, 0}};
-  uint32_t s4 = 0;
+  Codes<BITS, kPiece> c;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t w = min16x2(v[i] & 0x7fff7fffu, kTop | kTop << 16) | (v[i] & 0x80008000u);
-    if (BITS == 8) {
-      if (BF16) {
-        const mx_bf16x2_t x = __builtin_bit_cast(mx_bf16x2_t, w);
-        s8[i >> 1] = i & 1 ? __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(s8[i >> 1], x, scale, true)
-                           : __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(s8[i >> 1], x, scale, false);
-      } else {
-        const mx_f16x2_t x = __builtin_bit_cast(mx_f16x2_t, w);
-        s8[i >> 1] = i & 1 ? __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(s8[i >> 1], x, scale, true)
-                           : __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(s8[i >> 1], x, scale, false);
-      }
-    } else if (BF16) {
-      const mx_bf16x2_t x = __builtin_bit_cast(mx_bf16x2_t, w);
-      s4 = i == 0   ? __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(s4, x, scale, 0)
-           : i == 1 ? __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(s4, x, scale, 1)
-           : i == 2 ? __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(s4, x, scale, 2)
-                    : __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(s4, x, scale, 3);
-    } else {
-      const mx_f16x2_t x = __builtin_bit_cast(mx_f16x2_t, w);
-      s4 = i == 0   ? __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(s4, x, scale, 0)
-           : i == 1 ? __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(s4, x, scale, 1)
-           : i == 2 ? __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(s4, x, scale, 2)
-                    : __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(s4, x, scale, 3);
-    }
+  for (int w = 0; w < Codes<BITS, kPiece>::kWords; ++w) c.w[w] = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t in = v[i >> 2][i & 3];
+    const uint32_t two = min16x2(in & 0x7fff7fffu, kTop | kTop << 16) | (in & 0x80008000u);
+    uint32_t* w = &c.w[i / (16 / BITS)];
+    const int at = i % (16 / BITS);
+    *w = at == 0   ? mx_code<BF16, BITS, 0>(*w, two, scale)
+         : at == 1 ? mx_code<BF16, BITS, 1>(*w, two, scale)
+         : at == 2 ? mx_code<BF16, BITS, 2>(*w, two, scale)
+                   : mx_code<BF16, BITS, 3>(*w, two, scale);
   }
-  if (BITS == 8) {
-    c.w[0] = odd ? 0u : __builtin_bit_cast(uint32_t, s8[0]);
-    c.w[BITS == 8 ? 1 : 0] = odd ? 0u : __builtin_bit_cast(uint32_t, s8[1]);
-  } else {
-    c.w[0] = odd ? 0u : s4;
-  }
+#pragma unroll
+  for (int w = 0; w < Codes<BITS, kPiece>::kWords; ++w)
+    if (odd) c.w[w] = 0;
   return c;
 }
 
@@ -148,29 +155,29 @@ __global__ __launch_bounds__(kThreads) void mx_store_kernel(MoveArgs a, int toke
   const int64_t left = a.tokens - t0;
   const uint32_t n =
       (uint32_t)(left < tokens_per_group ? left : tokens_per_group) * a.per_token.d;
-  for (uint32_t i0 = threadIdx.x; i0 < n; i0 += kThreads * kPieces) {
-    u32x4_t v[kPieces];
-    Place p[kPieces];
+  for (uint32_t i0 = threadIdx.x; i0 < n; i0 += kThreads * kStored) {
+    u32x4_t v[kStored][2];
+    Place p[kStored];
 #pragma unroll
-    for (int s = 0; s < kPieces; ++s) {
+    for (int s = 0; s < kStored; ++s) {
       const uint32_t i = i0 + s * kThreads;
       p[s].stored = false;
       if (i < n) {
         p[s] = place_of<BITS>(a, t0, i);
-        if (p[s].stored) v[s] = *reinterpret_cast<const u32x4_t*>(p[s].row);
+        if (p[s].stored) {
+          v[s][0] = *reinterpret_cast<const u32x4_t*>(p[s].row);
+          v[s][1] = *reinterpret_cast<const u32x4_t*>(p[s].row + 16);
+        }
       }
     }
     bool odd = false;
 #pragma unroll
-    for (int s = 0; s < kPieces; ++s) {
+    for (int s = 0; s < kStored; ++s) {
       if (!p[s].stored) continue;               // the same for the lanes of a block
       uint32_t byte;
-      const Codes<BITS, 8> c = quantise<BF16, BITS>(v[s], &byte);
-      if (BITS == 8)
-        *reinterpret_cast<u32x2_t*>(p[s].code) = u32x2_t{c.w[0], c.w[BITS == 8 ? 1 : 0]};
-      else
-        *reinterpret_cast<uint32_t*>(p[s].code) = c.w[0];
-      if ((threadIdx.x & 3) == 0) *p[s].scale = (unsigned char)byte;
+      const Codes<BITS, kPiece> c = quantise<BF16, BITS>(v[s], &byte);
+      c.store(p[s].code);
+      if ((threadIdx.x & 1) == 0) *p[s].scale = (unsigned char)byte;
       odd |= byte == 255u;
     }
     if (odd) raise_status(a.d_status, PAIR_ST_NONFINITE);
@@ -183,17 +190,17 @@ __global__ __launch_bounds__(kThreads) void mx_load_kernel(MoveArgs a, int token
   const int64_t left = a.tokens - t0;
   const uint32_t n =
       (uint32_t)(left < tokens_per_group ? left : tokens_per_group) * a.per_token.d;
-  for (uint32_t i0 = threadIdx.x; i0 < n; i0 += kThreads * kPieces) {
-    Codes<BITS, 8> c[kPieces];
-    uint32_t byte[kPieces];
-    unsigned char* to[kPieces];
+  for (uint32_t i0 = threadIdx.x; i0 < n; i0 += kThreads * kLoaded) {
+    Codes<BITS, kPiece> c[kLoaded];
+    uint32_t byte[kLoaded];
+    unsigned char* to[kLoaded];
 #pragma unroll
-    for (int s = 0; s < kPieces; ++s) {
+    for (int s = 0; s < kLoaded; ++s) {
       const uint32_t i = i0 + s * kThreads;
       to[s] = nullptr;
       byte[s] = 0;
 #pragma unroll
-      for (int w = 0; w < Codes<BITS, 8>::kWords; ++w) c[s].w[w] = 0;
+      for (int w = 0; w < Codes<BITS, kPiece>::kWords; ++w) c[s].w[w] = 0;
       if (i < n) {
         const Place p = place_of<BITS>(a, t0, i);
         to[s] = p.row;
@@ -204,11 +211,12 @@ __global__ __launch_bounds__(kThreads) void mx_load_kernel(MoveArgs a, int token
       }
     }
 #pragma unroll
-    for (int s = 0; s < kPieces; ++s) {
+    for (int s = 0; s < kLoaded; ++s) {
       if (to[s] == nullptr) continue;
-      uint32_t v[4];
+      uint32_t v[kPiece / 2];
       c[s].template values<BF16>(mx_scale(byte[s]), v);
       *reinterpret_cast<u32x4_t*>(to[s]) = u32x4_t{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<u32x4_t*>(to[s] + 16) = u32x4_t{v[4], v[5], v[6], v[7]};
     }
   }
 }
@@ -234,7 +242,7 @@ int launch_mx_move(bool store, const MxCache& cache, int64_t tokens, bool bf16, 
   a.scale_slot = cache.scale_slot;
   a.scale_head = cache.scale_head;
   a.page = fast_div((uint32_t)cache.page);
-  const uint32_t per_head = (uint32_t)cache.dim / 8;
+  const uint32_t per_head = (uint32_t)cache.dim / kPiece;
   a.per_head = fast_div(per_head);
   a.half = (uint32_t)cache.kv_heads * per_head;
   a.per_token = fast_div(2 * a.half);
@@ -242,9 +250,9 @@ int launch_mx_move(bool store, const MxCache& cache, int64_t tokens, bool bf16, 
   a.slots = slots;
   a.tokens = tokens;
   a.d_status = d_status;
-  // About four pieces a lane, at least one token a workgroup, and no more of them
+  // About the lanes' pieces, at least one token a workgroup, and no more of them
   // than a launch can have (below 2^32 threads).
-  int per_group = (int)(kThreads * kPieces / a.per_token.d);
+  int per_group = (int)(kThreads * (store ? kStored : kLoaded) / a.per_token.d);
   const int least = (int)((tokens + (1 << 23) - 1) >> 23);
   if (per_group < least) per_group = least;
   const dim3 grid((unsigned)((tokens + per_group - 1) / per_group));
