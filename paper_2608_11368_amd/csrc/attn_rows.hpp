@@ -199,7 +199,7 @@ __device__ __forceinline__ void add_odd_block(WaveLds<BITS, DIM, NT>* lds, const
 template <int BITS, bool BF16, int DIM, int NT>
 __device__ __forceinline__ void weigh_block(const RowArgs& s, const f32x4_t (&sc)[NT][2],
                                             const int (&limit)[NT], int first_limit, int len,
-                                            int kb, Piece<DIM> (&vr)[8],
+                                            int kb, Piece<DIM> (&vr)[8], int tiles,
                                             WaveLds<BITS, DIM, NT>* lds, State<DIM, NT>* st) {
   constexpr int ND = DIM / 16;       // dims of a lane's piece of a value row
   const int g = (threadIdx.x & (kWave - 1)) >> 4;
@@ -207,6 +207,7 @@ __device__ __forceinline__ void weigh_block(const RowArgs& s, const f32x4_t (&sc
   const bool masked = kb + kBlock - 1 > first_limit;   // some row does not see some key
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
+    if (nt >= tiles) continue;
 #pragma unroll
     for (int e = 0; e < 8; ++e) p[nt][e] = sc[nt][e >> 2][e & 3] * s.scale_log2;
     if (masked) {
@@ -265,7 +266,8 @@ __device__ __forceinline__ void weigh_block(const RowArgs& s, const f32x4_t (&sc
       vt[w] = __builtin_amdgcn_perm(vr[2 * w + 1].w[j >> 1], vr[2 * w].w[j >> 1],
                                     (j & 1) ? 0x07060302u : 0x05040100u);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) st->acc[nt][j] = mma16<BF16>(vt, pf[nt], st->acc[nt][j]);
+    for (int nt = 0; nt < NT; ++nt)
+      if (nt < tiles) st->acc[nt][j] = mma16<BF16>(vt, pf[nt], st->acc[nt][j]);
   }
 }
 
@@ -303,7 +305,7 @@ __device__ __forceinline__ void add_block(const RowArgs& s, const u32x4_t (&qf)[
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) sc[nt][t] = mma16<BF16>(kf, qf[nt][c], sc[nt][t]);
     }
-  weigh_block<16, BF16, DIM, NT>(s, sc, limit, first_limit, len, kb, vr, lds, st);
+  weigh_block<16, BF16, DIM, NT>(s, sc, limit, first_limit, len, kb, vr, NT, lds, st);
 }
 
 template <bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
@@ -378,7 +380,7 @@ template <int BITS, bool BF16, int DIM, int NT, bool ALIGNED, int WAVES>
 __device__ __forceinline__ void add_codes(const RowArgs& s,
                                           const u32x4_t (&qf)[NT][DIM / 32],
                                           const int (&limit)[NT], int first_limit, int64_t r,
-                                          int64_t kvh, int len, int k0, int k1,
+                                          int64_t kvh, int len, int k0, int k1, int tiles,
                                           WaveLds<BITS, DIM, NT>* lds, State<DIM, NT>* st) {
   using Lds = WaveLds<BITS, DIM, NT>;
   constexpr int W = DIM * BITS / 8;                        // bytes of a row
@@ -499,7 +501,7 @@ __device__ __forceinline__ void add_codes(const RowArgs& s,
         sc[nt][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int j = 0; j < DIM / 32; ++j)
-          sc[nt][t] = mma16<BF16>(u32x4_t{kf[4 * j], kf[4 * j + 1], kf[4 * j + 2], kf[4 * j + 3]},
+          if (nt < tiles) sc[nt][t] = mma16<BF16>(u32x4_t{kf[4 * j], kf[4 * j + 1], kf[4 * j + 2], kf[4 * j + 3]},
                                   qf[nt][j], sc[nt][t]);
       }
     }
@@ -515,7 +517,7 @@ __device__ __forceinline__ void add_codes(const RowArgs& s,
             __uint_as_float(__builtin_amdgcn_alignbit(four[i], four[i], v_turn)), vr[4 * t + i].w);
       }
     }
-    weigh_block<BITS, BF16, DIM, NT>(s, sc, limit, first_limit, len, kb, vr, lds, st);
+    weigh_block<BITS, BF16, DIM, NT>(s, sc, limit, first_limit, len, kb, vr, tiles, lds, st);
   };
   if (k0 < k1) lookup(k0);
   if (kAhead && k0 < k1) {
@@ -576,7 +578,8 @@ __device__ __forceinline__ void attend(const RowArgs& s, int64_t r, int kvh, int
                                             k0 + kBlock * wave, end, lds + wave, &st);
   else
     add_codes<BITS, BF16, DIM, NT, ALIGNED, WAVES>(s, qf, limit, q.len - q.tokens, r, kvh, q.len,
-                                                   k0 + kBlock * wave, end, lds + wave, &st);
+                                                   k0 + kBlock * wave, end,
+                                                   NT == 1 || rows <= 16 ? 1 : 2, lds + wave, &st);
 
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
