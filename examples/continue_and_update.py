@@ -13,6 +13,10 @@ The policy is one attention layer with random weights, and rewards and scores ar
 synthetic: the point is the order of the calls, none of which waits for the GPU.
 
     python examples/continue_and_update.py [--prompts 16] [--group 8] [--steps 12]
+                                           [--cache bf16|fp8|fp4]
+
+With --cache fp8 or fp4 the cache holds keys and values in 8 or 4 bits with a scale
+for every 32 of them, a little over a half or a quarter of the memory.
 """
 import argparse
 import os
@@ -29,7 +33,7 @@ class Policy:
     """One attention layer over a paged cache; tied to `n` candidates."""
 
     def __init__(self, n, longest, gen, width=512, q_heads=8, kv_heads=2, dim=64, vocab=512,
-                 page=16, device="cuda:0"):
+                 page=16, device="cuda:0", cache="bf16"):
         def rand(*shape, scale=1.0):
             return (torch.randn(*shape, generator=gen, device=device) * scale).bfloat16()
 
@@ -39,8 +43,14 @@ class Policy:
         self.w_out = rand(q_heads * dim, vocab, scale=4 * (q_heads * dim) ** -0.5)
         per = -(-longest // page)
         shape = (n * per, page, kv_heads, dim)
-        self.k_cache = torch.zeros(shape, dtype=torch.bfloat16, device=device)
-        self.v_cache = torch.zeros_like(self.k_cache)
+        if cache == "bf16":
+            self.cache = tuple(torch.zeros(shape, dtype=torch.bfloat16, device=device)
+                               for _ in range(2))
+            self.store, self.attention = pair.cache_store, pair.paged_attention
+        else:
+            codes = torch.float8_e4m3fn if cache == "fp8" else torch.float4_e2m1fn_x2
+            self.cache = pair.mx_cache(*shape, dtype=codes, device=device)
+            self.store, self.attention = pair.cache_store_mx, pair.paged_attention_mx
         self.table = torch.full((n, per), -1, dtype=torch.int32, device=device)
         self.free = torch.arange(n * per, dtype=torch.int32, device=device)
         self.free_count = torch.full((1,), n * per, dtype=torch.int64, device=device)
@@ -58,19 +68,19 @@ class Policy:
                                                    plan["lens"])
         qkv = (self.embed[tokens_of(plan)] @ self.w_qkv).view(rows, q_heads + 2 * kv_heads, dim)
         q, k, v = qkv.split([q_heads, kv_heads, kv_heads], dim=1)
-        store = pair.cache_store(k, v, plan["slots"], self.k_cache, self.v_cache)
-        a = pair.paged_attention(q, self.k_cache, self.v_cache, plan["table"], plan["q_offsets"],
-                                 plan["lens"], most, self.longest)
+        store = self.store(k, v, plan["slots"], *self.cache)
+        a = self.attention(q, *self.cache, plan["table"], plan["q_offsets"], plan["lens"], most,
+                           self.longest)
         self.status |= plan["status"] | store["status"] | a["status"]
         return a["out"].flatten(1) @ self.w_out, plan
 
 
 def run(prompts=16, group=8, steps=12, prefix=48, blocks=(4096, 777, 20_000), max_norm=0.5, seed=0,
-        device="cuda:0"):
+        device="cuda:0", cache="bf16"):
     gen = torch.Generator(device=device)
     gen.manual_seed(seed)
     n = prompts * group
-    policy = Policy(n, prefix + steps, gen, device=device)
+    policy = Policy(n, prefix + steps, gen, device=device, cache=cache)
     vocab = policy.embed.shape[0]
     owner = torch.arange(n, device=device)
     one = torch.ones(n, dtype=torch.int32, device=device)
@@ -113,8 +123,9 @@ def main():
     ap.add_argument("--prompts", type=int, default=16)
     ap.add_argument("--group", type=int, default=8)
     ap.add_argument("--steps", type=int, default=12)
+    ap.add_argument("--cache", choices=("bf16", "fp8", "fp4"), default="bf16")
     args = ap.parse_args()
-    r = run(args.prompts, args.group, args.steps)
+    r = run(args.prompts, args.group, args.steps, cache=args.cache)
     kept = int(r["mask"].sum())
     print(f"{kept} of {r['mask'].numel()} candidates continued for {args.steps} tokens, "
           f"{int(r['free_count'])} pages free; gradient norm {float(r['norm']):.4g}, "

@@ -543,7 +543,18 @@ def _mx_refused(k_cache, v_cache, k_scale, v_scale):
     if k_scale.shape[:3] != k_cache.shape[:3] or k_scale.shape[3] * 32 != dim:
         raise ValueError(f"rows of {dim} elements need a scale for every 32 of them, got "
                          f"{tuple(k_scale.shape)} for {tuple(k_cache.shape)}")
-    raise ValueError("keys and values must have the same strides and contiguous rows")
+    raise ValueError("keys and values must be on one device, with the same strides and "
+                     "contiguous rows")
+
+
+def _one_device(device, **tensors):
+    """Kernels run on the current device's stream: every tensor has to be there."""
+    if device != _device_index():
+        raise ValueError(f"the caches are on cuda:{device}, the current device is "
+                         f"cuda:{_device_index()}")
+    for name, t in tensors.items():
+        if isinstance(t, torch.Tensor) and t.get_device() != device:
+            raise ValueError(f"{name} must be on cuda:{device} like the caches")
 
 
 def _half_code(t, name):
@@ -567,10 +578,11 @@ def _pair_of_rows(native, k, v, code, heads, dim):
 def pair_cache_store_mx(k, v, slots, k_cache, v_cache, k_scale, v_scale, d_status=None,
                         stream=None):
     native = _native()
-    cache, heads, dim = (native.mx_cache(k_cache, v_cache, k_scale, v_scale)
-                         or _mx_refused(k_cache, v_cache, k_scale, v_scale))
+    cache, heads, dim, device = (native.mx_cache(k_cache, v_cache, k_scale, v_scale)
+                                 or _mx_refused(k_cache, v_cache, k_scale, v_scale))
     code = _half_code(k, "k")
     kp, vp, tok, head, tokens = _pair_of_rows(native, k, v, code, heads, dim)
+    _one_device(device, k=k, v=v, slots=slots, d_status=d_status)
     _rc(lib().pair_cache_store_mx(
         cache, tokens, code, kp, vp, tok, head,
         native.address(slots, "slots", torch.int64, tokens),
@@ -582,10 +594,11 @@ def pair_cache_store_mx(k, v, slots, k_cache, v_cache, k_scale, v_scale, d_statu
 def pair_cache_load_mx(slots, k_cache, v_cache, k_scale, v_scale, k, v, d_status=None,
                        stream=None):
     native = _native()
-    cache, heads, dim = (native.mx_cache(k_cache, v_cache, k_scale, v_scale)
-                         or _mx_refused(k_cache, v_cache, k_scale, v_scale))
+    cache, heads, dim, device = (native.mx_cache(k_cache, v_cache, k_scale, v_scale)
+                                 or _mx_refused(k_cache, v_cache, k_scale, v_scale))
     code = _half_code(k, "k")
     kp, vp, tok, head, tokens = _pair_of_rows(native, k, v, code, heads, dim)
+    _one_device(device, k=k, v=v, slots=slots, d_status=d_status)
     _rc(lib().pair_cache_load_mx(
         cache, tokens, native.address(slots, "slots", torch.int64, tokens), code, kp, vp, tok, head,
         native.address(d_status, "d_status", torch.int32, 1, True), _stream(stream)),
@@ -602,8 +615,8 @@ def pair_paged_attention_mx_workspace_bytes(n, tokens, q_heads, kv_heads, dim, f
 def pair_paged_attention_mx(q, k_cache, v_cache, k_scale, v_scale, table, q_offsets, lens, max_q,
                             max_len, scale, out, lse, workspace, d_status=None, stream=None):
     native = _native()
-    cache, _, dim = (native.mx_cache(k_cache, v_cache, k_scale, v_scale)
-                     or _mx_refused(k_cache, v_cache, k_scale, v_scale))
+    cache, _, dim, device = (native.mx_cache(k_cache, v_cache, k_scale, v_scale)
+                             or _mx_refused(k_cache, v_cache, k_scale, v_scale))
     code = _half_code(q, "q")
     qp, qt, qh, tokens, heads = (native.rows(q, code, 0, dim)
                                  or _rows_refused(q, "q", q.dtype, 0, dim))
@@ -614,6 +627,8 @@ def pair_paged_attention_mx(q, k_cache, v_cache, k_scale, v_scale, table, q_offs
         raise ValueError("table must be a 2-D tensor with a row for each request")
     if orows < tokens:
         raise ValueError(f"out holds {orows} tokens, needs {tokens}")
+    _one_device(device, q=q, out=out, table=table, q_offsets=q_offsets, lens=lens, lse=lse,
+                workspace=workspace, d_status=d_status)
     at = native.address
     _rc(lib().pair_paged_attention_mx(
         cache, n, tokens, heads, code, qp, qt, qh, at(table, "table", torch.int32), table.shape[1],
@@ -1017,8 +1032,8 @@ def cache_store_mx(k, v, slots, k_cache, v_cache, k_scale, v_scale, stream=None)
 def cache_load_mx(slots, k_cache, v_cache, k_scale, v_scale, dtype=torch.bfloat16, stream=None):
     """The keys and values of `slots` (int64; zeros where one is negative) out of a
     cache in 8 or 4 bits, [tokens][kv_heads][dim] of `dtype`, bfloat16 or float16: the
-    very values that attention over the cache works with.  Both are parts of one
-    allocation and share a storage (clone what is to last)."""
+    very values that attention over the cache works with.  No gradient goes through.
+    Both are parts of one allocation and share a storage (clone what is to last)."""
     tokens, heads = slots.numel(), k_cache.shape[2]
     shape = (tokens, heads, 32 * k_scale.shape[3])
     k, v = _native().parts(k_cache.get_device(), dtype, shape, dtype, shape)
@@ -1033,11 +1048,12 @@ def paged_attention_mx(q, k_cache, v_cache, k_scale, v_scale, table, q_offsets, 
     """paged_attention over a cache in 8 or 4 bits, read as it is: q, bfloat16 or
     float16, is the type that its values are taken in (exactly, if they were stored
     from it).  All else as for paged_attention."""
-    if q.requires_grad and out is None and torch.is_grad_enabled():
+    if ((q.requires_grad or k_cache.requires_grad or v_cache.requires_grad) and out is None
+            and torch.is_grad_enabled()):
         out, lse, st = _NoGradient.apply(
             lambda: paged_attention_mx(q, k_cache, v_cache, k_scale, v_scale, table, q_offsets,
                                        lens, max_q, max_len, scale, want_lse, None, workspace,
-                                       stream), q)
+                                       stream), q, k_cache, v_cache)
         return {"out": out, "lse": lse, "status": st}
     tokens, heads, dim = q.shape
     parts, index, lse = _native().parts, q.get_device(), None

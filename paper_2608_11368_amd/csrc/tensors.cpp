@@ -152,7 +152,7 @@ PyObject* cache(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 // mx_cache(k_cache, v_cache, k_scale, v_scale) -> (pair_mx_cache as bytes, heads,
-// width), or None if they are not a cache in 8 or 4 bits.
+// width, device), or None if they are not a cache in 8 or 4 bits on one device.
 PyObject* mx_cache(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != 4) {
     PyErr_SetString(PyExc_TypeError, "mx_cache(k_cache, v_cache, k_scale, v_scale)");
@@ -170,7 +170,8 @@ PyObject* mx_cache(PyObject*, PyObject* const* args, Py_ssize_t n) {
         vs.scalar_type() != at::kFloat8_e8m0fnu || v.sizes() != k.sizes() ||
         v.strides() != k.strides() || ks.dim() != 4 || vs.sizes() != ks.sizes() ||
         vs.strides() != ks.strides() || k.stride(3) != 1 ||
-        (ks.stride(3) != 1 && ks.size(3) > 1))
+        (ks.stride(3) != 1 && ks.size(3) > 1) || v.get_device() != k.get_device() ||
+        ks.get_device() != k.get_device() || vs.get_device() != k.get_device())
       Py_RETURN_NONE;
     const int64_t dim = wide ? k.size(3) : 2 * k.size(3);
     if (ks.size(0) != k.size(0) || ks.size(1) != k.size(1) || ks.size(2) != k.size(2) ||
@@ -193,8 +194,8 @@ PyObject* mx_cache(PyObject*, PyObject* const* args, Py_ssize_t n) {
     c.kv_heads = (int32_t)k.size(2);
     c.dim = (int32_t)dim;
     c.format = wide ? PAIR_MXFP8 : PAIR_MXFP4;
-    return Py_BuildValue("y#ii", reinterpret_cast<const char*>(&c), (Py_ssize_t)sizeof(c),
-                         (int)c.kv_heads, (int)c.dim);
+    return Py_BuildValue("y#iii", reinterpret_cast<const char*>(&c), (Py_ssize_t)sizeof(c),
+                         (int)c.kv_heads, (int)c.dim, (int)k.get_device());
   } catch (...) {
     torch::translate_exception_to_python(std::current_exception());
     return nullptr;
@@ -325,7 +326,8 @@ PyMethodDef kMethods[] = {
      METH_FASTCALL, "cache(k_cache, v_cache): addresses and layout, None if it is no cache."},
     {"mx_cache", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(mx_cache)),
      METH_FASTCALL,
-     "mx_cache(k_cache, v_cache, k_scale, v_scale): (pair_mx_cache, heads, width), or None."},
+     "mx_cache(k_cache, v_cache, k_scale, v_scale): (pair_mx_cache, heads, width, device), "
+     "or None."},
     {"rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(rows)),
      METH_FASTCALL, "rows(tensor, type code, heads, width): address and layout, or None."},
     {"parts", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(parts)),

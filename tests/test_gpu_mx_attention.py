@@ -344,6 +344,72 @@ def test_gradients_are_refused():
     assert out._version == before + 1
 
 
+@pytest.mark.parametrize("cache", ["fp8", "fp4"])
+def test_update_example(cache):
+    """The example's calls in a row over a cache in 8 and 4 bits: its status, its
+    pool's pages, and attention over what the cache ends with."""
+    log(f"update example: 6 prompts of 5, {cache}")
+    from examples import continue_and_update as example
+
+    prefix, steps = 48, 12
+    r = example.run(prompts=6, group=5, steps=steps, prefix=prefix, max_norm=0.05, cache=cache)
+    torch.cuda.synchronize()
+    assert int(r["status"].item()) == 0
+    mask, policy = r["mask"].bool(), r["policy"]
+    assert 0 < int(mask.sum()) < mask.numel()
+    assert bool((r["lens"][mask] == prefix + steps).all()) and bool((r["lens"][~mask] == 0).all())
+    per = policy.table.shape[1]
+    assert int(r["free_count"]) == int((~mask).sum()) * per
+    # the last kept candidate's keys are its tokens' projections, to the formats' half step
+    c = int(torch.nonzero(mask)[-1])
+    x = torch.arange(prefix + steps, device=DEV)
+    slots = policy.table[c][x // policy.page].long() * policy.page + x % policy.page
+    got = pair.cache_load_mx(slots, *policy.cache)
+    q_heads, kv_heads, dim = policy.heads
+    qkv = (policy.embed[r["text"][c]] @ policy.w_qkv).view(-1, q_heads + 2 * kv_heads, dim)
+    for name, want in (("k", qkv[:, q_heads:q_heads + kv_heads]), ("v", qkv[:, q_heads + kv_heads:])):
+        want = want.double().cpu().numpy()
+        code, scale = mx.quantise(want, 8 if cache == "fp8" else 4, torch.bfloat16)
+        # the projection of other rows of a batch may be off by a bf16 rounding: a
+        # code's step beside it, the largest being a 8th (half) of the largest code
+        step = np.repeat(2.0 ** (scale - 127.0), 32, -1) * (32 if cache == "fp8" else 2)
+        have = got[name].double().cpu().numpy()
+        assert np.all(np.abs(have - want) <= step / 2 + np.abs(want) * 2.0 ** -6), name
+
+
+def test_tensors_of_another_device(monkeypatch):
+    """Kernels run on the current device's stream; caches of another are refused."""
+    c = Cache([40, 9], [1, 1], 4, 2, 64, 16, "bf16", seed=10)
+    cache, args = c.tensors(), (*c.arguments(), 1, 40)
+    slots = torch.arange(3, device=DEV)
+    k = torch.zeros((3, 2, 64), dtype=torch.bfloat16, device=DEV)
+    monkeypatch.setattr(pair, "_device_index", lambda: 1)
+    out, ws = torch.empty_like(c.q), torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+    for call in (lambda: pair.pair_paged_attention_mx(c.q, *cache, *args, 0.1, out, None, ws),
+                 lambda: pair.pair_cache_store_mx(k, k, slots, *cache),
+                 lambda: pair.pair_cache_load_mx(slots, *cache, k, k.clone())):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+
+
+def test_nothing_to_do():
+    """No token, no slot: nothing is launched or written."""
+    c = Cache([40, 9], [1, 1], 4, 2, 64, 16, "bf16", seed=10)
+    cache = c.tensors()
+    before = [x.view(torch.uint8).clone() for x in cache]
+    table, off, lens = c.arguments()
+    none = torch.zeros(0, dtype=torch.int64, device=DEV)
+    r = pair.paged_attention_mx(c.q[:0], *cache, table, torch.zeros_like(off), lens, 0, 40,
+                                want_lse=True)
+    s = pair.cache_store_mx(c.q[:0, :2], c.q[:0, :2], none, *cache)
+    g = pair.cache_load_mx(none, *cache)
+    torch.cuda.synchronize()
+    assert r["out"].shape == (0, 4, 64) and r["lse"].shape == (0, 4) and g["k"].shape == (0, 2, 64)
+    assert int(r["status"].item()) == int(s["status"].item()) == int(g["status"].item()) == 0
+    for x, y in zip(cache, before):
+        assert torch.equal(x.view(torch.uint8), y)
+
+
 def test_refusals():
     c = Cache([40, 9], [1, 1], 4, 2, 64, 16, "bf16", seed=10)
     kc, vc, ks, vs = c.tensors()
