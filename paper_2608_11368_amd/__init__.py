@@ -547,14 +547,13 @@ def _mx_refused(k_cache, v_cache, k_scale, v_scale):
                      "contiguous rows")
 
 
-def _one_device(device, **tensors):
+def _one_device(native, device, *tensors):
     """Kernels run on the current device's stream: every tensor has to be there."""
     if device != _device_index():
         raise ValueError(f"the caches are on cuda:{device}, the current device is "
                          f"cuda:{_device_index()}")
-    for name, t in tensors.items():
-        if isinstance(t, torch.Tensor) and t.get_device() != device:
-            raise ValueError(f"{name} must be on cuda:{device} like the caches")
+    if not native.on_device(device, *tensors):
+        raise ValueError(f"every tensor must be on cuda:{device} like the caches")
 
 
 def _half_code(t, name):
@@ -582,7 +581,7 @@ def pair_cache_store_mx(k, v, slots, k_cache, v_cache, k_scale, v_scale, d_statu
                                  or _mx_refused(k_cache, v_cache, k_scale, v_scale))
     code = _half_code(k, "k")
     kp, vp, tok, head, tokens = _pair_of_rows(native, k, v, code, heads, dim)
-    _one_device(device, k=k, v=v, slots=slots, d_status=d_status)
+    _one_device(native, device, k, v, slots, d_status)
     _rc(lib().pair_cache_store_mx(
         cache, tokens, code, kp, vp, tok, head,
         native.address(slots, "slots", torch.int64, tokens),
@@ -598,7 +597,7 @@ def pair_cache_load_mx(slots, k_cache, v_cache, k_scale, v_scale, k, v, d_status
                                  or _mx_refused(k_cache, v_cache, k_scale, v_scale))
     code = _half_code(k, "k")
     kp, vp, tok, head, tokens = _pair_of_rows(native, k, v, code, heads, dim)
-    _one_device(device, k=k, v=v, slots=slots, d_status=d_status)
+    _one_device(native, device, k, v, slots, d_status)
     _rc(lib().pair_cache_load_mx(
         cache, tokens, native.address(slots, "slots", torch.int64, tokens), code, kp, vp, tok, head,
         native.address(d_status, "d_status", torch.int32, 1, True), _stream(stream)),
@@ -627,8 +626,7 @@ def pair_paged_attention_mx(q, k_cache, v_cache, k_scale, v_scale, table, q_offs
         raise ValueError("table must be a 2-D tensor with a row for each request")
     if orows < tokens:
         raise ValueError(f"out holds {orows} tokens, needs {tokens}")
-    _one_device(device, q=q, out=out, table=table, q_offsets=q_offsets, lens=lens, lse=lse,
-                workspace=workspace, d_status=d_status)
+    _one_device(native, device, q, out, table, q_offsets, lens, lse, workspace, d_status)
     at = native.address
     _rc(lib().pair_paged_attention_mx(
         cache, n, tokens, heads, code, qp, qt, qh, at(table, "table", torch.int32), table.shape[1],

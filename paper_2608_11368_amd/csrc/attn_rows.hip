@@ -8,15 +8,14 @@ using namespace rows;
 
 namespace {
 
-// Joins the partial sums of the requests that were cut: one workgroup per
-// request, head and row.  The parts' maxima first, a lane each, then their sums
-// with several parts' loads in flight.
+// Joins the partial sums of the requests that were cut: a workgroup per request and
+// head, or several that take its rows in turn.  The parts' maxima first, a lane each,
+// then their sums with several parts' loads in flight.
 template <bool BF16, int DIM>
 __global__ __launch_bounds__(kThreads) void join_rows_kernel(RowArgs s, int rows_slot) {
   const int64_t heads = s.a.kv_heads;
   const int64_t r = blockIdx.x / (uint32_t)s.a.kv_heads;
   const int kvh = (int)(blockIdx.x - r * heads);
-  const int i = blockIdx.y;
   const int64_t u0 = s.starts[r], u1 = s.starts[r + 1];
   if (u0 == u1) return;
   const int64_t units = s.starts[s.a.n], runs = runs_of(s, units);
@@ -26,61 +25,65 @@ __global__ __launch_bounds__(kThreads) void join_rows_kernel(RowArgs s, int rows
   Request q;
   int32_t bad = 0;
   if (!attention_request(s.a, s.page.d, r, &q, &bad)) return;
-  if (i >= q.tokens * (int)s.group.d) return;
-  const int tok = (int)div_by((uint32_t)i, s.group);
-  const int h = kvh * (int)s.group.d + i - tok * (int)s.group.d;
+  const int rows = q.tokens * (int)s.group.d;
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
   constexpr int PER = DIM / kWave;
   __shared__ float weight[kMostRuns], sum[kWaves][DIM];
   const int parts = (int)(w1 - w0) + 1;
   // a request that starts inside a run is in the run's second part
   const int64_t first = 2 * w0 + (run_start(units, runs, w0) != u0 ? 1 : 0);
-  auto place = [&](int p) {
-    return ((p == 0 ? first : 2 * (w0 + p)) * heads + kvh) * rows_slot + i;
-  };
-  float m = -INFINITY;
-  for (int p = lane; p < parts; p += kWave) m = fmaxf(m, s.part_ml[place(p) * 2]);
+  for (int i = blockIdx.y; i < rows; i += gridDim.y) {
+    const int tok = (int)div_by((uint32_t)i, s.group);
+    const int h = kvh * (int)s.group.d + i - tok * (int)s.group.d;
+    auto place = [&](int p) {
+      return ((p == 0 ? first : 2 * (w0 + p)) * heads + kvh) * rows_slot + i;
+    };
+    float m = -INFINITY;
+    for (int p = lane; p < parts; p += kWave) m = fmaxf(m, s.part_ml[place(p) * 2]);
 #pragma unroll
-  for (int by = 1; by < kWave; by <<= 1) m = fmaxf(m, __shfl_xor(m, by, kWave));
-  const float base = m == -INFINITY ? 0.0f : m;
-  float l = 0.0f;
-  for (int p = lane; p < parts; p += kWave) {
-    const float mp = s.part_ml[place(p) * 2], lp = s.part_ml[place(p) * 2 + 1];
-    const bool none = mp == -INFINITY && lp == 0.0f;       // saw no key
-    const float f = none ? 0.0f : __builtin_amdgcn_exp2f(mp - base);
-    l += none ? 0.0f : lp * f;
-    if (wave == 0) weight[p] = f;
-  }
-  l = wave_sum(l);
-  __syncthreads();
-  float o[PER];
+    for (int by = 1; by < kWave; by <<= 1) m = fmaxf(m, __shfl_xor(m, by, kWave));
+    const float base = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f;
+    for (int p = lane; p < parts; p += kWave) {
+      const float mp = s.part_ml[place(p) * 2], lp = s.part_ml[place(p) * 2 + 1];
+      const bool none = mp == -INFINITY && lp == 0.0f;       // saw no key
+      const float f = none ? 0.0f : __builtin_amdgcn_exp2f(mp - base);
+      l += none ? 0.0f : lp * f;
+      if (wave == 0) weight[p] = f;
+    }
+    l = wave_sum(l);
+    __syncthreads();
+    float o[PER];
 #pragma unroll
-  for (int e = 0; e < PER; ++e) o[e] = 0.0f;
+    for (int e = 0; e < PER; ++e) o[e] = 0.0f;
 #pragma unroll 4
-  for (int p = wave; p < parts; p += kWaves) {
-    const float f = weight[p];
-    const float* from = s.part_o + place(p) * DIM;
+    for (int p = wave; p < parts; p += kWaves) {
+      const float f = weight[p];
+      const float* from = s.part_o + place(p) * DIM;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) o[e] = __builtin_fmaf(from[e * kWave + lane], f, o[e]);
+      for (int e = 0; e < PER; ++e) o[e] = __builtin_fmaf(from[e * kWave + lane], f, o[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < PER; ++e) sum[wave][e * kWave + lane] = o[e];
+    __syncthreads();
+    if (threadIdx.x < DIM / 2) {
+      const int d = threadIdx.x * 2;
+      float a = 0.0f, b = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        a += sum[w][d];
+        b += sum[w][d + 1];
+      }
+      const bool none = limit_of(q, tok) < 0;
+      const float inv = 1.0f / l;
+      *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(s.a.out) + (q.q0 + tok) * s.a.out_token +
+                                   h * s.a.out_head + d) =
+          none ? 0u : pack2<BF16>(a * inv, b * inv);
+      if (s.a.lse != nullptr && threadIdx.x == 0)
+        s.a.lse[(q.q0 + tok) * s.a.q_heads + h] = none ? -INFINITY : log_sum<BF16>(m, l);
+    }
+    __syncthreads();                     // the next row's weights and sums
   }
-#pragma unroll
-  for (int e = 0; e < PER; ++e) sum[wave][e * kWave + lane] = o[e];
-  __syncthreads();
-  if (threadIdx.x >= DIM / 2) return;
-  const int d = threadIdx.x * 2;
-  float a = 0.0f, b = 0.0f;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    a += sum[w][d];
-    b += sum[w][d + 1];
-  }
-  const bool none = limit_of(q, tok) < 0;
-  const float inv = 1.0f / l;
-  *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(s.a.out) + (q.q0 + tok) * s.a.out_token +
-                               h * s.a.out_head + d) = none ? 0u : pack2<BF16>(a * inv, b * inv);
-  if (s.a.lse != nullptr && threadIdx.x == 0)
-    s.a.lse[(q.q0 + tok) * s.a.q_heads + h] =
-        none ? -INFINITY : log_sum<BF16>(m, l);
 }
 
 }  // namespace
@@ -126,7 +129,13 @@ RowArgs rows::args_of(const AttnCall& a, const Plan& p, void* workspace) {
 
 int rows::join_rows(const RowArgs& s, const Plan& p, hipStream_t stream) {
   if (p.runs == 0) return PAIR_OK;
-  const dim3 grid((unsigned)(s.a.n * s.a.kv_heads), (unsigned)p.rows);
+  // About eight workgroups a compute unit: most find their request uncut, and each takes
+  // a chain of loads and divisions for that (72 requests of which 64 have two rows and
+  // none over 32, 8 heads: 14 us with a workgroup for each of 32 rows, 5 so).
+  const int64_t each = s.a.n * s.a.kv_heads;
+  int64_t turns = 8 * (int64_t)device_cu_count() / each;
+  if (turns > p.rows) turns = p.rows;
+  const dim3 grid((unsigned)each, (unsigned)(turns < 1 ? 1 : turns));
 #define PAIR_JOIN(BF16, DIM)                                                                     \
   hipLaunchKernelGGL((join_rows_kernel<BF16, DIM>), grid, dim3(kThreads), 0, stream, s, 16 * p.tiles)
   if (s.a.dim == 64) {

@@ -316,6 +316,20 @@ PyObject* written(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+// on_device(device, tensor or None, ...): whether all are on that device.
+PyObject* on_device(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n < 1 || !PyLong_Check(args[0])) {
+    PyErr_SetString(PyExc_TypeError, "on_device(device, tensor, ...)");
+    return nullptr;
+  }
+  const long device = PyLong_AsLong(args[0]);
+  if (device == -1 && PyErr_Occurred()) return nullptr;
+  for (Py_ssize_t i = 1; i < n; ++i)
+    if (THPVariable_Check(args[i]) && THPVariable_Unpack(args[i]).get_device() != device)
+      Py_RETURN_FALSE;
+  Py_RETURN_TRUE;
+}
+
 PyMethodDef kMethods[] = {
     {"grad_table", grad_table, METH_VARARGS,
      "grad_table(list, name): addresses, sizes and type codes of GPU tensors, as bytes."},
@@ -333,6 +347,8 @@ PyMethodDef kMethods[] = {
     {"parts", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(parts)),
      METH_FASTCALL,
      "parts(device, dtype, shape, ...): uninitialised GPU tensors of one allocation."},
+    {"on_device", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(on_device)),
+     METH_FASTCALL, "on_device(device, tensor or None, ...): whether all are there."},
     {"written", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(written)),
      METH_FASTCALL, "written(tensor, list or None, ...): counts a write to each tensor."},
     {nullptr, nullptr, 0, nullptr}};
