@@ -1040,12 +1040,18 @@ def cache_load_mx(slots, k_cache, v_cache, k_scale, v_scale, dtype=torch.bfloat1
     return {"k": k, "v": v, "status": st}
 
 
+# Workspaces up to this size are cut from the results' allocation: each further one
+# takes 1.1 us, of a call that takes 13.
+_SHARED_BYTES = 1 << 20
+
+
 @_allocating
 def paged_attention_mx(q, k_cache, v_cache, k_scale, v_scale, table, q_offsets, lens, max_q,
                        max_len, scale=None, want_lse=False, out=None, workspace=None, stream=None):
     """paged_attention over a cache in 8 or 4 bits, read as it is: q, bfloat16 or
     float16, is the type that its values are taken in (exactly, if they were stored
-    from it).  All else as for paged_attention."""
+    from it).  All else as for paged_attention; results may share a storage with each
+    other and with a workspace of up to 1 MB (clone what is to last)."""
     if ((q.requires_grad or k_cache.requires_grad or v_cache.requires_grad) and out is None
             and torch.is_grad_enabled()):
         out, lse, st = _NoGradient.apply(
@@ -1055,15 +1061,22 @@ def paged_attention_mx(q, k_cache, v_cache, k_scale, v_scale, table, q_offsets, 
         return {"out": out, "lse": lse, "status": st}
     tokens, heads, dim = q.shape
     parts, index, lse = _native().parts, q.get_device(), None
-    if out is None:
-        out, = parts(index, q.dtype, (tokens, heads, dim))
-    if want_lse:
-        lse, = parts(index, torch.float32, (tokens, heads))
     max_q, max_len = int(max_q), int(max_len)
     need = _attention_mx_workspace(_device_index(), lens.numel(), tokens, heads, k_cache.shape[2],
                                    dim, PAIR_MXFP8 if k_cache.dtype == _MX_CODES[0] else PAIR_MXFP4,
                                    max_q, max_len)
-    if workspace is None or workspace.numel() < need:
+    if workspace is not None and workspace.numel() < need:
+        workspace = None
+    if out is None and workspace is None and want_lse and need <= _SHARED_BYTES:
+        out, lse, workspace = parts(index, q.dtype, (tokens, heads, dim), torch.float32,
+                                    (tokens, heads), torch.uint8, need)
+    elif out is None and workspace is None and need <= _SHARED_BYTES:
+        out, workspace = parts(index, q.dtype, (tokens, heads, dim), torch.uint8, need)
+    if out is None:
+        out, = parts(index, q.dtype, (tokens, heads, dim))
+    if want_lse and lse is None:
+        lse, = parts(index, torch.float32, (tokens, heads))
+    if workspace is None:
         workspace, = parts(index, torch.uint8, need)
     st = _status(q.device)
     pair_paged_attention_mx(q, k_cache, v_cache, k_scale, v_scale, table, q_offsets, lens, max_q,

@@ -232,6 +232,24 @@ def test_bounds_are_only_bounds():
         c.check(a)
 
 
+def test_given_results_and_workspaces():
+    """Results and workspaces of the caller's, too small ones among them: the same bits."""
+    log("mx attention: given results and workspaces")
+    c = Cache([1500, 3000], [1, 2], 8, 2, 128, 16, "f16", seed=13, bits=4)
+    args = (c.q, *c.tensors(), *c.arguments(), 2, 3000)
+    want = pair.paged_attention_mx(*args, want_lse=True)
+    need = pair.pair_paged_attention_mx_workspace_bytes(2, 3, 8, 2, 128, pair.PAIR_MXFP4, 2, 3000)
+    assert need > 256
+    for out in (None, torch.full_like(c.q, 7.0)):
+        for size in (None, 256, need, need + 4096):
+            ws = None if size is None else torch.full((size,), 255, dtype=torch.uint8, device=DEV)
+            for lse in (False, True):
+                r = pair.paged_attention_mx(*args, want_lse=lse, out=out, workspace=ws)
+                torch.cuda.synchronize()
+                assert torch.equal(r["out"], want["out"]) and (out is None or r["out"] is out)
+                assert (r["lse"] is None) if not lse else torch.equal(r["lse"], want["lse"])
+
+
 def test_status_of_bad_requests():
     log("mx attention: bad requests")
     for what in ("len", "page", "offsets", "narrow"):
