@@ -50,7 +50,8 @@ extern "C" {
 #define PAIR_EDTYPE (-2)     /* a dtype that the call does not take             */
 #define PAIR_ERANGE (-3)     /* gmax outside [2, 64], D < 1, R < 1, ld < D ...  */
 #define PAIR_EALIGN (-4)     /* scores, caches or rows: a base or stride not
-                                16-byte aligned; gradients: not to an element  */
+                                16-byte aligned; gradients: not to an element;
+                                scales of a cache: not to their row           */
 #define PAIR_EHIP (-5)       /* a HIP launch or runtime call failed             */
 #define PAIR_EWORKSPACE (-6) /* workspace missing, misaligned or too small      */
 #define PAIR_ESCRATCH (-7)   /* one prompt's audit needs more than the static

@@ -508,9 +508,10 @@ __device__ __forceinline__ void add_codes(const RowArgs& s,
       for (int nt = 0; nt < NT; ++nt) {
         sc[nt][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int j = 0; j < DIM / 32; ++j)
-          if (nt < tiles) sc[nt][t] = mma16<BF16>(u32x4_t{kf[4 * j], kf[4 * j + 1], kf[4 * j + 2], kf[4 * j + 3]},
-                                  qf[nt][j], sc[nt][t]);
+        for (int j = 0; j < DIM / 32; ++j) {
+          const u32x4_t eight = {kf[4 * j], kf[4 * j + 1], kf[4 * j + 2], kf[4 * j + 3]};
+          if (nt < tiles) sc[nt][t] = mma16<BF16>(eight, qf[nt][j], sc[nt][t]);
+        }
       }
     }
     Piece<DIM> vr[8];

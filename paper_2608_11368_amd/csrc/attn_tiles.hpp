@@ -306,7 +306,8 @@ __device__ __forceinline__ void attend_tile(const TileArgs& s, uint32_t block,
   constexpr int NC = DIM / 16;              // k pieces of a score product
   constexpr int ND = DIM / 32;              // dim tiles of the output
   // A lane's piece of a row: 16 bytes in memory (8 of 4 bits at width 64), kPut
-  // times 16 in LDS.
+  // times 16 in LDS.  (Pieces of eight elements in 8 bits, three chunks of 1501 to 2048
+  // tokens after 6000 keys: 648 us, 632 so.)
   constexpr int kOwn = BITS == 16 ? 8 : BITS == 4 && DIM == 128 ? 32 : 16;   // elements
   constexpr int kPut = kOwn / 8;
   constexpr int kPer = DIM / kOwn;          // pieces of a row
