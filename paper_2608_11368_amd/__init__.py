@@ -525,12 +525,23 @@ def pair_paged_attention(q, k_cache, v_cache, table, q_offsets, lens, max_q, max
 
 
 _MX_CODES = (torch.float8_e4m3fn, torch.float4_e2m1fn_x2)
-_HALF_CODES = {torch.bfloat16: PAIR_BF16, torch.float16: PAIR_F16}
+_HALVES = (torch.bfloat16, torch.float16)
+_functions = {}
 
 
-def _mx_refused(k_cache, v_cache, k_scale, v_scale):
-    for name, c in (("k_cache", k_cache), ("v_cache", v_cache), ("k_scale", k_scale),
-                    ("v_scale", v_scale)):
+def _function(name):
+    """The address of a C entry point, for the native calls."""
+    at = _functions.get(name)
+    if at is None:
+        at = _functions[name] = ctypes.cast(getattr(lib(), name), ctypes.c_void_p).value
+    return at
+
+
+def _mx_refused(k_cache, v_cache, k_scale, v_scale, **tensors):
+    """Why the native call took no such tensors: raises, or returns the heads' width
+    where the caches and their devices are as they should be."""
+    cache = (("k_cache", k_cache), ("v_cache", v_cache), ("k_scale", k_scale), ("v_scale", v_scale))
+    for name, c in cache:
         if not isinstance(c, torch.Tensor) or not c.is_cuda or c.dim() != 4:
             raise ValueError(f"{name} must be a 4-D CUDA tensor [pages][page][kv_heads][..]")
     if k_cache.dtype not in _MX_CODES or v_cache.dtype != k_cache.dtype:
@@ -543,65 +554,54 @@ def _mx_refused(k_cache, v_cache, k_scale, v_scale):
     if k_scale.shape[:3] != k_cache.shape[:3] or k_scale.shape[3] * 32 != dim:
         raise ValueError(f"rows of {dim} elements need a scale for every 32 of them, got "
                          f"{tuple(k_scale.shape)} for {tuple(k_cache.shape)}")
-    raise ValueError("keys and values must be on one device, with the same strides and "
-                     "contiguous rows")
+    if (v_cache.stride() != k_cache.stride() or v_scale.stride() != k_scale.stride()
+            or k_cache.stride(3) != 1 or (k_scale.stride(3) != 1 and k_scale.shape[3] > 1)):
+        raise ValueError("keys and values must have the same strides and contiguous rows")
+    for name, t in (*cache, *tensors.items()):     # kernels run on the current device's stream
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != _device_index():
+            raise ValueError(f"{name} is on cuda:{t.get_device()}, the current device is "
+                             f"cuda:{_device_index()}")
+    return dim
 
 
-def _one_device(native, device, *tensors):
-    """Kernels run on the current device's stream: every tensor has to be there."""
-    if device != _device_index():
-        raise ValueError(f"the caches are on cuda:{device}, the current device is "
-                         f"cuda:{_device_index()}")
-    if not native.on_device(device, *tensors):
-        raise ValueError(f"every tensor must be on cuda:{device} like the caches")
-
-
-def _half_code(t, name):
-    code = _HALF_CODES.get(t.dtype) if isinstance(t, torch.Tensor) else None
-    if code is None:
+def _half_rows(t, name, dtype, heads, dim):
+    if dtype is None and (not isinstance(t, torch.Tensor) or t.dtype not in _HALVES):
         raise TypeError(f"{name} must be a bfloat16 or float16 tensor")
-    return code
+    dtype = t.dtype if dtype is None else dtype
+    if _native().rows(t, PAIR_BF16 if dtype == torch.bfloat16 else PAIR_F16, heads, dim) is None:
+        _rows_refused(t, name, dtype, heads, dim)
 
 
-def _pair_of_rows(native, k, v, code, heads, dim):
-    """Addresses, strides and the count of the rows of two like tensors."""
-    kp, tok, head, tokens, _ = (native.rows(k, code, heads, dim)
-                                or _rows_refused(k, "k", k.dtype, heads, dim))
-    vp, vtok, vhead, vtokens, _ = (native.rows(v, code, heads, dim)
-                                   or _rows_refused(v, "v", k.dtype, heads, dim))
-    if vtok != tok or vhead != head or vtokens != tokens:
+def _move_refused(k, v, slots, cache, d_status):
+    dim = _mx_refused(*cache, k=k, v=v, slots=slots, d_status=d_status)
+    _half_rows(k, "k", None, cache[0].shape[2], dim)
+    _half_rows(v, "v", k.dtype, cache[0].shape[2], dim)
+    if v.stride() != k.stride() or v.shape != k.shape:
         raise ValueError("k and v must have the same shape and strides")
-    return kp, vp, tok, head, tokens
+    _native().address(slots, "slots", torch.int64, k.shape[0])
+    _native().address(d_status, "d_status", torch.int32, 1, True)
+    raise ValueError("a size is out of range")
 
 
 def pair_cache_store_mx(k, v, slots, k_cache, v_cache, k_scale, v_scale, d_status=None,
                         stream=None):
     native = _native()
-    cache, heads, dim, device = (native.mx_cache(k_cache, v_cache, k_scale, v_scale)
-                                 or _mx_refused(k_cache, v_cache, k_scale, v_scale))
-    code = _half_code(k, "k")
-    kp, vp, tok, head, tokens = _pair_of_rows(native, k, v, code, heads, dim)
-    _one_device(native, device, k, v, slots, d_status)
-    _rc(lib().pair_cache_store_mx(
-        cache, tokens, code, kp, vp, tok, head,
-        native.address(slots, "slots", torch.int64, tokens),
-        native.address(d_status, "d_status", torch.int32, 1, True), _stream(stream)),
-        "pair_cache_store_mx")
+    code = native.store_mx(_function("pair_cache_store_mx"), k, v, slots, k_cache, v_cache, k_scale,
+                           v_scale, d_status, _device_index(), _stream(stream))
+    if code is None:
+        _move_refused(k, v, slots, (k_cache, v_cache, k_scale, v_scale), d_status)
+    _rc(code, "pair_cache_store_mx")
     native.written(k_cache, v_cache, k_scale, v_scale)
 
 
 def pair_cache_load_mx(slots, k_cache, v_cache, k_scale, v_scale, k, v, d_status=None,
                        stream=None):
     native = _native()
-    cache, heads, dim, device = (native.mx_cache(k_cache, v_cache, k_scale, v_scale)
-                                 or _mx_refused(k_cache, v_cache, k_scale, v_scale))
-    code = _half_code(k, "k")
-    kp, vp, tok, head, tokens = _pair_of_rows(native, k, v, code, heads, dim)
-    _one_device(native, device, k, v, slots, d_status)
-    _rc(lib().pair_cache_load_mx(
-        cache, tokens, native.address(slots, "slots", torch.int64, tokens), code, kp, vp, tok, head,
-        native.address(d_status, "d_status", torch.int32, 1, True), _stream(stream)),
-        "pair_cache_load_mx")
+    code = native.load_mx(_function("pair_cache_load_mx"), k, v, slots, k_cache, v_cache, k_scale,
+                          v_scale, d_status, _device_index(), _stream(stream))
+    if code is None:
+        _move_refused(k, v, slots, (k_cache, v_cache, k_scale, v_scale), d_status)
+    _rc(code, "pair_cache_load_mx")
     native.written(k, v)
 
 
@@ -611,31 +611,36 @@ def pair_paged_attention_mx_workspace_bytes(n, tokens, q_heads, kv_heads, dim, f
                                                              format, max_q, max_len))
 
 
+def _attention_mx_refused(q, cache, table, q_offsets, lens, out, lse, workspace, d_status):
+    dim = _mx_refused(*cache, q=q, out=out, table=table, q_offsets=q_offsets, lens=lens, lse=lse,
+                      workspace=workspace, d_status=d_status)
+    _half_rows(q, "q", None, 0, dim)
+    _half_rows(out, "out", q.dtype, q.shape[1], dim)
+    at, n, tokens = _native().address, lens.numel(), q.shape[0]
+    if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[0] < n:
+        raise ValueError("table must be a 2-D tensor with a row for each request")
+    if out.shape[0] < tokens:
+        raise ValueError(f"out holds {out.shape[0]} tokens, needs {tokens}")
+    at(table, "table", torch.int32)
+    at(q_offsets, "q_offsets", torch.int64, n + 1)
+    at(lens, "lens", torch.int32, n)
+    at(lse, "lse", torch.float32, tokens * q.shape[1], True)
+    at(workspace, "workspace", torch.uint8)
+    at(d_status, "d_status", torch.int32, 1, True)
+    raise ValueError("a size is out of range")
+
+
 def pair_paged_attention_mx(q, k_cache, v_cache, k_scale, v_scale, table, q_offsets, lens, max_q,
                             max_len, scale, out, lse, workspace, d_status=None, stream=None):
     native = _native()
-    cache, _, dim, device = (native.mx_cache(k_cache, v_cache, k_scale, v_scale)
-                             or _mx_refused(k_cache, v_cache, k_scale, v_scale))
-    code = _half_code(q, "q")
-    qp, qt, qh, tokens, heads = (native.rows(q, code, 0, dim)
-                                 or _rows_refused(q, "q", q.dtype, 0, dim))
-    op, ot, oh, orows, _ = (native.rows(out, code, heads, dim)
-                            or _rows_refused(out, "out", q.dtype, heads, dim))
-    n = lens.numel()
-    if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[0] < n:
-        raise ValueError("table must be a 2-D tensor with a row for each request")
-    if orows < tokens:
-        raise ValueError(f"out holds {orows} tokens, needs {tokens}")
-    _one_device(native, device, q, out, table, q_offsets, lens, lse, workspace, d_status)
-    at = native.address
-    _rc(lib().pair_paged_attention_mx(
-        cache, n, tokens, heads, code, qp, qt, qh, at(table, "table", torch.int32), table.shape[1],
-        at(q_offsets, "q_offsets", torch.int64, n + 1), at(lens, "lens", torch.int32, n),
-        int(max_q), int(max_len), float(scale), op, ot, oh,
-        at(lse, "lse", torch.float32, tokens * heads, True),
-        at(workspace, "workspace", torch.uint8), workspace.numel(),
-        at(d_status, "d_status", torch.int32, 1, True), _stream(stream)),
-        "pair_paged_attention_mx")
+    code = native.attention_mx(_function("pair_paged_attention_mx"), q, k_cache, v_cache, k_scale,
+                               v_scale, table, q_offsets, lens, int(max_q), int(max_len),
+                               float(scale), out, lse, workspace, d_status, _device_index(),
+                               _stream(stream))
+    if code is None:
+        _attention_mx_refused(q, (k_cache, v_cache, k_scale, v_scale), table, q_offsets, lens, out,
+                              lse, workspace, d_status)
+    _rc(code, "pair_paged_attention_mx")
     native.written(out, lse)
 
 
@@ -1041,7 +1046,7 @@ def cache_load_mx(slots, k_cache, v_cache, k_scale, v_scale, dtype=torch.bfloat1
 
 
 # Workspaces up to this size are cut from the results' allocation: each further one
-# takes 1.1 us, of a call that takes 13.
+# takes 1.1 us, of a call that takes 9.
 _SHARED_BYTES = 1 << 20
 
 

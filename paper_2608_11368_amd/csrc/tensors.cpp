@@ -6,7 +6,6 @@
 #include <Python.h>
 
 #include <exception>
-#include <string.h>
 
 #include <ATen/ops/empty.h>
 #include <torch/csrc/Dtype.h>
@@ -151,51 +150,162 @@ PyObject* cache(PyObject*, PyObject* const* args, Py_ssize_t n) {
   }
 }
 
-// mx_cache(k_cache, v_cache, k_scale, v_scale) -> (pair_mx_cache as bytes, heads,
-// width, device), or None if they are not a cache in 8 or 4 bits on one device.
-PyObject* mx_cache(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 4) {
-    PyErr_SetString(PyExc_TypeError, "mx_cache(k_cache, v_cache, k_scale, v_scale)");
+// The four tensors of a cache in 8 or 4 bits on `device` as the C ABI's struct.
+bool mx_struct(PyObject* const* args, int device, pair_mx_cache* c) {
+  for (int i = 0; i < 4; ++i)
+    if (!THPVariable_Check(args[i])) return false;
+  const at::Tensor &k = THPVariable_Unpack(args[0]), &v = THPVariable_Unpack(args[1]),
+                   &ks = THPVariable_Unpack(args[2]), &vs = THPVariable_Unpack(args[3]);
+  const bool wide = k.scalar_type() == at::kFloat8_e4m3fn;
+  if (!k.is_cuda() || !v.is_cuda() || !ks.is_cuda() || !vs.is_cuda() || k.dim() != 4 ||
+      (!wide && k.scalar_type() != at::kFloat4_e2m1fn_x2) || v.scalar_type() != k.scalar_type() ||
+      ks.scalar_type() != at::kFloat8_e8m0fnu || vs.scalar_type() != at::kFloat8_e8m0fnu ||
+      v.sizes() != k.sizes() || v.strides() != k.strides() || ks.dim() != 4 ||
+      vs.sizes() != ks.sizes() || vs.strides() != ks.strides() || k.stride(3) != 1 ||
+      (ks.stride(3) != 1 && ks.size(3) > 1) || k.get_device() != device ||
+      v.get_device() != device || ks.get_device() != device || vs.get_device() != device)
+    return false;
+  const int64_t dim = wide ? k.size(3) : 2 * k.size(3);
+  if (ks.size(0) != k.size(0) || ks.size(1) != k.size(1) || ks.size(2) != k.size(2) ||
+      ks.size(3) * 32 != dim || k.size(1) > INT32_MAX || k.size(2) > INT32_MAX || dim > INT32_MAX)
+    return false;
+  c->k = k.data_ptr();
+  c->v = v.data_ptr();
+  c->k_scale = ks.data_ptr();
+  c->v_scale = vs.data_ptr();
+  c->page_stride = k.stride(0);
+  c->slot_stride = k.stride(1);
+  c->head_stride = k.stride(2);
+  c->scale_page = ks.stride(0);
+  c->scale_slot = ks.stride(1);
+  c->scale_head = ks.stride(2);
+  c->n_pages = k.size(0);
+  c->page = (int32_t)k.size(1);
+  c->kv_heads = (int32_t)k.size(2);
+  c->dim = (int32_t)dim;
+  c->format = wide ? PAIR_MXFP8 : PAIR_MXFP4;
+  return true;
+}
+
+// A contiguous tensor of a type and a least size on `device`, or (if `optional`) None.
+bool flat(PyObject* x, at::ScalarType type, int64_t least, int device, bool optional, void** at) {
+  *at = nullptr;
+  if (x == Py_None) return optional;
+  if (!THPVariable_Check(x)) return false;
+  const at::Tensor& t = THPVariable_Unpack(x);
+  if (!t.is_cuda() || t.get_device() != device || t.scalar_type() != type || !t.is_contiguous() ||
+      t.numel() < least)
+    return false;
+  *at = t.data_ptr();
+  return true;
+}
+
+// 16-bit rows [rows][heads][width] of a type code (0: either) and of `heads` (0: any).
+struct Rows {
+  void* at;
+  int64_t row, head, count, heads;
+  int32_t code;
+};
+
+bool half_rows(PyObject* x, int32_t code, int64_t heads, int64_t width, int device, Rows* r) {
+  if (!THPVariable_Check(x)) return false;
+  const at::Tensor& t = THPVariable_Unpack(x);
+  if (!t.is_cuda() || t.get_device() != device || t.dim() != 3 || !half(t) ||
+      (code != 0 && dtype_code(t.scalar_type()) != code) || t.size(2) != width ||
+      t.stride(2) != 1 || (heads != 0 && t.size(1) != heads))
+    return false;
+  *r = {t.data_ptr(), t.stride(0), t.stride(1), t.size(0), t.size(1), dtype_code(t.scalar_type())};
+  return true;
+}
+
+// An address or a handle given as an int.
+void* pointer(PyObject* x) { return PyLong_AsVoidPtr(x); }
+
+// The calls of such a cache, whole: read through the interpreter their arguments take
+// 3 us, as long as the launch.  Each takes the C function's address first and
+// returns its code, or None if some tensor is not as the call needs it.
+
+// store_mx(function, k, v, slots, k_cache, v_cache, k_scale, v_scale, status or None,
+// device, stream), load_mx(...) the same.
+template <bool STORE>
+PyObject* move_mx(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 11) {
+    PyErr_SetString(PyExc_TypeError, "eleven arguments");
     return nullptr;
   }
-  for (Py_ssize_t i = 0; i < 4; ++i)
-    if (!THPVariable_Check(args[i])) Py_RETURN_NONE;
+  void *function = pointer(args[0]), *stream = pointer(args[10]);
+  const int device = (int)PyLong_AsLong(args[9]);
+  if (PyErr_Occurred()) return nullptr;
   try {
-    const at::Tensor &k = THPVariable_Unpack(args[0]), &v = THPVariable_Unpack(args[1]),
-                     &ks = THPVariable_Unpack(args[2]), &vs = THPVariable_Unpack(args[3]);
-    const bool wide = k.scalar_type() == at::kFloat8_e4m3fn;
-    if (!k.is_cuda() || !v.is_cuda() || !ks.is_cuda() || !vs.is_cuda() || k.dim() != 4 ||
-        (!wide && k.scalar_type() != at::kFloat4_e2m1fn_x2) ||
-        v.scalar_type() != k.scalar_type() || ks.scalar_type() != at::kFloat8_e8m0fnu ||
-        vs.scalar_type() != at::kFloat8_e8m0fnu || v.sizes() != k.sizes() ||
-        v.strides() != k.strides() || ks.dim() != 4 || vs.sizes() != ks.sizes() ||
-        vs.strides() != ks.strides() || k.stride(3) != 1 ||
-        (ks.stride(3) != 1 && ks.size(3) > 1) || v.get_device() != k.get_device() ||
-        ks.get_device() != k.get_device() || vs.get_device() != k.get_device())
-      Py_RETURN_NONE;
-    const int64_t dim = wide ? k.size(3) : 2 * k.size(3);
-    if (ks.size(0) != k.size(0) || ks.size(1) != k.size(1) || ks.size(2) != k.size(2) ||
-        ks.size(3) * 32 != dim || k.size(1) > INT32_MAX || k.size(2) > INT32_MAX || dim > INT32_MAX)
-      Py_RETURN_NONE;
     pair_mx_cache c;
-    memset(&c, 0, sizeof(c));
-    c.k = k.data_ptr();
-    c.v = v.data_ptr();
-    c.k_scale = ks.data_ptr();
-    c.v_scale = vs.data_ptr();
-    c.page_stride = k.stride(0);
-    c.slot_stride = k.stride(1);
-    c.head_stride = k.stride(2);
-    c.scale_page = ks.stride(0);
-    c.scale_slot = ks.stride(1);
-    c.scale_head = ks.stride(2);
-    c.n_pages = k.size(0);
-    c.page = (int32_t)k.size(1);
-    c.kv_heads = (int32_t)k.size(2);
-    c.dim = (int32_t)dim;
-    c.format = wide ? PAIR_MXFP8 : PAIR_MXFP4;
-    return Py_BuildValue("y#iii", reinterpret_cast<const char*>(&c), (Py_ssize_t)sizeof(c),
-                         (int)c.kv_heads, (int)c.dim, (int)k.get_device());
+    Rows k, v;
+    void *slots, *status;
+    if (!mx_struct(args + 4, device, &c) || !half_rows(args[1], 0, c.kv_heads, c.dim, device, &k) ||
+        !half_rows(args[2], k.code, c.kv_heads, c.dim, device, &v) || v.row != k.row ||
+        v.head != k.head || v.count != k.count ||
+        !flat(args[3], at::kLong, k.count, device, false, &slots) ||
+        !flat(args[8], at::kInt, 1, device, true, &status))
+      Py_RETURN_NONE;
+    int code;
+    Py_BEGIN_ALLOW_THREADS
+    if (STORE)
+      code = reinterpret_cast<decltype(&pair_cache_store_mx)>(function)(
+          &c, k.count, k.code, k.at, v.at, k.row, k.head, static_cast<const int64_t*>(slots),
+          static_cast<int32_t*>(status), stream);
+    else
+      code = reinterpret_cast<decltype(&pair_cache_load_mx)>(function)(
+          &c, k.count, static_cast<const int64_t*>(slots), k.code, k.at, v.at, k.row, k.head,
+          static_cast<int32_t*>(status), stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(code);
+  } catch (...) {
+    torch::translate_exception_to_python(std::current_exception());
+    return nullptr;
+  }
+}
+
+// attention_mx(function, q, k_cache, v_cache, k_scale, v_scale, table, q_offsets, lens,
+// max_q, max_len, scale, out, lse or None, workspace, status or None, device, stream).
+PyObject* attention_mx(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 18) {
+    PyErr_SetString(PyExc_TypeError, "eighteen arguments");
+    return nullptr;
+  }
+  void *function = pointer(args[0]), *stream = pointer(args[17]);
+  const int device = (int)PyLong_AsLong(args[16]);
+  const long long max_q = PyLong_AsLongLong(args[9]), max_len = PyLong_AsLongLong(args[10]);
+  const double scale = PyFloat_AsDouble(args[11]);
+  if (PyErr_Occurred()) return nullptr;
+  try {
+    pair_mx_cache c;
+    Rows q, out;
+    void *offsets, *lens, *lse, *workspace, *status, *table;
+    if (!mx_struct(args + 2, device, &c) || !half_rows(args[1], 0, 0, c.dim, device, &q) ||
+        !half_rows(args[12], q.code, q.heads, c.dim, device, &out) || out.count < q.count ||
+        !flat(args[8], at::kInt, 0, device, false, &lens) ||
+        !flat(args[6], at::kInt, 0, device, false, &table) || max_q < INT32_MIN ||
+        max_q > INT32_MAX || max_len < INT32_MIN || max_len > INT32_MAX || q.heads > INT32_MAX)
+      Py_RETURN_NONE;
+    const at::Tensor& rows = THPVariable_Unpack(args[6]);
+    const int64_t requests = THPVariable_Unpack(args[8]).numel();
+    if (rows.dim() != 2 || rows.size(0) < requests ||
+        !flat(args[7], at::kLong, requests + 1, device, false, &offsets) ||
+        !flat(args[13], at::kFloat, q.count * q.heads, device, true, &lse) ||
+        !flat(args[14], at::kByte, 0, device, false, &workspace) ||
+        !flat(args[15], at::kInt, 1, device, true, &status))
+      Py_RETURN_NONE;
+    const size_t bytes = (size_t)THPVariable_Unpack(args[14]).numel();
+    const int64_t width = rows.size(1);
+    int code;
+    Py_BEGIN_ALLOW_THREADS
+    code = reinterpret_cast<decltype(&pair_paged_attention_mx)>(function)(
+        &c, requests, q.count, (int32_t)q.heads, q.code, q.at, q.row, q.head,
+        static_cast<const int32_t*>(table), width, static_cast<const int64_t*>(offsets),
+        static_cast<const int32_t*>(lens), (int32_t)max_q, (int32_t)max_len, (float)scale, out.at,
+        out.row, out.head, static_cast<float*>(lse), workspace, bytes,
+        static_cast<int32_t*>(status), stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(code);
   } catch (...) {
     torch::translate_exception_to_python(std::current_exception());
     return nullptr;
@@ -316,20 +426,6 @@ PyObject* written(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
-// on_device(device, tensor or None, ...): whether all are on that device.
-PyObject* on_device(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n < 1 || !PyLong_Check(args[0])) {
-    PyErr_SetString(PyExc_TypeError, "on_device(device, tensor, ...)");
-    return nullptr;
-  }
-  const long device = PyLong_AsLong(args[0]);
-  if (device == -1 && PyErr_Occurred()) return nullptr;
-  for (Py_ssize_t i = 1; i < n; ++i)
-    if (THPVariable_Check(args[i]) && THPVariable_Unpack(args[i]).get_device() != device)
-      Py_RETURN_FALSE;
-  Py_RETURN_TRUE;
-}
-
 PyMethodDef kMethods[] = {
     {"grad_table", grad_table, METH_VARARGS,
      "grad_table(list, name): addresses, sizes and type codes of GPU tensors, as bytes."},
@@ -338,17 +434,17 @@ PyMethodDef kMethods[] = {
      "address(tensor, name, dtype, least=0, optional=False): a checked tensor's data pointer."},
     {"cache", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(cache)),
      METH_FASTCALL, "cache(k_cache, v_cache): addresses and layout, None if it is no cache."},
-    {"mx_cache", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(mx_cache)),
-     METH_FASTCALL,
-     "mx_cache(k_cache, v_cache, k_scale, v_scale): (pair_mx_cache, heads, width, device), "
-     "or None."},
+    {"store_mx", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(move_mx<true>)),
+     METH_FASTCALL, "pair_cache_store_mx with tensors: its code, or None if one does not fit."},
+    {"load_mx", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(move_mx<false>)),
+     METH_FASTCALL, "pair_cache_load_mx with tensors: its code, or None if one does not fit."},
+    {"attention_mx", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(attention_mx)),
+     METH_FASTCALL, "pair_paged_attention_mx with tensors: its code, or None if one does not fit."},
     {"rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(rows)),
      METH_FASTCALL, "rows(tensor, type code, heads, width): address and layout, or None."},
     {"parts", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(parts)),
      METH_FASTCALL,
      "parts(device, dtype, shape, ...): uninitialised GPU tensors of one allocation."},
-    {"on_device", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(on_device)),
-     METH_FASTCALL, "on_device(device, tensor or None, ...): whether all are there."},
     {"written", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(written)),
      METH_FASTCALL, "written(tensor, list or None, ...): counts a write to each tensor."},
     {nullptr, nullptr, 0, nullptr}};

@@ -402,6 +402,7 @@ def test_tensors_of_another_device(monkeypatch):
     slots = torch.arange(3, device=DEV)
     k = torch.zeros((3, 2, 64), dtype=torch.bfloat16, device=DEV)
     monkeypatch.setattr(pair, "_device_index", lambda: 1)
+    monkeypatch.setattr(pair, "_stream", lambda stream: 0)
     out, ws = torch.empty_like(c.q), torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
     for call in (lambda: pair.pair_paged_attention_mx(c.q, *cache, *args, 0.1, out, None, ws),
                  lambda: pair.pair_cache_store_mx(k, k, slots, *cache),
