@@ -178,6 +178,30 @@ def test_many_requests(n, case, bits):
     c.check(c.call(), only=[0, 3, 5, 7, 8, 9, 63, 64, 65, n // 2, n - 2, n - 1])
 
 
+def test_16_million_requests():
+    """A token each over one shared page, as many workgroups as a launch can have: all
+    the same, and the same as of few."""
+    n = (1 << 24) - 1
+    log(f"mx attention: {n} requests")
+    cache = pair.mx_cache(1, 16, 1, 64, torch.float4_e2m1fn_x2)
+    rows = torch.randn((2, 16, 1, 64), device=DEV).bfloat16()
+    pair.cache_store_mx(rows[0], rows[1], torch.arange(16, device=DEV), *cache)
+    q = torch.randn((1, 1, 64), device=DEV).bfloat16()
+
+    def call(n):
+        return pair.paged_attention_mx(q.expand(n, 1, 64), *cache,
+                                       torch.zeros((n, 1), dtype=torch.int32, device=DEV),
+                                       torch.arange(n + 1, device=DEV),
+                                       torch.full((n,), 7, dtype=torch.int32, device=DEV), 1, 7)
+
+    r, few = call(n), call(5)
+    torch.cuda.synchronize()
+    assert int(r["status"].item()) == 0 and int(few["status"].item()) == 0
+    assert bool((r["out"] == few["out"][0]).all()) and bool(few["out"].any())
+    with pytest.raises(pair.PairError, match="size out of the supported range"):
+        call(n + 1)
+
+
 @pytest.mark.parametrize("bits", [8, 4])
 @pytest.mark.parametrize("page", [16, 20])
 @pytest.mark.parametrize("dim,dtype", [(64, "bf16"), (128, "f16")])
