@@ -98,14 +98,18 @@ Plan rows::plan_of(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim, in
   // eight steps, which take less than the second launch would (4 requests of 700
   // keys: 8.0 us uncut, 9.5 us cut; of 1000: 9.3 and 9.9; of 2000: 21 and 11; 32
   // requests of 1000: 22 and 27), or the requests are so many that they fill the
-  // card by themselves.
+  // card by themselves.  In 8 and 4 bits 16 steps, with the next block on its way: in 8
+  // bits, 8 heads of 128, uncut and cut, 4 requests of 1500 keys 15.7 and 16.0 us, 16
+  // 16.5 and 21, 64 36 and 42, 128 68 and 76, 256 of 300 41 and 52; five tokens of 64
+  // 43 and 63.  (32 steps: 256 of 1000, up to 4000, 97 and 100, of two heads 41 and 37.)
+  const int whole = bits == 16 ? 8 : 16;
   const int64_t most = n * ((max_len + kUnit - 1) / kUnit);
   const int per_cu = p.tiles == 1 ? groups_per_cu(bits, dim) : 2;
   int64_t runs = per_cu * (int64_t)device_cu_count() / kv_heads;
   if (runs > most) runs = most;
   if (runs > kMostRuns) runs = kMostRuns;
   if (runs < 1) runs = 1;
-  p.runs = n > kMostScanned || max_len <= 8 * kUnit || most > 0x7fffffff ? 0 : (int32_t)runs;
+  p.runs = n > kMostScanned || max_len <= whole * kUnit || most > 0x7fffffff ? 0 : (int32_t)runs;
   const size_t parts = 2 * (size_t)p.runs * kv_heads * 16 * p.tiles;
   p.starts = ((size_t)(n + 1) * 4 + 255) / 256 * 256;
   p.ml = (parts * 8 + 255) / 256 * 256;

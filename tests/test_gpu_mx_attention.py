@@ -219,7 +219,7 @@ def test_chunks_beside_few(new, past, only, dim, dtype, page, bits):
 
 
 @pytest.mark.parametrize("bits", [8, 4])
-@pytest.mark.parametrize("n,most", [(3, 1024), (3, 1025), (140, 1024), (140, 1025)])
+@pytest.mark.parametrize("n,most", [(3, 1025), (3, 2048), (3, 2049), (140, 2048), (140, 2049)])
 @pytest.mark.parametrize("page", [16, 20])
 def test_short_requests_around_the_cut(n, most, page, bits):
     log(f"mx attention: {bits} bits, {n} requests of at most {most} keys, pages of {page}")
@@ -227,6 +227,20 @@ def test_short_requests_around_the_cut(n, most, page, bits):
     lens[:3], lens[n - 1] = [33, 257, 0], most
     c = Cache(lens, np.ones(n, dtype=np.int64), 4, 2, 128, page, "bf16", seed=n, bits=bits)
     c.check(c.call(), only=[0, 1, 2, n // 2, n - 1])
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("page", [16, 20])
+@pytest.mark.parametrize("new,dim", [([5, 3, 4], 128), ([8, 1, 2], 64), ([1, 90, 1, 7], 128),
+                                     ([1, 1, 40, 0, 2], 64)])
+def test_long_requests_are_cut(new, dim, page, bits):
+    """Requests long enough for a call to be cut into runs and joined: one tile of rows
+    and two, alone and beside chunks."""
+    log(f"mx attention: {bits} bits, new {new} over 2600, width {dim}, pages of {page}")
+    lens = [2600 + 300 * i for i in range(len(new))]
+    lens[0] = 70
+    c = Cache(lens, new, 32, 8, dim, page, "bf16", seed=dim + page, bits=bits)
+    c.check(c.call(), [0, 1, 4, 7, 39, 89])
 
 
 @pytest.mark.parametrize("new", [[1, 1, 0, 1], [70, 1, 0, 40]])
@@ -263,7 +277,7 @@ def test_given_results_and_workspaces():
     args = (c.q, *c.tensors(), *c.arguments(), 2, 3000)
     want = pair.paged_attention_mx(*args, want_lse=True)
     need = pair.pair_paged_attention_mx_workspace_bytes(2, 3, 8, 2, 128, pair.PAIR_MXFP4, 2, 3000)
-    assert need > 256
+    assert need > 256                    # cut
     for out in (None, torch.full_like(c.q, 7.0)):
         for size in (None, 256, need, need + 4096):
             ws = None if size is None else torch.full((size,), 255, dtype=torch.uint8, device=DEV)
