@@ -730,7 +730,8 @@ typedef struct pair_mx_cache {
  *                h * new_head_stride + d (the same strides for both, in elements,
  *                multiples of 8; bases 16-byte aligned)
  *   cache        HOST struct, read during the call; its rows share no byte
- *                (PAIR_EINVAL), nor do its four arrays
+ *                (PAIR_EINVAL), with those of its other arrays and of k and v
+ *                neither (an array may lie between another's rows)
  * Device status: PAIR_ST_PAGES (a slot beyond the cache; it is skipped),
  * PAIR_ST_NONFINITE (a block was stored as NaN).
  */
@@ -747,8 +748,8 @@ int pair_cache_store_mx(const pair_mx_cache* cache, int64_t tokens, int32_t dtyp
  *                slot any number of times; zeros where the slot is negative
  *   dtype        PAIR_BF16 or PAIR_F16, of k and v
  *   k, v         out: element d of head h of row t at t * token_stride +
- *                out_head_stride * h + d (strides and bases as above; rows share no
- *                element: PAIR_EINVAL)
+ *                out_head_stride * h + d (strides and bases as above; rows of both
+ *                share no byte, and none with the cache: PAIR_EINVAL)
  * Device status: PAIR_ST_PAGES (a slot beyond the cache; its row is zeros).
  */
 int pair_cache_load_mx(const pair_mx_cache* cache, int64_t tokens, const int64_t* slots,

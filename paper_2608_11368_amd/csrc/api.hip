@@ -86,6 +86,68 @@ bool rows_overlap(Strided (&dims)[N], int64_t width) {
   return false;
 }
 
+// Rows of `width` bytes at all multiples of the strides, in bytes, from `at` on.
+struct Rows {
+  const void* at;
+  int64_t width;
+  Strided dims[3];
+};
+
+// Steps of a distance between two rows: j * stride, least <= j <= most.
+struct Steps {
+  int64_t stride, least, most;
+};
+
+// Whether some choice of a step of each (those of `n`, by falling stride) brings a
+// distance x to -before < x < after.  For nested arrays two or three steps of a stride
+// come near at most; a search that `left` more steps do not end counts as a yes.
+bool comes_near(const Steps* s, int n, __int128 x, int64_t before, int64_t after, int* left) {
+  if (n == 0) return -before < x && x < after;
+  __int128 low = 0, high = 0;                     // of the further steps together
+  for (int k = 1; k < n; ++k) {
+    low += (__int128)s[k].least * s[k].stride;
+    high += (__int128)s[k].most * s[k].stride;
+  }
+  auto floor_div = [&](__int128 a) {
+    const __int128 q = a / s->stride;
+    return q * s->stride > a ? q - 1 : q;
+  };
+  __int128 j = floor_div(-before - x - high) + 1, last = floor_div(after - 1 - x - low);
+  if (j < s->least) j = s->least;
+  if (last > s->most) last = s->most;
+  for (; j <= last; ++j)
+    if (--*left < 0 || comes_near(s + 1, n - 1, x + j * s->stride, before, after, left)) return true;
+  return false;
+}
+
+// Whether two arrays of rows share bytes; arrays that lie between each other's rows
+// (a page's keys, values and scales side by side, say) do not.
+bool share_bytes(const Rows& a, const Rows& b) {
+  Steps steps[6];
+  int n = 0;
+  auto add = [&](int64_t stride, int64_t least, int64_t most) {
+    if (stride > 0 && least < most) steps[n++] = {stride, least, most};
+  };
+  __int128 a_bytes = a.width, b_bytes = b.width;
+  for (int k = 0; k < 3; ++k) {
+    const Strided &x = a.dims[k], &y = b.dims[k];
+    if (x.count > 1) a_bytes += (__int128)(x.count - 1) * x.stride;
+    if (y.count > 1) b_bytes += (__int128)(y.count - 1) * y.stride;
+    if (x.stride == y.stride) {
+      add(x.stride, 1 - x.count, y.count - 1);
+    } else {
+      add(x.stride, 1 - x.count, 0);
+      add(y.stride, 0, y.count - 1);
+    }
+  }
+  const __int128 apart = (__int128)reinterpret_cast<uintptr_t>(b.at) -
+                         (__int128)reinterpret_cast<uintptr_t>(a.at);
+  if (apart >= a_bytes || -apart >= b_bytes) return false;
+  std::sort(steps, steps + n, [](const Steps& x, const Steps& y) { return x.stride > y.stride; });
+  int left = 4096;
+  return comes_near(steps, n, apart, b.width, a.width, &left);
+}
+
 hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }
 
 }  // namespace
@@ -579,6 +641,26 @@ static int check_mx(const pair_mx_cache* c, pair::MxCache* out) {
   return PAIR_OK;
 }
 
+// The cache's arrays, as the checks of overlaps see them.
+static void mx_arrays(const pair::MxCache& c, Rows (&to)[4]) {
+  const Rows codes = {nullptr, c.dim * c.bits / 8,
+                      {{c.n_pages, c.page_stride}, {c.page, c.slot_stride}, {c.kv_heads, c.head_stride}}};
+  const Rows scales = {nullptr, c.dim / 32,
+                       {{c.n_pages, c.scale_page}, {c.page, c.scale_slot}, {c.kv_heads, c.scale_head}}};
+  to[0] = to[1] = codes;
+  to[2] = to[3] = scales;
+  to[0].at = c.k;
+  to[1].at = c.v;
+  to[2].at = c.k_scale;
+  to[3].at = c.v_scale;
+}
+
+// The 16-bit rows of `at` that a call moves.
+static Rows half_rows(const pair::MxCache& c, const void* at, int64_t tokens, int64_t token_stride,
+                      int64_t head_stride) {
+  return {at, 2 * c.dim, {{tokens, 2 * token_stride}, {1, 0}, {c.kv_heads, 2 * head_stride}}};
+}
+
 // The 16-bit rows that a call of an mx cache moves.
 static int check_rows(int64_t tokens, const void* k, const void* v, int64_t token_stride,
                       int64_t head_stride, const int64_t* slots) {
@@ -604,10 +686,15 @@ int pair_cache_store_mx(const pair_mx_cache* cache, int64_t tokens, int32_t dtyp
   Strided codes[] = {{c.n_pages, c.page_stride}, {c.page, c.slot_stride}, {c.kv_heads, c.head_stride}};
   Strided scales[] = {{c.n_pages, c.scale_page}, {c.page, c.scale_slot}, {c.kv_heads, c.scale_head}};
   if (rows_overlap(codes, c.dim * c.bits / 8) || rows_overlap(scales, c.dim / 32)) return PAIR_EINVAL;
-  const void* arrays[] = {c.k, c.v, c.k_scale, c.v_scale};
-  for (int i = 0; i < 4; ++i)
+  Rows arrays[4];
+  mx_arrays(c, arrays);
+  for (int i = 0; i < 4; ++i) {
     for (int j = 0; j < i; ++j)
-      if (arrays[i] == arrays[j]) return PAIR_EINVAL;
+      if (share_bytes(arrays[j], arrays[i])) return PAIR_EINVAL;
+    for (const void* from : {k, v})
+      if (share_bytes(half_rows(c, from, tokens, token_stride, new_head_stride), arrays[i]))
+        return PAIR_EINVAL;
+  }
   return pair::launch_mx_move(true, c, tokens, dtype == PAIR_BF16, const_cast<void*>(k),
                               const_cast<void*>(v), token_stride, new_head_stride, slots, d_status,
                               as_stream(stream));
@@ -625,7 +712,14 @@ int pair_cache_load_mx(const pair_mx_cache* cache, int64_t tokens, const int64_t
   st = check_rows(tokens, k, v, token_stride, out_head_stride, slots);
   if (st) return st;
   Strided rows[] = {{tokens, token_stride}, {c.kv_heads, out_head_stride}};
-  if (rows_overlap(rows, c.dim) || k == v) return PAIR_EINVAL;
+  if (rows_overlap(rows, c.dim)) return PAIR_EINVAL;
+  const Rows out[] = {half_rows(c, k, tokens, token_stride, out_head_stride),
+                      half_rows(c, v, tokens, token_stride, out_head_stride)};
+  if (share_bytes(out[0], out[1])) return PAIR_EINVAL;
+  Rows arrays[4];
+  mx_arrays(c, arrays);
+  for (const Rows& a : arrays)
+    if (share_bytes(out[0], a) || share_bytes(out[1], a)) return PAIR_EINVAL;
   return pair::launch_mx_move(false, c, tokens, dtype == PAIR_BF16, k, v, token_stride,
                               out_head_stride, slots, d_status, as_stream(stream));
 }
