@@ -248,7 +248,8 @@ __device__ __forceinline__ void weigh_block(const RowArgs& s, const f32x4_t (&sc
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int w = 0; w < 4; ++w) pf[nt][w] = pack2<BF16>(p[nt][2 * w], p[nt][2 * w + 1]);
+    for (int w = 0; w < 4; ++w)
+      pf[nt][w] = nt < tiles ? pack2<BF16>(p[nt][2 * w], p[nt][2 * w + 1]) : 0u;
   // Values that some row must not see: past the end they are no values at
   // all, and within the chunk a weight of zero does not hide a NaN or an
   // infinity from the matrix product.
