@@ -1,5 +1,7 @@
 // Attention of a few new tokens per request: the launches, and the joining of
 // requests that were cut (attn_rows.hpp has the kernel's body).
+#include <type_traits>
+
 #include "attn_rows.hpp"
 
 namespace pair {
@@ -8,11 +10,16 @@ using namespace rows;
 
 namespace {
 
+// Rows that a workgroup joins side by side where it has several.
+constexpr int kJoined = kWaves;
+
 // Joins the partial sums of the requests that were cut: a workgroup per request and
-// head, or several that take its rows in turn.  The parts' maxima first, a lane each,
-// then their sums with several parts' loads in flight.
+// head, or several that take its rows in turn, one or kJoined at a time.  First a row's
+// parts' maxima and weights, a wave for each row, a lane for each part, then the parts'
+// sums with several loads in flight.
 template <bool BF16, int DIM>
-__global__ __launch_bounds__(kThreads) void join_rows_kernel(RowArgs s, int rows_slot) {
+__global__ __launch_bounds__(kThreads) void join_rows_kernel(RowArgs s, int rows_slot,
+                                                             int rows_turn) {
   const int64_t heads = s.a.kv_heads;
   const int64_t r = blockIdx.x / (uint32_t)s.a.kv_heads;
   const int kvh = (int)(blockIdx.x - r * heads);
@@ -28,61 +35,89 @@ __global__ __launch_bounds__(kThreads) void join_rows_kernel(RowArgs s, int rows
   const int rows = q.tokens * (int)s.group.d;
   const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
   constexpr int PER = DIM / kWave;
-  __shared__ float weight[kMostRuns], sum[kWaves][DIM];
+  __shared__ float weight[kMostRuns][kJoined], sum[kWaves][kJoined][DIM], stat[kJoined][2];
   const int parts = (int)(w1 - w0) + 1;
   // a request that starts inside a run is in the run's second part
   const int64_t first = 2 * w0 + (run_start(units, runs, w0) != u0 ? 1 : 0);
-  for (int i = blockIdx.y; i < rows; i += gridDim.y) {
-    const int tok = (int)div_by((uint32_t)i, s.group);
-    const int h = kvh * (int)s.group.d + i - tok * (int)s.group.d;
-    auto place = [&](int p) {
-      return ((p == 0 ? first : 2 * (w0 + p)) * heads + kvh) * rows_slot + i;
+  for (int i0 = blockIdx.y * rows_turn; i0 < rows; i0 += gridDim.y * rows_turn) {
+    const int count = rows - i0 < rows_turn ? rows - i0 : rows_turn;
+    auto place = [&](int p) {            // of row i0
+      return ((p == 0 ? first : 2 * (w0 + p)) * heads + kvh) * rows_slot + i0;
     };
-    float m = -INFINITY;
-    for (int p = lane; p < parts; p += kWave) m = fmaxf(m, s.part_ml[place(p) * 2]);
+    if (wave < count) {
+      float m = -INFINITY;
+      for (int p = lane; p < parts; p += kWave) m = fmaxf(m, s.part_ml[(place(p) + wave) * 2]);
 #pragma unroll
-    for (int by = 1; by < kWave; by <<= 1) m = fmaxf(m, __shfl_xor(m, by, kWave));
-    const float base = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f;
-    for (int p = lane; p < parts; p += kWave) {
-      const float mp = s.part_ml[place(p) * 2], lp = s.part_ml[place(p) * 2 + 1];
-      const bool none = mp == -INFINITY && lp == 0.0f;       // saw no key
-      const float f = none ? 0.0f : __builtin_amdgcn_exp2f(mp - base);
-      l += none ? 0.0f : lp * f;
-      if (wave == 0) weight[p] = f;
+      for (int by = 1; by < kWave; by <<= 1) m = fmaxf(m, __shfl_xor(m, by, kWave));
+      const float base = m == -INFINITY ? 0.0f : m;
+      float l = 0.0f;
+      for (int p = lane; p < parts; p += kWave) {
+        const int64_t at = (place(p) + wave) * 2;
+        const float mp = s.part_ml[at], lp = s.part_ml[at + 1];
+        const bool none = mp == -INFINITY && lp == 0.0f;       // saw no key
+        const float f = none ? 0.0f : __builtin_amdgcn_exp2f(mp - base);
+        l += none ? 0.0f : lp * f;
+        weight[p][wave] = f;
+      }
+      l = wave_sum(l);
+      if (lane == 0) {
+        stat[wave][0] = m;
+        stat[wave][1] = l;
+      }
     }
-    l = wave_sum(l);
     __syncthreads();
-    float o[PER];
+    auto add = [&](auto rows_now) {      // a wave's share of the parts
+      constexpr int N = decltype(rows_now)::value;
+      float o[N][PER];
 #pragma unroll
-    for (int e = 0; e < PER; ++e) o[e] = 0.0f;
+      for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int e = 0; e < PER; ++e) o[k][e] = 0.0f;
 #pragma unroll 4
-    for (int p = wave; p < parts; p += kWaves) {
-      const float f = weight[p];
-      const float* from = s.part_o + place(p) * DIM;
+      for (int p = wave; p < parts; p += kWaves) {
+        const float* from = s.part_o + place(p) * DIM;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) o[e] = __builtin_fmaf(from[e * kWave + lane], f, o[e]);
-    }
+        for (int k = 0; k < N; ++k)
 #pragma unroll
-    for (int e = 0; e < PER; ++e) sum[wave][e * kWave + lane] = o[e];
+          for (int e = 0; e < PER; ++e)
+            o[k][e] = __builtin_fmaf(from[k * DIM + e * kWave + lane], weight[p][k], o[k][e]);
+      }
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int e = 0; e < PER; ++e) sum[wave][k][e * kWave + lane] = o[k][e];
+    };
+    static_assert(kJoined == 4, "the cases");
+    if (count == 1)
+      add(std::integral_constant<int, 1>());
+    else if (count == 2)
+      add(std::integral_constant<int, 2>());
+    else if (count == 3)
+      add(std::integral_constant<int, 3>());
+    else
+      add(std::integral_constant<int, 4>());
     __syncthreads();
-    if (threadIdx.x < DIM / 2) {
-      const int d = threadIdx.x * 2;
+    const int k = (int)threadIdx.x / (DIM / 2);
+    if (k < count) {
+      const int d = ((int)threadIdx.x - k * (DIM / 2)) * 2;
+      const int tok = (int)div_by((uint32_t)(i0 + k), s.group);
+      const int h = kvh * (int)s.group.d + i0 + k - tok * (int)s.group.d;
       float a = 0.0f, b = 0.0f;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        a += sum[w][d];
-        b += sum[w][d + 1];
+        a += sum[w][k][d];
+        b += sum[w][k][d + 1];
       }
       const bool none = limit_of(q, tok) < 0;
+      const float m = stat[k][0], l = stat[k][1];
       const float inv = 1.0f / l;
       *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(s.a.out) + (q.q0 + tok) * s.a.out_token +
                                    h * s.a.out_head + d) =
           none ? 0u : pack2<BF16>(a * inv, b * inv);
-      if (s.a.lse != nullptr && threadIdx.x == 0)
+      if (s.a.lse != nullptr && d == 0)
         s.a.lse[(q.q0 + tok) * s.a.q_heads + h] = none ? -INFINITY : log_sum<BF16>(m, l);
     }
-    __syncthreads();                     // the next row's weights and sums
+    __syncthreads();                     // the next rows' weights and sums
   }
 }
 
@@ -133,15 +168,23 @@ RowArgs rows::args_of(const AttnCall& a, const Plan& p, void* workspace) {
 
 int rows::join_rows(const RowArgs& s, const Plan& p, hipStream_t stream) {
   if (p.runs == 0) return PAIR_OK;
-  // About eight workgroups a compute unit: most find their request uncut, and each takes
-  // a chain of loads and divisions for that (72 requests of which 64 have two rows and
-  // none over 32, 8 heads: 14 us with a workgroup for each of 32 rows, 5 so).
-  const int64_t each = s.a.n * s.a.kv_heads;
-  int64_t turns = 8 * (int64_t)device_cu_count() / each;
-  if (turns > p.rows) turns = p.rows;
+  // A workgroup for each row while those are at most 16 a compute unit.  Beyond, most
+  // find their request uncut, and each takes a chain of loads and divisions for that:
+  // about 16 a compute unit, for kJoined rows at a time.  2000 requests, one of 60,000
+  // keys among those of 100, with 32 rows each on a key head of 64: 74 us with a workgroup
+  // for each row, 149 with one for all, row by row, 59 so; 256 on 8 heads of 128, 146,
+  // 196 and 130; 2000 of 1200 keys on 8 heads of 64, 1284 and 1065.  (72 requests of which
+  // 64 have two rows and none over 32, 8 heads: the joins take 14 us with a workgroup for
+  // each of 32 rows, 5 so.)
+  const int64_t each = s.a.n * s.a.kv_heads, most = 16 * (int64_t)device_cu_count();
+  const int rows_turn = each * p.rows <= most ? 1 : kJoined;
+  int64_t turns = most / each;
+  const int all = (p.rows + rows_turn - 1) / rows_turn;
+  if (turns > all) turns = all;
   const dim3 grid((unsigned)each, (unsigned)(turns < 1 ? 1 : turns));
 #define PAIR_JOIN(BF16, DIM)                                                                     \
-  hipLaunchKernelGGL((join_rows_kernel<BF16, DIM>), grid, dim3(kThreads), 0, stream, s, 16 * p.tiles)
+  hipLaunchKernelGGL((join_rows_kernel<BF16, DIM>), grid, dim3(kThreads), 0, stream, s, 16 * p.tiles, \
+                     rows_turn)
   if (s.a.dim == 64) {
     if (s.a.bf16) PAIR_JOIN(true, 64); else PAIR_JOIN(false, 64);
   } else {
