@@ -133,11 +133,21 @@ Plan rows::plan_of(int64_t n, int32_t q_heads, int32_t kv_heads, int32_t dim, in
   // eight steps, which take less than the second launch would (4 requests of 700
   // keys: 8.0 us uncut, 9.5 us cut; of 1000: 9.3 and 9.9; of 2000: 21 and 11; 32
   // requests of 1000: 22 and 27), or the requests are so many that they fill the
-  // card by themselves.  In 8 and 4 bits 16 steps, with the next block on its way: in 8
-  // bits, 8 heads of 128, uncut and cut, 4 requests of 1500 keys 15.7 and 16.0 us, 16
-  // 16.5 and 21, 64 36 and 42, 128 68 and 76, 256 of 300 41 and 52; five tokens of 64
-  // 43 and 63.  (32 steps: 256 of 1000, up to 4000, 97 and 100, of two heads 41 and 37.)
-  const int whole = bits == 16 ? 8 : 16;
+  // card by themselves.
+  // In 8 and 4 bits 16 steps, with the next block on its way: in 8 bits, 8 heads of
+  // 128, uncut and cut, 16 requests of 1500 keys 16.5 and 21 us, 64 36 and 42, 128 68 and
+  // 76, 256 of 300 41 and 52; five tokens of 64 43 and 63.  (32 steps: 256 of 1000, up to
+  // 4000, 97 and 100, of two heads 41 and 37.)  But 12 where at most 32 workgroups leave
+  // the card idle and a step is long: rows of 128 bytes (of 1640 to 2048 keys, a token of 2
+  // requests 17.0 and 12.4, of 4 16.8 and 14.0; of 920 to 1150 12.1 and 13.0), or two tiles
+  // of rows, whose next block is not on its way (eight tokens of 2 22.9 and 15.5, of 4 23.7
+  // and 20.3; in 4 bits 22.0 and 17.2, 22.0 and 20.6; 3 tokens beside a chunk of 500 over
+  // 2000 keys 46 and 38).  Else the second launch takes what the cut gains (one tile of 4
+  // requests in 4 bits 15.7 and 15.3, of 64 elements 13.5 and 14.9; eight tokens of 64
+  // requests, one head, 25 and 30).
+  int whole = 8;
+  if (bits != 16)
+    whole = n * kv_heads <= 32 && (p.tiles == 2 || bits * dim == 1024) ? 12 : 16;
   const int64_t most = n * ((max_len + kUnit - 1) / kUnit);
   const int per_cu = p.tiles == 1 ? groups_per_cu(bits, dim) : 2;
   int64_t runs = per_cu * (int64_t)device_cu_count() / kv_heads;
