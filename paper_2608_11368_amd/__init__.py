@@ -537,6 +537,11 @@ def _function(name):
     return at
 
 
+def _steps(t):
+    """The strides that a tensor's elements are found by: none where there is one."""
+    return [s if n > 1 else 0 for n, s in zip(t.shape, t.stride())]
+
+
 def _mx_refused(k_cache, v_cache, k_scale, v_scale, **tensors):
     """Why the native call took no such tensors: raises, or returns the heads' width
     where the caches and their devices are as they should be."""
@@ -554,7 +559,7 @@ def _mx_refused(k_cache, v_cache, k_scale, v_scale, **tensors):
     if k_scale.shape[:3] != k_cache.shape[:3] or k_scale.shape[3] * 32 != dim:
         raise ValueError(f"rows of {dim} elements need a scale for every 32 of them, got "
                          f"{tuple(k_scale.shape)} for {tuple(k_cache.shape)}")
-    if (v_cache.stride() != k_cache.stride() or v_scale.stride() != k_scale.stride()
+    if (_steps(v_cache) != _steps(k_cache) or _steps(v_scale) != _steps(k_scale)
             or k_cache.stride(3) != 1 or (k_scale.stride(3) != 1 and k_scale.shape[3] > 1)):
         raise ValueError("keys and values must have the same strides and contiguous rows")
     for name, t in (*cache, *tensors.items()):     # kernels run on the current device's stream
@@ -576,7 +581,7 @@ def _move_refused(k, v, slots, cache, d_status):
     dim = _mx_refused(*cache, k=k, v=v, slots=slots, d_status=d_status)
     _half_rows(k, "k", None, cache[0].shape[2], dim)
     _half_rows(v, "v", k.dtype, cache[0].shape[2], dim)
-    if v.stride() != k.stride() or v.shape != k.shape:
+    if _steps(v) != _steps(k) or v.shape != k.shape:
         raise ValueError("k and v must have the same shape and strides")
     _native().address(slots, "slots", torch.int64, k.shape[0])
     _native().address(d_status, "d_status", torch.int32, 1, True)

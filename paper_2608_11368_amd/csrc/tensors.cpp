@@ -150,6 +150,16 @@ PyObject* cache(PyObject*, PyObject* const* args, Py_ssize_t n) {
   }
 }
 
+// The stride of a dimension, 0 where there is nothing to step over: such a one is
+// whatever the slice that made it left.
+int64_t step(const at::Tensor& t, int64_t d) { return t.size(d) > 1 ? t.stride(d) : 0; }
+
+bool same_steps(const at::Tensor& a, const at::Tensor& b) {
+  for (int64_t d = 0; d < a.dim(); ++d)
+    if (step(a, d) != step(b, d)) return false;
+  return true;
+}
+
 // The four tensors of a cache in 8 or 4 bits on `device` as the C ABI's struct.
 bool mx_struct(PyObject* const* args, int device, pair_mx_cache* c) {
   for (int i = 0; i < 4; ++i)
@@ -160,8 +170,8 @@ bool mx_struct(PyObject* const* args, int device, pair_mx_cache* c) {
   if (!k.is_cuda() || !v.is_cuda() || !ks.is_cuda() || !vs.is_cuda() || k.dim() != 4 ||
       (!wide && k.scalar_type() != at::kFloat4_e2m1fn_x2) || v.scalar_type() != k.scalar_type() ||
       ks.scalar_type() != at::kFloat8_e8m0fnu || vs.scalar_type() != at::kFloat8_e8m0fnu ||
-      v.sizes() != k.sizes() || v.strides() != k.strides() || ks.dim() != 4 ||
-      vs.sizes() != ks.sizes() || vs.strides() != ks.strides() || k.stride(3) != 1 ||
+      v.sizes() != k.sizes() || !same_steps(v, k) || ks.dim() != 4 || vs.sizes() != ks.sizes() ||
+      !same_steps(vs, ks) || k.stride(3) != 1 ||
       (ks.stride(3) != 1 && ks.size(3) > 1) || k.get_device() != device ||
       v.get_device() != device || ks.get_device() != device || vs.get_device() != device)
     return false;
@@ -173,12 +183,12 @@ bool mx_struct(PyObject* const* args, int device, pair_mx_cache* c) {
   c->v = v.data_ptr();
   c->k_scale = ks.data_ptr();
   c->v_scale = vs.data_ptr();
-  c->page_stride = k.stride(0);
-  c->slot_stride = k.stride(1);
-  c->head_stride = k.stride(2);
-  c->scale_page = ks.stride(0);
-  c->scale_slot = ks.stride(1);
-  c->scale_head = ks.stride(2);
+  c->page_stride = step(k, 0);
+  c->slot_stride = step(k, 1);
+  c->head_stride = step(k, 2);
+  c->scale_page = step(ks, 0);
+  c->scale_slot = step(ks, 1);
+  c->scale_head = step(ks, 2);
   c->n_pages = k.size(0);
   c->page = (int32_t)k.size(1);
   c->kv_heads = (int32_t)k.size(2);
@@ -214,7 +224,7 @@ bool half_rows(PyObject* x, int32_t code, int64_t heads, int64_t width, int devi
       (code != 0 && dtype_code(t.scalar_type()) != code) || t.size(2) != width ||
       t.stride(2) != 1 || (heads != 0 && t.size(1) != heads))
     return false;
-  *r = {t.data_ptr(), t.stride(0), t.stride(1), t.size(0), t.size(1), dtype_code(t.scalar_type())};
+  *r = {t.data_ptr(), step(t, 0), step(t, 1), t.size(0), t.size(1), dtype_code(t.scalar_type())};
   return true;
 }
 
