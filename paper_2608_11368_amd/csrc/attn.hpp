@@ -129,7 +129,7 @@ __device__ __forceinline__ int32_t checked_page(const AttnCall& a, int32_t id, i
 // a query head of a token) and attn_tiles.hpp (those of at least `least_rows`;
 // with a workspace for the others, both).  32 rows of 8 heads of 128, by the first
 // and by the second: 2 requests of 131,000 keys 187 and 207 us, 256 of 1000 200 and
-// 215, 32 of 4000 112 and 104.  Of 40 and 64 rows, for which only tiles are built:
+// 215, 32 of 4000 105 and 104.  Of 40 and 64 rows, for which only tiles are built:
 // 209 and 231, 222 and 233, 105 and 109.
 constexpr int kRowsMost = 32;
 

@@ -39,8 +39,8 @@
 // Over a cache in 8 or 4 bits codes come from memory 16 bytes a lane and are converted
 // on their way into LDS, which costs what the smaller loads save: three chunks of 1501
 // to 2048 tokens after 4000 to 8000 keys at width 128 970 TFLOP/s in 8 bits, 975 in 4,
-// eight of 1000 to 2048 after 16,000 1045; 8 prompts of 301 to 4096 (16 on 4) at width
-// 64 700.
+// eight of 1000 to 2048 after 16,000 1045; at width 64 the three 840 and 870, 8 prompts of
+// 301 to 4096 (16 on 4) 680 and 690 to 740 (8 bits there: 4 registers spilled).
 #pragma once
 
 #include <type_traits>
