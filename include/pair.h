@@ -729,9 +729,9 @@ typedef struct pair_mx_cache {
  *   k, v         element d of head h of row t at t * token_stride +
  *                h * new_head_stride + d (the same strides for both, in elements,
  *                multiples of 8; bases 16-byte aligned)
- *   cache        HOST struct, read during the call; its rows share no byte
- *                (PAIR_EINVAL), with those of its other arrays and of k and v
- *                neither (an array may lie between another's rows)
+ *   cache        HOST struct, read during the call; its rows share no byte with
+ *                each other, those of its other arrays, k or v (PAIR_EINVAL; an
+ *                array may lie between another's rows)
  * Device status: PAIR_ST_PAGES (a slot beyond the cache; it is skipped),
  * PAIR_ST_NONFINITE (a block was stored as NaN).
  */
